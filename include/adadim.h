@@ -348,6 +348,86 @@ int adadim_gemv_ic_meta16(adadim_ctx* ctx, const uint32_t* packed, const uint16_
                           int64_t out, int64_t in, int bits, int group, void* y);
 
 /*
+ * Microscaled 4-bit values ("mx4"): blocks of 32 consecutive values of a row share one power of two, kept in a byte as
+ * its exponent + 127 (255: NaN); each value is a 4-bit float: sign, two bits of exponent, one of mantissa, the magnitudes
+ * 0, .5, 1, 1.5, 2, 3, 4, 6.  4.25 bits per value, multiplied by gfx950's matrix cores as they are.
+ * A row is held in pieces of 128 values, 64 bytes of codes and a word of four scale bytes:
+ *   codes   u8 [rows, 64*pieces], pieces = ceil(cols/128); value 2i of a row in the low half of byte i; 16-byte aligned
+ *   scales  u8 [pieces, rows, 4]: the words of a piece side by side for all rows; 4-byte aligned
+ * The last piece is filled up with codes 0 and scale bytes 127 (2^0), by whoever writes it: the products read whole pieces.
+ * adadim_mx4_code_bytes / _scale_bytes give the sizes of the two arrays.
+ */
+#define ADADIM_TYPE_F16  0
+#define ADADIM_TYPE_BF16 1
+#define ADADIM_TYPE_F32  2
+#define ADADIM_TYPE_MX4  3
+int64_t adadim_mx4_code_bytes(int64_t rows, int64_t cols);
+int64_t adadim_mx4_scale_bytes(int64_t rows, int64_t cols);
+
+/*
+ * Rows to mx4.  Per block, amax its largest magnitude: e = floor(log2 amax) - 2, at least -127 (0 if amax = 0); each value the
+ * nearest magnitude to |x| / 2^e with the sign of x, ties to the one with mantissa 0, at most 6 (what lies in
+ * (6, 8) 2^e is cut to 6).  A block that holds an infinity or a NaN gets the scale NaN and codes 0.
+ *   X       [rows, cols] of x_type F16, BF16 or F32, row pitch ldx >= cols in elements; any alignment of an element
+ *   dW      optional [rows, cols], X minus the value stored, one rounding: F32, F16 or F16_SCALED as in adadim_quantize
+ *           (colscale fp32 [cols] with F16_SCALED), so that a layer's mx4 form is scored beside its per-OC and per-IC ones
+ * rows may be 0.
+ */
+int adadim_mx4_quantize(adadim_ctx* ctx, const void* X, int x_type, int64_t rows, int64_t cols, int64_t ldx, uint8_t* codes,
+                        uint8_t* scales, void* dW, int dW_dtype, const float* colscale);
+
+/* The values of mx4 rows: Y [rows, cols] of y_type F16, BF16 or F32, pitch ldy.  Exact in F32 and BF16 (down to the subnormals of 2^-133,
+ * up to their largest number); in F16 for scales of 2^-23 to 2^13, rounded to nearest beyond. */
+int adadim_mx4_dequantize(adadim_ctx* ctx, const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, void* Y, int y_type,
+                          int64_t ldy);
+
+/*
+ * Y = X W^T with W [out, in] in mx4 (codes, scales as above).
+ *   X       [tokens, in]: F16 or BF16 with pitch ldx, or MX4: X its codes, x_scales its scales, ldx ignored
+ *   Y       [tokens, out] of y_type F16, BF16 or F32, pitch ldy
+ * Products are exact (a weight outside fp16's range meets fp16 activations as bf16 in two parts), sums are fp32 on the
+ * matrix cores in a fixed order (the same bits every run; the order depends on the sizes), rounded once.  tokens may be 0.
+ */
+int adadim_mx4_matmul(adadim_ctx* ctx, const void* X, const uint8_t* x_scales, int x_type, int64_t tokens, int64_t ldx,
+                      const uint8_t* codes, const uint8_t* scales, int64_t out, int64_t in, void* Y, int y_type, int64_t ldy);
+
+/*
+ * The same with one weight per expert and the rows of Y in groups: row r with offsets[e] <= r < offsets[e+1] is
+ * Y[r] = X[rows[r]] W_e^T.  The host never learns how long the groups are.
+ *   codes u8 [experts, out, 64*pieces], scales u8 [experts, pieces, out, 4]
+ *   offsets  int32 [experts + 1], device: not decreasing, inside [0, n_rows] (values outside are taken as the nearer end).
+ *            Groups may be empty.  Rows of Y in no group are not written.
+ *   rows     int32 [n_rows], device, or NULL: row r of X (then tokens == n_rows).  An entry outside [0, tokens) stands for a row of zeros.
+ *   experts  1..1024
+ */
+int adadim_mx4_matmul_experts(adadim_ctx* ctx, const void* X, const uint8_t* x_scales, int x_type, int64_t tokens, int64_t ldx,
+                              const int32_t* rows, int64_t n_rows, const int32_t* offsets, int experts, const uint8_t* codes,
+                              const uint8_t* scales, int64_t out, int64_t in, void* Y, int y_type, int64_t ldy);
+
+/*
+ * A router's scores to the k experts of each token and the rows sorted by expert.
+ *   logits   [tokens, experts] of type F16, BF16 or F32, pitch ldl
+ *   chosen   int32 [tokens, k]: the k largest scores, largest first, of equal ones the lowest index first.  -infinity (a mask)
+ *            and NaN are never chosen; a token with fewer than k others has -1 in the places left.
+ *   weights  fp32 [tokens, k]: exp(l - max) over the sum of these over the chosen (renormalize = 1) or over all experts (0); scores
+ *            of +infinity share evenly among themselves; 0 where chosen is -1
+ *   offsets  int32 [experts + 1], rows int32 [tokens * k], for adadim_mx4_matmul_experts: rows offsets[e] .. offsets[e+1] are
+ *            the tokens that chose e, in their order; -1 behind offsets[experts]
+ *   slots    int32 [tokens, k]: the place of (token, choice) in rows; -1 where chosen is -1
+ * experts 1..1024, k 1..32.  With tokens = 0 only offsets are written (zeros).
+ */
+int adadim_expert_route(adadim_ctx* ctx, const void* logits, int type, int64_t tokens, int64_t ldl, int experts, int k, int renormalize,
+                        int32_t* chosen, float* weights, int32_t* offsets, int32_t* rows, int32_t* slots);
+
+/*
+ * Y[t] = sum_j weights[t, j] Z[slots[t, j]], fp32 in the order of j, rounded once: the experts' rows back to their tokens.
+ *   Z  [n_rows, cols] of z_type, pitch ldz;  Y [tokens, cols] of y_type, pitch ldy;  both F16, BF16 or F32
+ *   slots  a place outside [0, n_rows) adds nothing (its row of Z is not read); a token without any is a row of zeros.  k 1..1024.
+ */
+int adadim_expert_combine(adadim_ctx* ctx, const void* Z, int z_type, int64_t n_rows, int64_t cols, int64_t ldz, const int32_t* slots,
+                          const float* weights, int64_t tokens, int k, void* Y, int y_type, int64_t ldy);
+
+/*
  * Recording a sequence of calls as one HIP graph.  A layer's search is a dozen short kernels; launched one by
  * one the gaps between them are a tenth of the step on a 4096 x 4096 layer, replayed as a graph they close.
  *   adadim_capture_begin  starts recording on the context's stream, which must not be the default

@@ -16,6 +16,8 @@ LIB_PATH = os.path.join(_HERE, "libadadim.so")
 OK, EINVAL, ENULL, EALIGN, EHIP = 0, -1, -2, -3, -4
 DIM_OC, DIM_IC = 0, 1
 DW_F32, DW_F16, DW_F16_SCALED = 0, 1, 2
+TYPE_F16, TYPE_BF16, TYPE_F32, TYPE_MX4 = 0, 1, 2, 3
+_TYPES = {"torch.float16": TYPE_F16, "torch.bfloat16": TYPE_BF16, "torch.float32": TYPE_F32}
 
 EXPORTS = (
     "adadim_create", "adadim_destroy", "adadim_last_error", "adadim_version", "adadim_score_elems",
@@ -27,6 +29,8 @@ EXPORTS = (
     "adadim_profile", "adadim_profile_only", "adadim_profile_read", "adadim_profile_read_spread",
     "adadim_probe_gram_timeline", "adadim_probe_gemv_read",
     "adadim_layer_error_batch_select_noalloc", "adadim_noalloc_scratch_bytes", "adadim_probe_mfma", "adadim_probe_mfma_f64",
+    "adadim_mx4_code_bytes", "adadim_mx4_scale_bytes", "adadim_mx4_quantize", "adadim_mx4_dequantize", "adadim_mx4_matmul",
+    "adadim_mx4_matmul_experts", "adadim_expert_route", "adadim_expert_combine",
 )
 
 _lib = None
@@ -154,6 +158,17 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
     lib.adadim_gptq_quantize_meta16.argtypes = [c_void_p, c_void_p, c_int64, c_int64, c_int, c_int, c_int, c_void_p, c_void_p,
                                                 c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
     lib.adadim_gptq_quantize_meta16.restype = c_int
+    p, i64 = c_void_p, c_int64
+    for name, res, args in (
+            ("adadim_mx4_code_bytes", c_int64, [i64, i64]), ("adadim_mx4_scale_bytes", c_int64, [i64, i64]),
+            ("adadim_mx4_quantize", c_int, [p, p, c_int, i64, i64, i64, p, p, p, c_int, p]),
+            ("adadim_mx4_dequantize", c_int, [p, p, p, i64, i64, p, c_int, i64]),
+            ("adadim_mx4_matmul", c_int, [p, p, p, c_int, i64, i64, p, p, i64, i64, p, c_int, i64]),
+            ("adadim_mx4_matmul_experts", c_int, [p, p, p, c_int, i64, i64, p, i64, p, c_int, p, p, i64, i64, p, c_int, i64]),
+            ("adadim_expert_route", c_int, [p, p, c_int, i64, i64, c_int, c_int, c_int, p, p, p, p, p]),
+            ("adadim_expert_combine", c_int, [p, p, c_int, i64, i64, i64, p, p, i64, c_int, p, c_int, i64])):
+        f = getattr(lib, name)
+        f.restype, f.argtypes = res, args
     if path is None:
         _lib = lib
     return lib
@@ -184,6 +199,34 @@ def _need(t, what: str, dtype: str | None = None, pitched: bool = False):
                          "tensor, not a transposed view")
     if not pitched and not t.is_contiguous():
         raise ValueError(f"{what}: must be contiguous (shape {tuple(t.shape)}, strides {tuple(t.stride())})")
+
+
+def mx4_shapes(rows: int, cols: int):
+    """Shapes of the codes and scales (uint8) of `rows` rows of `cols` values in mx4."""
+    pieces = (cols + 127) // 128
+    return (rows, 64 * pieces), (pieces, rows, 4)
+
+
+def _type_of(t, what: str) -> int:
+    try:
+        return _TYPES[str(t.dtype)]
+    except KeyError:
+        raise TypeError(f"{what}: expected float16, bfloat16 or float32, got {t.dtype}") from None
+
+
+def _rows_of(t, what: str, dtype: str | None = None, shape=None, pitched: bool = False):
+    """_need, and two axes (or those of `shape`)."""
+    _need(t, what, dtype, pitched=pitched)
+    if shape is None:
+        if t.dim() != 2:
+            raise ValueError(f"{what}: expected two axes, got shape {tuple(t.shape)}")
+    elif tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def _pitch(t) -> int:
+    """Row pitch in elements; that of a single row, or of none, is its length."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
 
 
 class Context:
@@ -385,6 +428,106 @@ class Context:
         self._check(self._lib.adadim_gptq_quantize(self._h, _ptr(W), out_f, in_f, dim, bits, group, _ptr(U), _ptr(perm),
                                                    _ptr(dead), _ptr(static_scales), _ptr(static_zeros), _ptr(codes),
                                                    _ptr(scales), _ptr(zeros), _ptr(dW), _ptr(packed)))
+
+    # -- microscaled 4-bit values and experts ----------------------------
+    def adadim_mx4_quantize(self, X, codes, scales, dW=None, dW_dtype: int = DW_F32, colscale=None):
+        """X [rows, cols] (rows may be a pitched view) to codes and scales of the shapes mx4_shapes gives."""
+        _rows_of(X, "X", pitched=True)
+        kind, (rows, cols) = _type_of(X, "X"), X.shape
+        c, s = mx4_shapes(rows, cols)
+        _rows_of(codes, "codes", "uint8", c)
+        _rows_of(scales, "scales", "uint8", s)
+        _need(dW, "dW", "float32" if dW_dtype == DW_F32 else "float16")
+        _need(colscale, "colscale", "float32")
+        need = score_elems(rows, cols) if dW_dtype == DW_F16_SCALED else rows * cols
+        if dW is not None and dW.numel() < need or colscale is not None and colscale.numel() < cols:
+            raise ValueError(f"dW needs {need} elements, colscale {cols}")
+        self._check(self._lib.adadim_mx4_quantize(self._h, _ptr(X), kind, rows, cols, _pitch(X), _ptr(codes), _ptr(scales), _ptr(dW),
+                                                  dW_dtype, _ptr(colscale)))
+
+    def adadim_mx4_dequantize(self, codes, scales, Y):
+        """The values of codes and scales into Y [rows, cols] (its rows may be pitched)."""
+        _rows_of(Y, "Y", pitched=True)
+        kind, (rows, cols) = _type_of(Y, "Y"), Y.shape
+        c, s = mx4_shapes(rows, cols)
+        _rows_of(codes, "codes", "uint8", c)
+        _rows_of(scales, "scales", "uint8", s)
+        self._check(self._lib.adadim_mx4_dequantize(self._h, _ptr(codes), _ptr(scales), rows, cols, _ptr(Y), kind, _pitch(Y)))
+
+    def _mx4_input(self, X, x_scales, in_f):
+        """(in, type, tokens, pitch) of a product's left operand; mx4 codes are told by their type and need in_f."""
+        if str(X.dtype) == "torch.uint8":
+            if in_f is None or x_scales is None:
+                raise ValueError("X in mx4 needs in_f and x_scales")
+            c, s = mx4_shapes(X.shape[0], in_f)
+            _rows_of(X, "X", "uint8", c)
+            _rows_of(x_scales, "x_scales", "uint8", s)
+            return in_f, TYPE_MX4, X.shape[0], 0
+        if x_scales is not None:
+            raise ValueError("x_scales go with X in mx4 (uint8 codes)")
+        _rows_of(X, "X", pitched=True)
+        kind = _type_of(X, "X")
+        if in_f is not None and X.shape[1] != in_f:
+            raise ValueError(f"X: expected {in_f} columns, got {X.shape[1]}")
+        return X.shape[1], kind, X.shape[0], _pitch(X)
+
+    def adadim_mx4_matmul(self, X, codes, scales, Y, in_f: int | None = None, x_scales=None):
+        """Y [tokens, out] = X W^T; X float16 or bfloat16 [tokens, in], or mx4 codes with x_scales and in_f."""
+        in_f, kind, tokens, ldx = self._mx4_input(X, x_scales, in_f)
+        _rows_of(Y, "Y", pitched=True)
+        y_kind, out = _type_of(Y, "Y"), Y.shape[1]
+        if Y.shape[0] != tokens:
+            raise ValueError(f"Y: expected {tokens} rows, got {Y.shape[0]}")
+        c, s = mx4_shapes(out, in_f)
+        _rows_of(codes, "codes", "uint8", c)
+        _rows_of(scales, "scales", "uint8", s)
+        self._check(self._lib.adadim_mx4_matmul(self._h, _ptr(X), _ptr(x_scales), kind, tokens, ldx, _ptr(codes), _ptr(scales), out,
+                                                in_f, _ptr(Y), y_kind, _pitch(Y)))
+
+    def adadim_mx4_matmul_experts(self, X, codes, scales, offsets, Y, in_f: int | None = None, x_scales=None, rows=None):
+        """Y[r] = X[rows[r]] W_e^T for the rows offsets[e] .. offsets[e + 1]; codes [experts, ..], scales [experts, ..]."""
+        in_f, kind, tokens, ldx = self._mx4_input(X, x_scales, in_f)
+        _rows_of(Y, "Y", pitched=True)
+        y_kind, (n_rows, out) = _type_of(Y, "Y"), Y.shape
+        experts = offsets.numel() - 1
+        c, s = mx4_shapes(out, in_f)
+        _rows_of(codes, "codes", "uint8", (experts, *c))
+        _rows_of(scales, "scales", "uint8", (experts, *s))
+        _need(offsets, "offsets", "int32")
+        if rows is not None:
+            _rows_of(rows, "rows", "int32", (n_rows,))
+        elif tokens != n_rows:
+            raise ValueError(f"without rows X has as many rows as Y: got {tokens} and {n_rows}")
+        self._check(self._lib.adadim_mx4_matmul_experts(self._h, _ptr(X), _ptr(x_scales), kind, tokens, ldx, _ptr(rows), n_rows,
+                                                        _ptr(offsets), experts, _ptr(codes), _ptr(scales), out, in_f, _ptr(Y),
+                                                        y_kind, _pitch(Y)))
+
+    def adadim_expert_route(self, logits, chosen, weights, offsets, rows, slots, renormalize: bool = True):
+        """logits [tokens, experts] to chosen, weights, slots [tokens, k], offsets [experts + 1] and rows [tokens * k]."""
+        _rows_of(logits, "logits", pitched=True)
+        kind, (tokens, experts) = _type_of(logits, "logits"), logits.shape
+        _rows_of(chosen, "chosen", "int32")
+        k = chosen.shape[1]
+        _rows_of(chosen, "chosen", "int32", (tokens, k))
+        _rows_of(weights, "weights", "float32", (tokens, k))
+        _rows_of(slots, "slots", "int32", (tokens, k))
+        _rows_of(offsets, "offsets", "int32", (experts + 1,))
+        _rows_of(rows, "rows", "int32", (tokens * k,))
+        self._check(self._lib.adadim_expert_route(self._h, _ptr(logits), kind, tokens, _pitch(logits), experts, k,
+                                                  1 if renormalize else 0, _ptr(chosen), _ptr(weights), _ptr(offsets), _ptr(rows),
+                                                  _ptr(slots)))
+
+    def adadim_expert_combine(self, Z, slots, weights, Y):
+        """Y [tokens, cols] = sum over j of weights[t, j] Z[slots[t, j]]."""
+        _rows_of(Z, "Z", pitched=True)
+        _rows_of(Y, "Y", pitched=True)
+        _rows_of(slots, "slots", "int32")
+        tokens, k = slots.shape
+        _rows_of(weights, "weights", "float32", (tokens, k))
+        if Y.shape[0] != tokens or Y.shape[1] != Z.shape[1]:
+            raise ValueError(f"Y: expected shape {(tokens, Z.shape[1])}, got {tuple(Y.shape)}")
+        self._check(self._lib.adadim_expert_combine(self._h, _ptr(Z), _type_of(Z, "Z"), Z.shape[0], Z.shape[1], _pitch(Z), _ptr(slots),
+                                                    _ptr(weights), tokens, k, _ptr(Y), _type_of(Y, "Y"), _pitch(Y)))
 
     def adadim_probe_mfma_f64(self, iters: int = 20000):
         """(TFLOP/s, shader clock in MHz) of a register-resident fp64 MFMA loop; waits for the stream."""

@@ -1,0 +1,59 @@
+// What the product kernels of microscaled 4-bit weights are given, and how they read it.
+//     Y[r, o] = sum_k W[o, k] X[src(r), k],   W in mx4; X in fp16, bf16 or mx4; sums in fp32, rounded once
+// One weight for all rows, or one per expert with the rows in groups: rows offsets[e] .. offsets[e + 1] belong to expert
+// e.  src(r) = r, or rows[r].
+#pragma once
+
+#include "mx4.h"
+
+namespace mx4 {
+
+struct Product {
+    const void* X;
+    const uint32_t* x_scales;      // mx4 only
+    int64_t tokens, ldx;           // rows of X, their pitch in elements (mx4: the codes are contiguous)
+    const int32_t* rows;           // or null
+    const int32_t* offsets;        // or null: one group of all rows
+    int64_t n_rows;
+    int experts;
+    const uint8_t* codes;
+    const uint32_t* scales;
+    int64_t out, in;
+    void* Y;
+    int y_type;
+    int64_t ldy;
+};
+
+struct Group {
+    int64_t lo, hi;
+    const uint8_t* codes;
+    const uint32_t* scales;
+};
+
+// Expert e's rows, held inside [0, n_rows] whatever the offsets say, and its weight.
+__device__ __forceinline__ Group group_of(const Product& a, int e) {
+    Group g{0, a.n_rows, a.codes, a.scales};
+    if (a.offsets) {
+        g.lo = min(int64_t(max(a.offsets[e], 0)), a.n_rows);
+        g.hi = min(int64_t(max(a.offsets[e + 1], 0)), a.n_rows);
+        g.codes += int64_t(e) * a.out * pieces(a.in) * PIECE_BYTES;
+        g.scales += int64_t(e) * a.out * pieces(a.in);
+    }
+    return g;
+}
+
+// The row of X behind row r of Y; -1 (read as zeros) behind the group's end or where rows[] names none.
+__device__ __forceinline__ int64_t source_row(const Product& a, int64_t r, int64_t hi) {
+    if (r >= hi) return -1;
+    const int64_t s = a.rows ? int64_t(a.rows[r]) : r;
+    return s >= 0 && s < a.tokens ? s : -1;
+}
+
+__device__ __forceinline__ void store_y(const Product& a, int64_t row, int64_t col, float v) {
+    const int64_t at = row * a.ldy + col;
+    if (a.y_type == ADADIM_TYPE_F16) static_cast<_Float16*>(a.Y)[at] = static_cast<_Float16>(v);
+    else if (a.y_type == ADADIM_TYPE_BF16) static_cast<__bf16*>(a.Y)[at] = static_cast<__bf16>(v);
+    else static_cast<float*>(a.Y)[at] = v;
+}
+
+}  // namespace mx4
