@@ -36,6 +36,7 @@ enum {
     WS_GPTQ_Q,          // u8 codes in visiting order
     WS_GPTQ_V,          // int32 position of each original channel in the visiting order
     WS_PROBE,           // output of the matrix-core rate probe
+    WS_MX4_X,           // rows of X copied to where 16-byte transfers can take them
     WS_ROUTE,           // the router's masks of tokens per expert and the places behind them
     WS_COUNT
 };

@@ -1,6 +1,8 @@
 // Products with microscaled 4-bit weights: Y = X W^T, alone or grouped by expert.
 #include "mx4_matmul.h"
 
+#include <type_traits>
+
 namespace {
 
 using namespace mx4;
@@ -112,9 +114,85 @@ __global__ __launch_bounds__(64 * RW_WAVES) void mx4_rows(Product a) {
     }
 }
 
+// Rows of X that the tiles' 16-byte transfers cannot take as they lie (an odd pitch or address, a length that is no multiple of 8):
+// copied once to rows of whole pieces, filled up with zeros.
+__global__ __launch_bounds__(256) void mx4_align_rows(const uint16_t* __restrict__ X, int64_t rows, int64_t cols, int64_t ldx,
+                                                      int64_t pitch, uint16_t* __restrict__ to) {
+    const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 8, row = i / pitch, c = i % pitch;
+    if (row >= rows) return;
+    Chunk<uint16_t, 8>::vec v = {};
+    if (c < cols) v = Chunk<uint16_t, 8>::load(X + row * ldx + c, static_cast<int>(min(int64_t(8), cols - c)));
+    *reinterpret_cast<Chunk<uint16_t, 8>::vec*>(to + i) = v;
+}
+
+}  // namespace
+
+#include "mx4_tiles.h"
+
+namespace {
+
+PerDeviceOnce g_tiles_once;
+
+template <int XT, int BM, int BN, int WT, int WO>
+constexpr int tile_lds() {
+    return 2 * (BM * (XT == XMX4 ? 128 : 256) + (XT == XMX4 ? BN * 128 : 0));
+}
+
+template <int XT>
+hipError_t raise_lds() {
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx4_tiles<XT, 256, 256, 2, 2>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_lds<XT, 256, 256, 2, 2>());
+    if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx4_tiles<XT, 128, 128, 2, 2>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_lds<XT, 128, 128, 2, 2>());
+    return e;
+}
+
+// Row tiles that the launch has to have workgroups for: each group may end in a tile of its own.
+inline int64_t most_row_tiles(const Product& a, int bm) {
+    return a.offsets ? a.n_rows / bm + min(int64_t(a.experts), a.n_rows) : (a.n_rows + bm - 1) / bm;
+}
+
+template <int XT, int BM, int BN, int WT, int WO>
+int launch_tiles(adadim_ctx* ctx, const Product& a) {
+    const int64_t tiles = most_row_tiles(a, BM) * ((a.out + BN - 1) / BN);
+    if (tiles > INT32_MAX - 8) return adadim_fail(ctx, ADADIM_EINVAL, "mx4 product: more tiles than a launch has workgroups");
+    ProfScope prof(ctx, "mx4_tiles");
+    hipLaunchKernelGGL((mx4_tiles<XT, BM, BN, WT, WO>), dim3(static_cast<unsigned>((tiles + 7) / 8 * 8)), dim3(64 * WT * WO),
+                       (tile_lds<XT, BM, BN, WT, WO>()), ctx->stream, a);
+    ADADIM_LAUNCH_CHECK(ctx, "mx4_tiles");
+    return ADADIM_OK;
+}
+
+template <int XT>
+int launch_many(adadim_ctx* ctx, Product a) {
+    ADADIM_HIP_TRY(ctx, g_tiles_once.run([] {
+        hipError_t e = raise_lds<XF16>();
+        if (e == hipSuccess) e = raise_lds<XBF16>();
+        if (e == hipSuccess) e = raise_lds<XMX4>();
+        return e;
+    }));
+    if (XT != XMX4 && (!aligned16(a.X) || a.ldx % 8 != 0 || a.in % 8 != 0)) {
+        const int64_t pitch = pieces(a.in) * PIECE, blocks = (a.tokens * pitch / 8 + 255) / 256;
+        if (blocks > INT32_MAX) return adadim_fail(ctx, ADADIM_EINVAL, "mx4 product: X too large to be copied to aligned rows");
+        uint16_t* to = static_cast<uint16_t*>(adadim_workspace(ctx, WS_MX4_X, size_t(a.tokens) * size_t(pitch) * 2));
+        if (!to) return ADADIM_EHIP;
+        ProfScope prof(ctx, "mx4_align_rows");
+        hipLaunchKernelGGL(mx4_align_rows, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, ctx->stream, static_cast<const uint16_t*>(a.X),
+                           a.tokens, a.in, a.ldx, pitch, to);
+        ADADIM_LAUNCH_CHECK(ctx, "mx4_align_rows");
+        a.X = to;
+        a.ldx = pitch;
+    }
+    const int64_t wide = most_row_tiles(a, 256) * ((a.out + 255) / 256);
+    return wide >= 200 ? launch_tiles<XT, 256, 256, 2, 2>(ctx, a) : launch_tiles<XT, 128, 128, 2, 2>(ctx, a);
+}
+
 }  // namespace
 
 int launch_mx4_matmul(adadim_ctx* ctx, const mx4::Product& a, int x_type) {
+    if (a.tokens > 0 && a.n_rows / a.experts > 64) {
+        if (x_type == XF16) return launch_many<XF16>(ctx, a);
+        if (x_type == XBF16) return launch_many<XBF16>(ctx, a);
+        return launch_many<XMX4>(ctx, a);
+    }
     const dim3 grid(static_cast<unsigned>((a.out + 15) / 16), static_cast<unsigned>(a.experts)), block(64 * RW_WAVES);
     ProfScope prof(ctx, "mx4_rows");
     if (x_type == XF16) hipLaunchKernelGGL((mx4_rows<XF16>), grid, block, 0, ctx->stream, a);
