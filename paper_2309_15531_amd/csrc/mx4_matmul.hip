@@ -140,7 +140,7 @@ constexpr int tile_lds() {
 
 template <int XT>
 hipError_t raise_lds() {
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx4_tiles<XT, 256, 256, 2, 2>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_lds<XT, 256, 256, 2, 2>());
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx4_tiles<XT, 256, 256, 2, 4>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_lds<XT, 256, 256, 2, 4>());
     if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx4_tiles<XT, 128, 128, 2, 2>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_lds<XT, 128, 128, 2, 2>());
     return e;
 }
@@ -182,7 +182,7 @@ int launch_many(adadim_ctx* ctx, Product a) {
         a.ldx = pitch;
     }
     const int64_t wide = most_row_tiles(a, 256) * ((a.out + 255) / 256);
-    return wide >= 200 ? launch_tiles<XT, 256, 256, 2, 2>(ctx, a) : launch_tiles<XT, 128, 128, 2, 2>(ctx, a);
+    return wide >= 200 ? launch_tiles<XT, 256, 256, 2, 4>(ctx, a) : launch_tiles<XT, 128, 128, 2, 2>(ctx, a);
 }
 
 }  // namespace

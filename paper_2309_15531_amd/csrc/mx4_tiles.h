@@ -225,6 +225,7 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(Product a) {
     auto x_frag = [&](int buf, int i, int c) { return lds_read16(xf + buf * STAGE + i * 32 * ROWB + ((c ^ fsw ^ swizzle<CH>(32 * (wt * TT + i))) << 4)); };
     auto w_frag = [&](int buf, int o, int c) { return lds_read16(wf + buf * STAGE + o * 32 * ROWB + ((c ^ fsw ^ swizzle<CH>(32 * (wo * TO + o))) << 4)); };
 
+    bool wide = false;                                        // fp16 X: a weight has gone by that no fp16 number holds
     auto compute = [&](int buf, const Side& d) {
         if constexpr (MX) {
             auto step = [&](auto tag) {
@@ -245,7 +246,6 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(Product a) {
             step(std::integral_constant<int, 3>{});
         } else {
             float sc[TO][2];
-            bool wide = false;
 #pragma unroll
             for (int o = 0; o < TO; ++o)
 #pragma unroll
@@ -254,25 +254,6 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(Product a) {
                     sc[o][b] = scale_operand(byte);
                     wide |= beyond_f16(byte);
                 }
-            if (XT == XF16 && __any(wide)) {                  // X in two parts of bf16
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    bf8v w[TO];
-#pragma unroll
-                    for (int o = 0; o < TO; ++o) w[o] = values8_bf16(d.w[o][j >> 2][j & 3], sc[o][j >> 2]);
-#pragma unroll
-                    for (int i = 0; i < TT; ++i) {
-                        bf8v hi, lo;
-                        split_f16(__builtin_bit_cast(half8v, x_frag(buf, i, j + 8 * fh)), hi, lo);
-#pragma unroll
-                        for (int o = 0; o < TO; ++o) {
-                            acc[o][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[o], hi, acc[o][i], 0, 0, 0);
-                            acc[o][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[o], lo, acc[o][i], 0, 0, 0);
-                        }
-                    }
-                }
-                return;
-            }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 uint4v x[TT];
@@ -311,6 +292,41 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(Product a) {
         __builtin_amdgcn_s_waitcnt(WAIT_VM0);
         __syncthreads();
         now = next;
+    }
+    if constexpr (XT == XF16) {
+        if (__syncthreads_or(wide)) {
+            // The tile once more with both operands in bf16, X in two parts.  Rare: a stage at a time.
+#pragma unroll
+            for (int o = 0; o < TO; ++o)
+#pragma unroll
+                for (int i = 0; i < TT; ++i) acc[o][i] = float16v{};
+#pragma unroll
+            for (int i = 0; i < XL; ++i) xp[i] -= int64_t(n_st) * ROWB;
+            for (int s = 0; s < n_st; ++s) {
+                fetch(s, 0);
+                const Side d = side(s);
+                __builtin_amdgcn_s_waitcnt(WAIT_VM0);
+                __syncthreads();
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    bf8v w[TO];
+#pragma unroll
+                    for (int o = 0; o < TO; ++o) w[o] = values8_bf16(d.w[o][j >> 2][j & 3], scale_operand((d.ws[o] >> (8 * (j >> 2))) & 255u));
+#pragma unroll
+                    for (int i = 0; i < TT; ++i) {
+                        bf8v hi, lo;
+                        split_f16(__builtin_bit_cast(half8v, x_frag(0, i, j + 8 * fh)), hi, lo);
+#pragma unroll
+                        for (int o = 0; o < TO; ++o) {
+                            acc[o][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[o], hi, acc[o][i], 0, 0, 0);
+                            acc[o][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[o], lo, acc[o][i], 0, 0, 0);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+                __syncthreads();
+            }
+        }
     }
 
     // ---- Y: a lane holds, of each 32 x 32 block, token fr and outputs 8 q + 4 h .. + 3.  A wave turns 32 tokens x its outputs through LDS of
