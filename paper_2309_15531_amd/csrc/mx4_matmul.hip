@@ -114,14 +114,15 @@ __global__ __launch_bounds__(64 * RW_WAVES) void mx4_rows(Product a) {
     }
 }
 
-// Rows of X that the tiles' 16-byte transfers cannot take as they lie (an odd pitch or address, a length that is no multiple of 8):
-// copied once to rows of whole pieces, filled up with zeros.
-__global__ __launch_bounds__(256) void mx4_align_rows(const uint16_t* __restrict__ X, int64_t rows, int64_t cols, int64_t ldx,
-                                                      int64_t pitch, uint16_t* __restrict__ to) {
+// Rows of X that the tiles' 16-byte transfers cannot take as they lie: copied once, in the order of Y's rows where rows[] is given, to rows of
+// whole pieces filled up with zeros.
+__global__ __launch_bounds__(256) void mx4_align_rows(Product a, int64_t n, int64_t pitch, uint16_t* __restrict__ to) {
     const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 8, row = i / pitch, c = i % pitch;
-    if (row >= rows) return;
+    if (row >= n) return;
+    const int64_t src = source_row(a, row, n);
     Chunk<uint16_t, 8>::vec v = {};
-    if (c < cols) v = Chunk<uint16_t, 8>::load(X + row * ldx + c, static_cast<int>(min(int64_t(8), cols - c)));
+    if (c < a.in && src >= 0)
+        v = Chunk<uint16_t, 8>::load(static_cast<const uint16_t*>(a.X) + src * a.ldx + c, static_cast<int>(min(int64_t(8), a.in - c)));
     *reinterpret_cast<Chunk<uint16_t, 8>::vec*>(to + i) = v;
 }
 
@@ -161,6 +162,11 @@ int launch_tiles(adadim_ctx* ctx, const Product& a) {
     return ADADIM_OK;
 }
 
+// Rows of X (those of a tile, or all that rows[] may name) that 32-bit offsets do not reach.
+inline bool far_rows(const Product& a, int x_type) {
+    return (a.rows ? a.tokens : 256) * (x_type == XMX4 ? pieces(a.in) * PIECE_BYTES : 2 * a.ldx) > int64_t(UINT32_MAX);
+}
+
 template <int XT>
 int launch_many(adadim_ctx* ctx, Product a) {
     ADADIM_HIP_TRY(ctx, g_tiles_once.run([] {
@@ -169,17 +175,18 @@ int launch_many(adadim_ctx* ctx, Product a) {
         if (e == hipSuccess) e = raise_lds<XMX4>();
         return e;
     }));
-    if (XT != XMX4 && (!aligned16(a.X) || a.ldx % 8 != 0 || a.in % 8 != 0)) {
-        const int64_t pitch = pieces(a.in) * PIECE, blocks = (a.tokens * pitch / 8 + 255) / 256;
+    if (XT != XMX4 && (!aligned16(a.X) || a.ldx % 8 != 0 || a.in % 8 != 0 || far_rows(a, XT))) {
+        const int64_t pitch = pieces(a.in) * PIECE, blocks = (a.n_rows * pitch / 8 + 255) / 256;
         if (blocks > INT32_MAX) return adadim_fail(ctx, ADADIM_EINVAL, "mx4 product: X too large to be copied to aligned rows");
-        uint16_t* to = static_cast<uint16_t*>(adadim_workspace(ctx, WS_MX4_X, size_t(a.tokens) * size_t(pitch) * 2));
+        uint16_t* to = static_cast<uint16_t*>(adadim_workspace(ctx, WS_MX4_X, size_t(a.n_rows) * size_t(pitch) * 2));
         if (!to) return ADADIM_EHIP;
         ProfScope prof(ctx, "mx4_align_rows");
-        hipLaunchKernelGGL(mx4_align_rows, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, ctx->stream, static_cast<const uint16_t*>(a.X),
-                           a.tokens, a.in, a.ldx, pitch, to);
+        hipLaunchKernelGGL(mx4_align_rows, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, ctx->stream, a, a.n_rows, pitch, to);
         ADADIM_LAUNCH_CHECK(ctx, "mx4_align_rows");
         a.X = to;
         a.ldx = pitch;
+        a.tokens = a.n_rows;
+        a.rows = nullptr;
     }
     const int64_t wide = most_row_tiles(a, 256) * ((a.out + 255) / 256);
     return wide >= 200 ? launch_tiles<XT, 256, 256, 2, 4>(ctx, a) : launch_tiles<XT, 128, 128, 2, 2>(ctx, a);
@@ -188,7 +195,7 @@ int launch_many(adadim_ctx* ctx, Product a) {
 }  // namespace
 
 int launch_mx4_matmul(adadim_ctx* ctx, const mx4::Product& a, int x_type) {
-    if (a.tokens > 0 && a.n_rows / a.experts > 64) {
+    if (a.tokens > 0 && a.n_rows / a.experts > 64 && !(x_type == XMX4 && far_rows(a, x_type))) {
         if (x_type == XF16) return launch_many<XF16>(ctx, a);
         if (x_type == XBF16) return launch_many<XBF16>(ctx, a);
         return launch_many<XMX4>(ctx, a);

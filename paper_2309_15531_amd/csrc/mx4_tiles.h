@@ -12,6 +12,15 @@ namespace tiles {
 __device__ __forceinline__ void g2l16(const void* g, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(g) : "memory", "m0");
 }
+__device__ __forceinline__ void g2l16_s(const void* sbase, uint32_t voff, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(voff), "s"(sbase) : "memory", "m0");
+}
+// The same value in every lane, told to the compiler.
+__device__ __forceinline__ const char* uniform(const void* p) {
+    const uintptr_t b = reinterpret_cast<uintptr_t>(p);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(b)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(b >> 32));
+    return reinterpret_cast<const char*>(uintptr_t(hi) << 32 | lo);
+}
 __device__ __forceinline__ uint4v lds_read16(uint32_t addr) {
     typedef uint4v __attribute__((address_space(3))) * lds_ptr;
     return *reinterpret_cast<lds_ptr>(uintptr_t(addr));
@@ -23,9 +32,9 @@ __device__ __forceinline__ void lds_write(uint32_t addr, const V& v) {
 }
 
 // Rows of 128 bytes (8 chunks of 16) or 256 bytes (16 chunks) in LDS; chunk c of row r lies at slot c ^ swizzle(r), so that
-// a fragment read (32 consecutive rows, one chunk each) touches every bank evenly.
+// a fragment read (32 consecutive rows, one chunk each) touches every bank evenly.  The same for rows 32 apart.
 template <int CHUNKS>
-__device__ __forceinline__ int swizzle(int row) { return CHUNKS == 8 ? (row ^ (row >> 3)) & 7 : row & 15; }
+__device__ __forceinline__ int swizzle(int row) { return CHUNKS == 8 ? (row & 7) ^ ((row >> 3) & 3) : row & 15; }
 
 template <int J>
 __device__ __forceinline__ float16v mma_mx4(uint4v w, uint32_t ws, uint4v x, uint32_t xs, float16v acc) {
@@ -40,7 +49,7 @@ __device__ __forceinline__ float16v mma_mx4(uint4v w, uint32_t ws, uint4v x, uin
 
 __device__ const uint4v zero_chunk = {0u, 0u, 0u, 0u};   // what the transfers of chunks that do not exist read
 
-constexpr int WAIT_VM0 = 0x0F70;                  // s_waitcnt vmcnt(0), nothing else
+constexpr int WAIT_VM0 = 0x0F70, WAIT_ALL = 0x0070;       // s_waitcnt vmcnt(0); vmcnt(0) lgkmcnt(0)
 
 // The tile (expert, first row, first output) of a workgroup.  Tiles are counted out on the device: every group has
 // ceil(rows / BM) of them, in the order of the experts.  Workgroups go to the eight XCDs in turn; each XCD takes a contiguous eighth
@@ -132,46 +141,40 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(Product a) {
         const int64_t s = source_row(a, r_first + i, gr.hi);
         return s < 0 ? int64_t(0) : s;
     };
-    const char* xp[XL];
-    const char* wp[WL > 0 ? WL : 1];
-    int xc[XL], wc[WL > 0 ? WL : 1];
+    // Transfers.  Number i of a wave takes ROWS_PER rows; every lane has the same chunk in all of them.  They are given as 32-bit offsets
+    // from a row that all share: the tile's first (W; X without rows[]) or that of token 0, which the host holds within 4 GB.
+    static_assert(NW % 4 == 0, "the swizzle is the same for all transfers of a wave");
+    const int t_row = ROWS_PER * wave + lane / CH, t_chunk = (lane % CH) ^ swizzle<CH>(t_row);
+    const int64_t x_pitch = MX ? np * PIECE_BYTES : 2 * a.ldx, x_first = a.rows ? 0 : r_first;
+    uint32_t xo[XL], wofs[MX ? WL : 1];
+    const char* x_base = uniform(static_cast<const char*>(a.X) + x_first * x_pitch);
+    const char* w_base = uniform(gr.codes + t.out0 * np * PIECE_BYTES);
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
-        const int row = ROWS_PER * (wave + NW * i) + lane / CH;
-        xc[i] = (lane % CH) ^ swizzle<CH>(row);
-        xp[i] = static_cast<const char*>(a.X) + x_row(row) * (MX ? np * PIECE_BYTES : 2 * a.ldx) + 16 * xc[i];
+        const int row = t_row + ROWS_PER * NW * i;
+        xo[i] = static_cast<uint32_t>((a.rows ? x_row(row) : min(int64_t(row), gr.hi - 1 - r_first)) * x_pitch + 16 * t_chunk);
     }
     if constexpr (MX) {
 #pragma unroll
-        for (int i = 0; i < WL; ++i) {
-            const int row = ROWS_PER * (wave + NW * i) + lane / CH;
-            wc[i] = (lane % CH) ^ swizzle<CH>(row);
-            wp[i] = reinterpret_cast<const char*>(gr.codes) + min(t.out0 + row, a.out - 1) * np * PIECE_BYTES + 16 * wc[i];
-        }
+        for (int i = 0; i < WL; ++i)
+            wofs[i] = static_cast<uint32_t>(min(int64_t(t_row + ROWS_PER * NW * i), a.out - 1 - t.out0) * np * PIECE_BYTES + 16 * t_chunk);
     }
-    // chunks of a row that exist in stage s
-    auto have = [&](int s) {
-        if constexpr (MX) return static_cast<int>(min(int64_t(8), 4 * (np - 2 * s)));
-        else return static_cast<int>(min(int64_t(16), (a.in - int64_t(PIECE) * s + 7) / 8));
+    // The last stage along k, which may be shorter, is computed first: stage q > 0 in the order of computation is number q - 1 along k.
+    // The chunks that stage 0 lacks, and all of the stages behind the last (nothing branches on them), read zeros.
+    auto fetch_first = [&]() {
+        const int64_t k = n_st - 1;
+        const int n = static_cast<int>(MX ? min(int64_t(8), 4 * (np - 2 * k)) : min(int64_t(16), (a.in - PIECE * k + 7) / 8));
+        const char* none = reinterpret_cast<const char*>(&zero_chunk);
+        const uint32_t to = lds0 + wave * 1024;
+#pragma unroll
+        for (int i = 0; i < XL; ++i) g2l16(t_chunk < n ? x_base + xo[i] + k * ROWB : none, to + NW * i * 1024);
+#pragma unroll
+        for (int i = 0; i < WL; ++i) g2l16(t_chunk < n ? w_base + wofs[i] + k * ROWB : none, to + X_BYTES + NW * i * 1024);
     };
-    auto fetch = [&](int s, int buf) {
-        const int n = have(s);
-        if (n == CH) {
-#pragma unroll
-            for (int i = 0; i < XL; ++i) g2l16(xp[i], lds0 + buf * STAGE + (wave + NW * i) * 1024);
-#pragma unroll
-            for (int i = 0; i < WL; ++i) g2l16(wp[i], lds0 + buf * STAGE + X_BYTES + (wave + NW * i) * 1024);
-        } else {
-            const char* none = reinterpret_cast<const char*>(&zero_chunk);
-#pragma unroll
-            for (int i = 0; i < XL; ++i) g2l16(xc[i] < n ? xp[i] : none, lds0 + buf * STAGE + (wave + NW * i) * 1024);
-#pragma unroll
-            for (int i = 0; i < WL; ++i) g2l16(wc[i] < n ? wp[i] : none, lds0 + buf * STAGE + X_BYTES + (wave + NW * i) * 1024);
-        }
-#pragma unroll
-        for (int i = 0; i < XL; ++i) xp[i] += ROWB;
-#pragma unroll
-        for (int i = 0; i < WL; ++i) wp[i] += ROWB;
+    auto fetch_one = [&](const char* xb, const char* wb, uint32_t mask, int buf, int i) {
+        const uint32_t to = lds0 + buf * STAGE + wave * 1024;
+        if (i < XL) g2l16_s(xb, xo[i < XL ? i : 0] & mask, to + NW * i * 1024);
+        else if constexpr (MX) g2l16_s(wb, wofs[i < XL ? 0 : i - XL] & mask, to + X_BYTES + NW * (i - XL) * 1024);
     };
 
     int64_t w_row[TO];
@@ -194,15 +197,16 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(Product a) {
 #pragma unroll
         for (int i = 0; i < TT; ++i) x_src[i] = x_row((wt * TT + i) * 32 + fr);
     }
-    auto side = [&](int s) {
+    auto side = [&](int q) {
+        const int s = q == 0 ? n_st - 1 : min(q, n_st) - 1;
         Side d;
         if constexpr (MX) {
-            const int64_t p = 2 * s + fh, q = min(p, np - 1);
+            const int64_t p = 2 * int64_t(s) + fh, at = min(p, np - 1);
 #pragma unroll
-            for (int o = 0; o < TO; ++o) d.ws[o] = gr.scales[q * a.out + w_row[o]];
+            for (int o = 0; o < TO; ++o) d.ws[o] = gr.scales[at * a.out + w_row[o]];
 #pragma unroll
-            for (int i = 0; i < TT; ++i) d.xs[i] = a.x_scales[q * a.tokens + x_src[i]];
-            if (p >= np) {                                    // half a stage: zeros from the zero page, of scale 1
+            for (int i = 0; i < TT; ++i) d.xs[i] = a.x_scales[at * a.tokens + x_src[i]];
+            if (q == 0 && p >= np) {                          // half a stage: what it lacks are zeros, of scale 1
 #pragma unroll
                 for (int o = 0; o < TO; ++o) d.ws[o] = ONE_WORD;
 #pragma unroll
@@ -220,32 +224,28 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(Product a) {
         return d;
     };
 
-    const uint32_t xf = lds0 + (wt * TT * 32 + fr) * ROWB, wf = lds0 + X_BYTES + (wo * TO * 32 + fr) * ROWB;
-    const int fsw = swizzle<CH>(fr);                          // (rows 32 apart have swizzles that differ by a constant)
-    auto x_frag = [&](int buf, int i, int c) { return lds_read16(xf + buf * STAGE + i * 32 * ROWB + ((c ^ fsw ^ swizzle<CH>(32 * (wt * TT + i))) << 4)); };
-    auto w_frag = [&](int buf, int o, int c) { return lds_read16(wf + buf * STAGE + o * 32 * ROWB + ((c ^ fsw ^ swizzle<CH>(32 * (wo * TO + o))) << 4)); };
+    // Fragment addresses: step j of half h reads chunk j + CH / 2 * h of its row.  They move between the two stages: those of step 0 a
+    // step before the others, since a stage's first operands are read during the last step of the one before.
+    constexpr int STEPS = CH / 2;
+    uint32_t xa[STEPS], wa[MX ? STEPS : 1];
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j) {
+        const uint32_t slot = static_cast<uint32_t>((j + STEPS * fh) ^ swizzle<CH>(fr)) << 4;
+        xa[j] = lds0 + (wt * TT * 32 + fr) * ROWB + slot;
+        if constexpr (MX) wa[j] = lds0 + X_BYTES + (wo * TO * 32 + fr) * ROWB + slot;
+    }
 
+    // ---- the pipeline.  A stage is CH / 2 steps of TO x TT matrix instructions; a step's operands are read (and, for 16-bit X, its
+    // weights converted) during the step before.  Before the last step of a stage all its reads have ended: there the wave waits for
+    // the next stage's transfers, meets the others, reads the next stage's first operands and sends for the one after it, into
+    // the buffer that has become free.
+    struct Frags {
+        uint4v w[TO], x[TT];
+    };
     bool wide = false;                                        // fp16 X: a weight has gone by that no fp16 number holds
-    auto compute = [&](int buf, const Side& d) {
-        if constexpr (MX) {
-            auto step = [&](auto tag) {
-                constexpr int J = decltype(tag)::value;
-                uint4v w[TO], x[TT];
-#pragma unroll
-                for (int o = 0; o < TO; ++o) w[o] = w_frag(buf, o, J + 4 * fh);
-#pragma unroll
-                for (int i = 0; i < TT; ++i) x[i] = x_frag(buf, i, J + 4 * fh);
-#pragma unroll
-                for (int o = 0; o < TO; ++o)
-#pragma unroll
-                    for (int i = 0; i < TT; ++i) acc[o][i] = mma_mx4<J>(w[o], d.ws[o], x[i], d.xs[i], acc[o][i]);
-            };
-            step(std::integral_constant<int, 0>{});
-            step(std::integral_constant<int, 1>{});
-            step(std::integral_constant<int, 2>{});
-            step(std::integral_constant<int, 3>{});
-        } else {
-            float sc[TO][2];
+    float sc[MX ? 1 : TO][2];
+    auto scales_of = [&](const Side& d) {
+        if constexpr (!MX) {
 #pragma unroll
             for (int o = 0; o < TO; ++o)
 #pragma unroll
@@ -254,45 +254,98 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(Product a) {
                     sc[o][b] = scale_operand(byte);
                     wide |= beyond_f16(byte);
                 }
+        }
+    };
+    // operand number k of a step: TO of W, then TT of X
+    auto read_one = [&](Frags& f, const Side& d, int step, int k) {
+        if (k >= TO) f.x[k - TO] = lds_read16(xa[step] + (k - TO) * 32 * ROWB);
+        else if constexpr (MX) f.w[k] = lds_read16(wa[step] + k * 32 * ROWB);
+        else if constexpr (XT == XF16) f.w[k] = __builtin_bit_cast(uint4v, values8_f16(d.w[k][step >> 2][step & 3], sc[k][step >> 2]));
+        else f.w[k] = __builtin_bit_cast(uint4v, values8_bf16(d.w[k][step >> 2][step & 3], sc[k][step >> 2]));
+    };
+    auto mma = [&](auto step_tag, const Frags& f, const Side& d, int m) {
+        constexpr int J = decltype(step_tag)::value;
+        const int o = m / TT, i = m % TT;
+        if constexpr (MX) acc[o][i] = mma_mx4<J & 3>(f.w[o], d.ws[o], f.x[i], d.xs[i], acc[o][i]);
+        else if constexpr (XT == XF16)
+            acc[o][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8v, f.w[o]), __builtin_bit_cast(half8v, f.x[i]), acc[o][i], 0, 0, 0);
+        else
+            acc[o][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8v, f.w[o]), __builtin_bit_cast(bf8v, f.x[i]), acc[o][i], 0, 0, 0);
+    };
+    constexpr int M = TO * TT, R = TO + TT, F = XL + WL;
+    // a step: its instructions with the next step's operands read between them, in this order
+    auto step = [&](auto step_tag, const Frags& f, const Side& d, Frags& nf, int nstep) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                uint4v x[TT];
-#pragma unroll
-                for (int i = 0; i < TT; ++i) x[i] = x_frag(buf, i, j + 8 * fh);
-#pragma unroll
-                for (int o = 0; o < TO; ++o) {
-                    const uint32_t word = d.w[o][j >> 2][j & 3];
-                    if constexpr (XT == XF16) {
-                        const half8v w = values8_f16(word, sc[o][j >> 2]);
-#pragma unroll
-                        for (int i = 0; i < TT; ++i)
-                            acc[o][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w, __builtin_bit_cast(half8v, x[i]), acc[o][i], 0, 0, 0);
-                    } else {
-                        const bf8v w = values8_bf16(word, sc[o][j >> 2]);
-#pragma unroll
-                        for (int i = 0; i < TT; ++i)
-                            acc[o][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, __builtin_bit_cast(bf8v, x[i]), acc[o][i], 0, 0, 0);
-                    }
-                }
-            }
+        for (int m = 0; m < (M > R ? M : R); ++m) {
+            if (m < R) read_one(nf, d, nstep, m);
+            if (m < M) mma(step_tag, f, d, m);
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
 
     Side now = side(0);
-    fetch(0, 0);
+    fetch_first();
     __builtin_amdgcn_s_waitcnt(WAIT_VM0);
     __syncthreads();
-    for (int s = 0; s < n_st; ++s) {
-        Side next = now;
-        if (s + 1 < n_st) {
-            next = side(s + 1);
-            fetch(s + 1, (s + 1) & 1);
+    Frags f0, f1;
+    scales_of(now);
+#pragma unroll
+    for (int k = 0; k < R; ++k) read_one(f0, now, 0, k);
+    xa[0] += STAGE;
+    if constexpr (MX) wa[0] += STAGE;
+    const char *xb = x_base, *wb = w_base;
+    uint32_t mask = ~0u;
+    int to_fetch = 1;
+    auto next_fetch = [&]() {                                 // where the next stage's transfers come from
+        const bool real = to_fetch < n_st;
+        xb = uniform(real ? x_base : reinterpret_cast<const char*>(&zero_chunk));
+        wb = uniform(real ? w_base : reinterpret_cast<const char*>(&zero_chunk));
+        mask = real ? ~0u : 0u;
+        ++to_fetch;
+        x_base += ROWB;
+        w_base += ROWB;
+    };
+    next_fetch();
+#pragma unroll
+    for (int i = 0; i < F; ++i) fetch_one(xb, wb, mask, 1, i);
+    for (int q = 0; q < n_st; ++q) {
+        const int buf = q & 1;
+        Side next = side(q + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        auto pair = [&](auto tag) {                           // steps J (even) and J + 1, unless that is the stage's last
+            constexpr int J = decltype(tag)::value;
+            step(std::integral_constant<int, J>{}, f0, now, f1, J + 1);
+            if constexpr (J + 2 < STEPS) step(std::integral_constant<int, J + 1>{}, f1, now, f0, J + 2);
+        };
+        pair(std::integral_constant<int, 0>{});
+        pair(std::integral_constant<int, 2>{});
+        if constexpr (STEPS == 8) {
+            pair(std::integral_constant<int, 4>{});
+            pair(std::integral_constant<int, 6>{});
         }
-        compute(s & 1, now);
-        __builtin_amdgcn_s_waitcnt(WAIT_VM0);
-        __syncthreads();
+        __builtin_amdgcn_s_waitcnt(WAIT_ALL);
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        next_fetch();
+        scales_of(next);
+#pragma unroll
+        for (int m = 0; m < (M > R ? M : R); ++m) {
+            if (m < R) read_one(f0, next, 0, m);
+#pragma unroll
+            for (int i = m * F / M; i < (m < M ? (m + 1) * F / M : 0); ++i) fetch_one(xb, wb, mask, buf, i);
+            if (m < M) mma(std::integral_constant<int, STEPS - 1>{}, f1, now, m);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        const uint32_t move = buf ? -STAGE : STAGE;
+#pragma unroll
+        for (int j = 0; j < STEPS; ++j) {
+            xa[j] += j ? move : -move;
+            if constexpr (MX) wa[j] += j ? move : -move;
+        }
         now = next;
     }
+    __builtin_amdgcn_s_waitcnt(WAIT_ALL);
+    __syncthreads();
     if constexpr (XT == XF16) {
         if (__syncthreads_or(wide)) {
             // The tile once more with both operands in bf16, X in two parts.  Rare: a stage at a time.
@@ -300,11 +353,18 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(Product a) {
             for (int o = 0; o < TO; ++o)
 #pragma unroll
                 for (int i = 0; i < TT; ++i) acc[o][i] = float16v{};
+            x_base -= int64_t(to_fetch - 1) * ROWB;
+            uint32_t x0[STEPS];
 #pragma unroll
-            for (int i = 0; i < XL; ++i) xp[i] -= int64_t(n_st) * ROWB;
-            for (int s = 0; s < n_st; ++s) {
-                fetch(s, 0);
-                const Side d = side(s);
+            for (int j = 0; j < STEPS; ++j)
+                x0[j] = lds0 + (wt * TT * 32 + fr) * ROWB + (static_cast<uint32_t>((j + STEPS * fh) ^ swizzle<CH>(fr)) << 4);
+            for (int q = 0; q < n_st; ++q) {
+                if (q == 0) fetch_first();
+                else {
+#pragma unroll
+                    for (int i = 0; i < XL; ++i) fetch_one(x_base + int64_t(q - 1) * ROWB, nullptr, ~0u, 0, i);
+                }
+                const Side d = side(q);
                 __builtin_amdgcn_s_waitcnt(WAIT_VM0);
                 __syncthreads();
 #pragma unroll
@@ -315,7 +375,7 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(Product a) {
 #pragma unroll
                     for (int i = 0; i < TT; ++i) {
                         bf8v hi, lo;
-                        split_f16(__builtin_bit_cast(half8v, x_frag(0, i, j + 8 * fh)), hi, lo);
+                        split_f16(__builtin_bit_cast(half8v, lds_read16(x0[j] + i * 32 * ROWB)), hi, lo);
 #pragma unroll
                         for (int o = 0; o < TO; ++o) {
                             acc[o][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[o], hi, acc[o][i], 0, 0, 0);
