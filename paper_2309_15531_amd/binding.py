@@ -18,6 +18,7 @@ DIM_OC, DIM_IC = 0, 1
 DW_F32, DW_F16, DW_F16_SCALED = 0, 1, 2
 TYPE_F16, TYPE_BF16, TYPE_F32, TYPE_MX4 = 0, 1, 2, 3
 _TYPES = {"torch.float16": TYPE_F16, "torch.bfloat16": TYPE_BF16, "torch.float32": TYPE_F32}
+_DTYPES: dict = {}      # element type -> (its name, its TYPE_ number or None), filled as types are met
 
 EXPORTS = (
     "adadim_create", "adadim_destroy", "adadim_last_error", "adadim_version", "adadim_score_elems",
@@ -207,26 +208,42 @@ def mx4_shapes(rows: int, cols: int):
     return (rows, 64 * pieces), (pieces, rows, 4)
 
 
-def _type_of(t, what: str) -> int:
+def _dtype(t):
+    """(name, TYPE_ number or None) of a tensor's element type."""
+    d = t.dtype
     try:
-        return _TYPES[str(t.dtype)]
+        return _DTYPES[d]
     except KeyError:
-        raise TypeError(f"{what}: expected float16, bfloat16 or float32, got {t.dtype}") from None
+        name = str(d)
+        _DTYPES[d] = r = (name, _TYPES.get(name))
+        return r
 
 
-def _rows_of(t, what: str, dtype: str | None = None, shape=None, pitched: bool = False):
-    """_need, and two axes (or those of `shape`)."""
-    _need(t, what, dtype, pitched=pitched)
-    if shape is None:
-        if t.dim() != 2:
-            raise ValueError(f"{what}: expected two axes, got shape {tuple(t.shape)}")
-    elif tuple(t.shape) != tuple(shape):
+# The calls of a decode step take a few microseconds on the GPU: what follows looks at each tensor no more often than it must.
+def _array(t, what: str, dtype: str, shape) -> int:
+    """Address of a contiguous device tensor of that element type and shape."""
+    if t.shape != shape or not t.is_contiguous() or not t.is_cuda or _dtype(t)[0] != dtype:
+        _need(t, what, dtype[6:])
         raise ValueError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr()
 
 
-def _pitch(t) -> int:
-    """Row pitch in elements; that of a single row, or of none, is its length."""
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+def _matrix(t, what: str):
+    """(address, TYPE_ number, rows, columns, row pitch in elements) of a device matrix in one of the float types whose
+    rows may be pitched."""
+    shape = t.shape
+    if len(shape) != 2:
+        raise ValueError(f"{what}: expected two axes, got shape {tuple(shape)}")
+    kind = _dtype(t)[1]
+    if kind is None:
+        raise TypeError(f"{what}: expected float16, bfloat16 or float32, got {t.dtype}")
+    rows, cols = shape
+    if t.is_contiguous():
+        if not t.is_cuda:
+            _need(t, what)
+        return t.data_ptr(), kind, rows, cols, cols if cols > 0 else 1
+    _need(t, what, pitched=True)
+    return t.data_ptr(), kind, rows, cols, t.stride(0) if rows > 1 else cols
 
 
 class Context:
@@ -432,102 +449,98 @@ class Context:
     # -- microscaled 4-bit values and experts ----------------------------
     def adadim_mx4_quantize(self, X, codes, scales, dW=None, dW_dtype: int = DW_F32, colscale=None):
         """X [rows, cols] (rows may be a pitched view) to codes and scales of the shapes mx4_shapes gives."""
-        _rows_of(X, "X", pitched=True)
-        kind, (rows, cols) = _type_of(X, "X"), X.shape
+        x, kind, rows, cols, pitch = _matrix(X, "X")
         c, s = mx4_shapes(rows, cols)
-        _rows_of(codes, "codes", "uint8", c)
-        _rows_of(scales, "scales", "uint8", s)
-        _need(dW, "dW", "float32" if dW_dtype == DW_F32 else "float16")
-        _need(colscale, "colscale", "float32")
-        need = score_elems(rows, cols) if dW_dtype == DW_F16_SCALED else rows * cols
-        if dW is not None and dW.numel() < need or colscale is not None and colscale.numel() < cols:
-            raise ValueError(f"dW needs {need} elements, colscale {cols}")
-        self._check(self._lib.adadim_mx4_quantize(self._h, _ptr(X), kind, rows, cols, _pitch(X), _ptr(codes), _ptr(scales), _ptr(dW),
-                                                  dW_dtype, _ptr(colscale)))
+        codes, scales = _array(codes, "codes", "torch.uint8", c), _array(scales, "scales", "torch.uint8", s)
+        if dW is not None:
+            _need(dW, "dW", "float32" if dW_dtype == DW_F32 else "float16")
+            _need(colscale, "colscale", "float32")
+            need = score_elems(rows, cols) if dW_dtype == DW_F16_SCALED else rows * cols
+            if dW.numel() < need or colscale is not None and colscale.numel() < cols:
+                raise ValueError(f"dW needs {need} elements, colscale {cols}")
+        rc = self._lib.adadim_mx4_quantize(self._h, x, kind, rows, cols, pitch, codes, scales, _ptr(dW), dW_dtype, _ptr(colscale))
+        if rc:
+            self._check(rc)
 
     def adadim_mx4_dequantize(self, codes, scales, Y):
         """The values of codes and scales into Y [rows, cols] (its rows may be pitched)."""
-        _rows_of(Y, "Y", pitched=True)
-        kind, (rows, cols) = _type_of(Y, "Y"), Y.shape
+        y, kind, rows, cols, pitch = _matrix(Y, "Y")
         c, s = mx4_shapes(rows, cols)
-        _rows_of(codes, "codes", "uint8", c)
-        _rows_of(scales, "scales", "uint8", s)
-        self._check(self._lib.adadim_mx4_dequantize(self._h, _ptr(codes), _ptr(scales), rows, cols, _ptr(Y), kind, _pitch(Y)))
+        codes, scales = _array(codes, "codes", "torch.uint8", c), _array(scales, "scales", "torch.uint8", s)
+        rc = self._lib.adadim_mx4_dequantize(self._h, codes, scales, rows, cols, y, kind, pitch)
+        if rc:
+            self._check(rc)
 
     def _mx4_input(self, X, x_scales, in_f):
-        """(in, type, tokens, pitch) of a product's left operand; mx4 codes are told by their type and need in_f."""
-        if str(X.dtype) == "torch.uint8":
+        """(address, scales' address, type, tokens, in, pitch) of a product's left operand; mx4 codes are told by their type
+        and need in_f."""
+        if _dtype(X)[0] == "torch.uint8":
             if in_f is None or x_scales is None:
                 raise ValueError("X in mx4 needs in_f and x_scales")
-            c, s = mx4_shapes(X.shape[0], in_f)
-            _rows_of(X, "X", "uint8", c)
-            _rows_of(x_scales, "x_scales", "uint8", s)
-            return in_f, TYPE_MX4, X.shape[0], 0
+            tokens = X.shape[0]
+            c, s = mx4_shapes(tokens, in_f)
+            return _array(X, "X", "torch.uint8", c), _array(x_scales, "x_scales", "torch.uint8", s), TYPE_MX4, tokens, in_f, 0
         if x_scales is not None:
             raise ValueError("x_scales go with X in mx4 (uint8 codes)")
-        _rows_of(X, "X", pitched=True)
-        kind = _type_of(X, "X")
-        if in_f is not None and X.shape[1] != in_f:
-            raise ValueError(f"X: expected {in_f} columns, got {X.shape[1]}")
-        return X.shape[1], kind, X.shape[0], _pitch(X)
+        x, kind, tokens, cols, pitch = _matrix(X, "X")
+        if in_f is not None and cols != in_f:
+            raise ValueError(f"X: expected {in_f} columns, got {cols}")
+        return x, None, kind, tokens, cols, pitch
 
     def adadim_mx4_matmul(self, X, codes, scales, Y, in_f: int | None = None, x_scales=None):
         """Y [tokens, out] = X W^T; X float16 or bfloat16 [tokens, in], or mx4 codes with x_scales and in_f."""
-        in_f, kind, tokens, ldx = self._mx4_input(X, x_scales, in_f)
-        _rows_of(Y, "Y", pitched=True)
-        y_kind, out = _type_of(Y, "Y"), Y.shape[1]
-        if Y.shape[0] != tokens:
-            raise ValueError(f"Y: expected {tokens} rows, got {Y.shape[0]}")
+        x, xs, kind, tokens, in_f, ldx = self._mx4_input(X, x_scales, in_f)
+        y, y_kind, rows, out, ldy = _matrix(Y, "Y")
+        if rows != tokens:
+            raise ValueError(f"Y: expected {tokens} rows, got {rows}")
         c, s = mx4_shapes(out, in_f)
-        _rows_of(codes, "codes", "uint8", c)
-        _rows_of(scales, "scales", "uint8", s)
-        self._check(self._lib.adadim_mx4_matmul(self._h, _ptr(X), _ptr(x_scales), kind, tokens, ldx, _ptr(codes), _ptr(scales), out,
-                                                in_f, _ptr(Y), y_kind, _pitch(Y)))
+        codes, scales = _array(codes, "codes", "torch.uint8", c), _array(scales, "scales", "torch.uint8", s)
+        rc = self._lib.adadim_mx4_matmul(self._h, x, xs, kind, tokens, ldx, codes, scales, out, in_f, y, y_kind, ldy)
+        if rc:
+            self._check(rc)
 
     def adadim_mx4_matmul_experts(self, X, codes, scales, offsets, Y, in_f: int | None = None, x_scales=None, rows=None):
         """Y[r] = X[rows[r]] W_e^T for the rows offsets[e] .. offsets[e + 1]; codes [experts, ..], scales [experts, ..]."""
-        in_f, kind, tokens, ldx = self._mx4_input(X, x_scales, in_f)
-        _rows_of(Y, "Y", pitched=True)
-        y_kind, (n_rows, out) = _type_of(Y, "Y"), Y.shape
+        x, xs, kind, tokens, in_f, ldx = self._mx4_input(X, x_scales, in_f)
+        y, y_kind, n_rows, out, ldy = _matrix(Y, "Y")
         experts = offsets.numel() - 1
         c, s = mx4_shapes(out, in_f)
-        _rows_of(codes, "codes", "uint8", (experts, *c))
-        _rows_of(scales, "scales", "uint8", (experts, *s))
-        _need(offsets, "offsets", "int32")
+        at = None
         if rows is not None:
-            _rows_of(rows, "rows", "int32", (n_rows,))
+            at = _array(rows, "rows", "torch.int32", (n_rows,))
         elif tokens != n_rows:
             raise ValueError(f"without rows X has as many rows as Y: got {tokens} and {n_rows}")
-        self._check(self._lib.adadim_mx4_matmul_experts(self._h, _ptr(X), _ptr(x_scales), kind, tokens, ldx, _ptr(rows), n_rows,
-                                                        _ptr(offsets), experts, _ptr(codes), _ptr(scales), out, in_f, _ptr(Y),
-                                                        y_kind, _pitch(Y)))
+        offsets = _array(offsets, "offsets", "torch.int32", (experts + 1,))
+        codes, scales = _array(codes, "codes", "torch.uint8", (experts, *c)), _array(scales, "scales", "torch.uint8", (experts, *s))
+        rc = self._lib.adadim_mx4_matmul_experts(self._h, x, xs, kind, tokens, ldx, at, n_rows, offsets, experts, codes, scales, out,
+                                                 in_f, y, y_kind, ldy)
+        if rc:
+            self._check(rc)
 
     def adadim_expert_route(self, logits, chosen, weights, offsets, rows, slots, renormalize: bool = True):
         """logits [tokens, experts] to chosen, weights, slots [tokens, k], offsets [experts + 1] and rows [tokens * k]."""
-        _rows_of(logits, "logits", pitched=True)
-        kind, (tokens, experts) = _type_of(logits, "logits"), logits.shape
-        _rows_of(chosen, "chosen", "int32")
-        k = chosen.shape[1]
-        _rows_of(chosen, "chosen", "int32", (tokens, k))
-        _rows_of(weights, "weights", "float32", (tokens, k))
-        _rows_of(slots, "slots", "int32", (tokens, k))
-        _rows_of(offsets, "offsets", "int32", (experts + 1,))
-        _rows_of(rows, "rows", "int32", (tokens * k,))
-        self._check(self._lib.adadim_expert_route(self._h, _ptr(logits), kind, tokens, _pitch(logits), experts, k,
-                                                  1 if renormalize else 0, _ptr(chosen), _ptr(weights), _ptr(offsets), _ptr(rows),
-                                                  _ptr(slots)))
+        l, kind, tokens, experts, ldl = _matrix(logits, "logits")
+        k = chosen.shape[-1]
+        choice = (tokens, k)
+        chosen, weights = _array(chosen, "chosen", "torch.int32", choice), _array(weights, "weights", "torch.float32", choice)
+        offsets = _array(offsets, "offsets", "torch.int32", (experts + 1,))
+        rows, slots = _array(rows, "rows", "torch.int32", (tokens * k,)), _array(slots, "slots", "torch.int32", choice)
+        rc = self._lib.adadim_expert_route(self._h, l, kind, tokens, ldl, experts, k, 1 if renormalize else 0, chosen, weights, offsets,
+                                           rows, slots)
+        if rc:
+            self._check(rc)
 
     def adadim_expert_combine(self, Z, slots, weights, Y):
         """Y [tokens, cols] = sum over j of weights[t, j] Z[slots[t, j]]."""
-        _rows_of(Z, "Z", pitched=True)
-        _rows_of(Y, "Y", pitched=True)
-        _rows_of(slots, "slots", "int32")
-        tokens, k = slots.shape
-        _rows_of(weights, "weights", "float32", (tokens, k))
-        if Y.shape[0] != tokens or Y.shape[1] != Z.shape[1]:
-            raise ValueError(f"Y: expected shape {(tokens, Z.shape[1])}, got {tuple(Y.shape)}")
-        self._check(self._lib.adadim_expert_combine(self._h, _ptr(Z), _type_of(Z, "Z"), Z.shape[0], Z.shape[1], _pitch(Z), _ptr(slots),
-                                                    _ptr(weights), tokens, k, _ptr(Y), _type_of(Y, "Y"), _pitch(Y)))
+        z, z_kind, n_rows, cols, ldz = _matrix(Z, "Z")
+        y, y_kind, tokens, y_cols, ldy = _matrix(Y, "Y")
+        k = slots.shape[-1]
+        if y_cols != cols:
+            raise ValueError(f"Y: expected {cols} columns, got {y_cols}")
+        slots, weights = _array(slots, "slots", "torch.int32", (tokens, k)), _array(weights, "weights", "torch.float32", (tokens, k))
+        rc = self._lib.adadim_expert_combine(self._h, z, z_kind, n_rows, cols, ldz, slots, weights, tokens, k, y, y_kind, ldy)
+        if rc:
+            self._check(rc)
 
     def adadim_probe_mfma_f64(self, iters: int = 20000):
         """(TFLOP/s, shader clock in MHz) of a register-resident fp64 MFMA loop; waits for the stream."""
