@@ -84,7 +84,7 @@ static int product_checked(adadim_ctx* ctx, const char* me, int x_type, const mx
 int adadim_mx4_matmul(adadim_ctx* ctx, const void* X, const uint8_t* x_scales, int x_type, int64_t tokens, int64_t ldx,
                       const uint8_t* codes, const uint8_t* scales, int64_t out, int64_t in, void* Y, int y_type, int64_t ldy) {
     if (!ctx) return ADADIM_ENULL;
-    const mx4::Product a{X, reinterpret_cast<const uint32_t*>(x_scales), tokens, ldx, nullptr, nullptr, tokens, 1, codes,
+    const mx4::Product a{X, reinterpret_cast<const uint32_t*>(x_scales), tokens, ldx, tokens, nullptr, false, nullptr, tokens, 1, codes,
                          reinterpret_cast<const uint32_t*>(scales), out, in, Y, y_type, ldy};
     return product_checked(ctx, "adadim_mx4_matmul", x_type, a);
 }
@@ -100,7 +100,7 @@ int adadim_mx4_matmul_experts(adadim_ctx* ctx, const void* X, const uint8_t* x_s
                            (long long)n_rows);
     if (!offsets) return adadim_fail(ctx, ADADIM_ENULL, "%s: offsets is NULL", me);
     if (!aligned_to(offsets, 4) || !aligned_to(rows, 4)) return adadim_fail(ctx, ADADIM_EALIGN, "%s: offsets and rows must be 4-byte aligned", me);
-    const mx4::Product a{X, reinterpret_cast<const uint32_t*>(x_scales), tokens, ldx, rows, offsets, n_rows, experts, codes,
+    const mx4::Product a{X, reinterpret_cast<const uint32_t*>(x_scales), tokens, ldx, tokens, rows, rows != nullptr, offsets, n_rows, experts, codes,
                          reinterpret_cast<const uint32_t*>(scales), out, in, Y, y_type, ldy};
     return product_checked(ctx, me, x_type, a);
 }

@@ -37,6 +37,7 @@ enum {
     WS_GPTQ_V,          // int32 position of each original channel in the visiting order
     WS_PROBE,           // output of the matrix-core rate probe
     WS_MX4_X,           // rows of X copied to where 16-byte transfers can take them
+    WS_MX4_PART,        // counters of the few-row products' output tiles, then their partial outputs
     WS_ROUTE,           // the router's masks of tokens per expert and the places behind them
     WS_COUNT
 };
@@ -64,6 +65,7 @@ struct adadim_ctx {
     void* ws[WS_COUNT];
     size_t ws_bytes[WS_COUNT];
     size_t zero_ready_bytes;         // size of WS_ZERO when it was last cleared
+    size_t mx4_ready_bytes;          // size of WS_MX4_PART when its counters were last cleared
     size_t gemv_ready_bytes;         // size of WS_GEMV_PART when its counters were last cleared
     // Gram launch plans already chosen, keyed by (token count, tile count, whether whole tiles may store): choosing
     // one simulates the launch's schedule (milliseconds of host time), and a model driver alternates between a few

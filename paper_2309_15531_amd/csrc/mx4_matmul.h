@@ -11,8 +11,10 @@ namespace mx4 {
 struct Product {
     const void* X;
     const uint32_t* x_scales;      // mx4 only
-    int64_t tokens, ldx;           // rows of X, their pitch in elements (mx4: the codes are contiguous)
+    int64_t tokens, ldx;           // rows of X that rows[] may name, their pitch in elements (mx4: the codes are contiguous)
+    int64_t x_rows;                // words of a piece of x_scales
     const int32_t* rows;           // or null
+    bool gather;                   // row r of Y is that of row rows[r] of X (otherwise X has been brought into that order)
     const int32_t* offsets;        // or null: one group of all rows
     int64_t n_rows;
     int experts;
@@ -42,11 +44,12 @@ __device__ __forceinline__ Group group_of(const Product& a, int e) {
     return g;
 }
 
-// The row of X behind row r of Y; -1 (read as zeros) behind the group's end or where rows[] names none.
+// The row of X behind row r of Y; -1 behind the group's end or where rows[] names none (that row of Y is zeros).
 __device__ __forceinline__ int64_t source_row(const Product& a, int64_t r, int64_t hi) {
     if (r >= hi) return -1;
-    const int64_t s = a.rows ? int64_t(a.rows[r]) : r;
-    return s >= 0 && s < a.tokens ? s : -1;
+    if (!a.rows) return r;
+    const int64_t s = a.rows[r];
+    return s >= 0 && s < a.tokens ? (a.gather ? s : r) : -1;
 }
 
 __device__ __forceinline__ void store_y(const Product& a, int64_t row, int64_t col, float v) {

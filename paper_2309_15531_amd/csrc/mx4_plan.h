@@ -1,0 +1,102 @@
+// Which kernel a microscaled product takes, from its sizes and X's type.  Host code without HIP.
+//
+// The kernels differ in how much of Y a workgroup owns.  Large tiles read each operand less often; small ones are more, start sooner and
+// leave fewer compute units idle, and where even they are few the contraction is shared.  Which is ahead depends on all of rows, outputs,
+// contraction, X's type and the groups, so each form's time is estimated and the shortest taken.  The estimates are fits to the
+// kernels' times over shapes drawn at random (1 to 8192 rows, 64 to 28672 outputs, 64 to 11008 deep; 4 to 64 experts): mean error 8 to 20 % a form, and
+// the form chosen is 2 % (one weight) and 5 % (experts) slower in the geometric mean than the best of them all.
+#pragma once
+
+#include <algorithm>
+#include <cstdint>
+
+namespace mx4 {
+
+// rows: 16 out_tiles outputs, a wave a share of the pieces.  The others by their tile (rows x outputs): ring32 32 x 256 (mx4 X: 32 x 128), ring64
+// 64 x 64, ring64w 64 x 128, mid 128 x 128, wide 128 x 256 (16-bit X only), big 256 x 256.
+enum class Form { rows, ring32, ring64, ring64w, mid, wide, big };
+
+struct Plan {
+    Form form;
+    int shares;                    // of the contraction
+    int out_tiles, row_tiles;      // of 16, of a workgroup (rows)
+};
+
+constexpr int MOST_SHARED = 1024;  // output tiles that can be shared: each has a counter
+
+struct TileForm {
+    Form form;
+    int bm, bn, pieces;            // the tile, pieces of a stage
+    bool shares;
+    float start, tile, stage;      // us: of the launch, of a tile, of a stage
+    float fill;                    // workgroups that run at once, over 256
+    float steps;                   // how far a last round that is not full counts as one: 1 wholly, 0 by its share
+    float share;                   // us: of adding up
+};
+constexpr TileForm TILE_FORMS_16[] = {
+    {Form::ring32, 32, 256, 1, true, 1.50f, 3.49f, 0.694f, 0.94f, 0.86f, 1.3f}, {Form::ring64, 64, 64, 1, true, 2.18f, 2.81f, 0.585f, 1.34f, 0.19f, 1.5f},
+    {Form::ring64w, 64, 128, 1, true, 3.42f, 2.24f, 0.765f, 1.20f, 0.19f, 2.4f}, {Form::mid, 128, 128, 1, true, 2.60f, 3.25f, 0.931f, 0.80f, 0.0f, 2.4f},
+    {Form::wide, 128, 256, 1, true, 5.20f, 1.41f, 1.348f, 0.88f, 1.0f, 4.0f},    {Form::big, 256, 256, 1, false, 2.76f, 6.00f, 2.596f, 0.81f, 0.68f, 0.0f}};
+constexpr TileForm TILE_FORMS_MX[] = {
+    {Form::ring32, 32, 128, 1, true, 3.14f, 1.33f, 0.233f, 0.94f, 0.52f, 1.4f},  {Form::ring64, 64, 64, 1, true, 2.91f, 1.42f, 0.217f, 1.44f, 0.56f, 1.3f},
+    {Form::ring64w, 64, 128, 1, true, 3.63f, 1.07f, 0.253f, 0.95f, 0.54f, 2.3f}, {Form::mid, 128, 128, 2, false, 1.64f, 3.74f, 0.642f, 1.0f, 0.14f, 0.0f},
+    {Form::big, 256, 256, 2, false, 1.50f, 5.04f, 1.515f, 0.82f, 1.0f, 0.0f}};
+struct RowForm {
+    int out_tiles;
+    float start, pass, piece, rows;   // us: of the launch, of a pass over the contraction, of a wave's piece, and of 16 rows of X with it
+    float fill, share;
+};
+constexpr RowForm ROW_FORMS_16[] = {{1, 3.87f, 0.66f, 0.03f, 1.12f, 0.84f, 0.7f}, {2, 3.98f, 0.89f, 0.11f, 1.53f, 0.8f, 0.6f}, {4, 4.14f, 0.88f, 0.49f, 2.31f, 0.8f, 0.6f}};
+constexpr RowForm ROW_FORMS_MX[] = {{1, 3.08f, 0.36f, 0.14f, 0.32f, 0.8f, 1.1f}, {2, 3.32f, 0.23f, 0.27f, 0.63f, 0.81f, 0.8f}, {4, 3.07f, 0.57f, 0.68f, 1.35f, 0.8f, 0.8f}};
+
+// experts 0: one weight.
+inline Plan mx4_plan(int64_t n_rows, int64_t out, int64_t in, int experts, bool mx) {
+    const double np = double((in + 127) / 128);
+    const double active = experts ? double(std::min<int64_t>(experts, n_rows)) : 1.0;         // groups that may have rows
+    const double weight = active * double(out) * np * 68.0;                                   // bytes of W
+    const double avg = double(n_rows) / active;
+    const double part = double(n_rows) * double(out) * 8.0;                                   // bytes of a share's sums, out and back
+    auto up = [](double v) { return double(int64_t(v) + (double(int64_t(v)) < v)); };
+    Plan best{Form::ring64, 1, 0, 0};
+    double least = 1e30;
+    auto take = [&](double t, Plan p) {
+        if (t < least) {
+            least = t;
+            best = p;
+        }
+    };
+    // few rows: at most six passes of 64 over a group
+    const int64_t per_group = experts ? (n_rows + experts - 1) / experts : n_rows;
+    if (per_group <= 96) {
+        const int rt = per_group <= 16 ? 1 : per_group <= 32 ? 2 : 4;
+        const double loops = std::max(1.0, (experts ? 2.0 : 1.0) * avg / (16 * rt));          // of the longest group
+        for (const RowForm& f : mx ? ROW_FORMS_MX : ROW_FORMS_16) {
+            const double tiles = up(double(out) / (16 * f.out_tiles));
+            for (int s = 1; s <= 8; s *= 2) {
+                if (s > 1 && (experts || n_rows > 64 || s > np || tiles > MOST_SHARED)) break;
+                const double rounds = std::max(1.0, active * tiles * s / (256 * f.fill)), rows = std::min(avg / loops, 16.0 * rt);
+                double t = f.start + rounds * loops * (f.pass + up(np / (8 * s)) * (f.piece + f.rows * rows / 16.0));
+                t = std::max(t, f.start + weight / 5.2e6) + (s > 1 ? f.share : 0.0);
+                take(t, Plan{Form::rows, s, f.out_tiles, rt});
+            }
+        }
+    }
+    auto tile = [&](const TileForm& f) {
+        const double rt = experts ? std::max(active, double(n_rows) / f.bm + 0.5 * active) : up(double(n_rows) / f.bm);
+        const double tiles = rt * up(double(out) / f.bn);
+        for (int s = 1; s <= (f.shares && !experts ? 8 : 1); s *= 2) {
+            if (s > 1 && (s > np || tiles * s > MOST_SHARED)) break;
+            const double full = std::max(1.0, tiles * s / (256 * f.fill)), rounds = f.steps * up(full - 1e-9) + (1.0 - f.steps) * full;
+            double t = f.start + rounds * (f.tile + up(np / (s * f.pieces)) * f.stage);
+            t = std::max(t, f.start + weight / 5.0e6) + (s > 1 ? f.share + s * part / 6.0e6 : 0.0);
+            take(t, Plan{f.form, s, 0, 0});
+        }
+    };
+    if (mx)
+        for (const TileForm& f : TILE_FORMS_MX) tile(f);
+    else
+        for (const TileForm& f : TILE_FORMS_16) tile(f);
+    return best;
+}
+
+}  // namespace mx4

@@ -106,6 +106,49 @@ __device__ __forceinline__ bool tile_of(const Product& a, Tile& t) {
     return true;
 }
 
+// Y of a wave: TT x 32 rows from `row0`, TO x 32 outputs from `out0`.  Of each 32 x 32 block a lane holds row lane & 31 and outputs
+// 8 q + 4 (lane >> 5) .. + 3.  32 rows at a time are turned through LDS of the wave's own, and stored 16 bytes a lane.
+template <int TO, int TT, int NW>
+__device__ __forceinline__ void store_tile(const Product& a, const float16v (&acc)[TO][TT], uint32_t lds0, int wave, int lane, int64_t row0,
+                                           int64_t row_end, int64_t out0) {
+    const int fr = lane & 31, fh = lane >> 5;
+    auto store = [&](auto tag) {
+        typedef decltype(tag) TY;
+        constexpr int N = 16 / sizeof(TY), COLS = TO * 32, PITCH = COLS * sizeof(TY) + 16, LANES = COLS / N, PER = 64 / LANES;
+        typedef TY outv __attribute__((ext_vector_type(N)));
+        typedef TY quad __attribute__((ext_vector_type(4)));
+        const uint32_t mine = lds0 + wave * 32 * PITCH;
+#pragma unroll
+        for (int i = 0; i < TT; ++i) {
+#pragma unroll
+            for (int o = 0; o < TO; ++o)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    quad v;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) v[r] = static_cast<TY>(acc[o][i][4 * q + r]);
+                    lds_write(mine + fr * PITCH + (32 * o + 8 * q + 4 * fh) * sizeof(TY), v);
+                }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int r0 = 0; r0 < 32; r0 += PER) {
+                const int row = r0 + lane / LANES, col = (lane % LANES) * N;
+                const int64_t r = row0 + i * 32 + row, c = out0 + col;
+                uint4v v = lds_read16(mine + row * PITCH + col * sizeof(TY));
+                if (r < row_end && c < a.out) {
+                    if (a.rows && source_row(a, r, row_end) < 0) v = uint4v{};
+                    Chunk<TY, N>::store(static_cast<TY*>(a.Y) + r * a.ldy + c, static_cast<int>(min(int64_t(N), a.out - c)),
+                                        __builtin_bit_cast(outv, v));
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    };
+    if (a.y_type == ADADIM_TYPE_F16) store(_Float16{});
+    else if (a.y_type == ADADIM_TYPE_BF16) store(__bf16{});
+    else store(float{});
+}
+
 }  // namespace tiles
 
 // Y tile of BM rows x BN outputs by WT x WO waves (along the rows, along the outputs).
@@ -139,20 +182,20 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(Product a) {
     // a row of X to read in place of one that does not exist: its products are not stored, or stored as zeros
     auto x_row = [&](int i) {
         const int64_t s = source_row(a, r_first + i, gr.hi);
-        return s < 0 ? int64_t(0) : s;
+        return s < 0 ? (a.gather ? int64_t(0) : r_first) : s;
     };
     // Transfers.  Number i of a wave takes ROWS_PER rows; every lane has the same chunk in all of them.  They are given as 32-bit offsets
-    // from a row that all share: the tile's first (W; X without rows[]) or that of token 0, which the host holds within 4 GB.
+    // from a row that all share: the tile's first (W; X in Y's order) or that of token 0, which the host holds within 4 GB.
     static_assert(NW % 4 == 0, "the swizzle is the same for all transfers of a wave");
     const int t_row = ROWS_PER * wave + lane / CH, t_chunk = (lane % CH) ^ swizzle<CH>(t_row);
-    const int64_t x_pitch = MX ? np * PIECE_BYTES : 2 * a.ldx, x_first = a.rows ? 0 : r_first;
+    const int64_t x_pitch = MX ? np * PIECE_BYTES : 2 * a.ldx, x_first = a.gather ? 0 : r_first;
     uint32_t xo[XL], wofs[MX ? WL : 1];
     const char* x_base = uniform(static_cast<const char*>(a.X) + x_first * x_pitch);
     const char* w_base = uniform(gr.codes + t.out0 * np * PIECE_BYTES);
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
         const int row = t_row + ROWS_PER * NW * i;
-        xo[i] = static_cast<uint32_t>((a.rows ? x_row(row) : min(int64_t(row), gr.hi - 1 - r_first)) * x_pitch + 16 * t_chunk);
+        xo[i] = static_cast<uint32_t>((a.gather ? x_row(row) : min(int64_t(row), gr.hi - 1 - r_first)) * x_pitch + 16 * t_chunk);
     }
     if constexpr (MX) {
 #pragma unroll
@@ -205,7 +248,7 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(Product a) {
 #pragma unroll
             for (int o = 0; o < TO; ++o) d.ws[o] = gr.scales[at * a.out + w_row[o]];
 #pragma unroll
-            for (int i = 0; i < TT; ++i) d.xs[i] = a.x_scales[at * a.tokens + x_src[i]];
+            for (int i = 0; i < TT; ++i) d.xs[i] = a.x_scales[at * a.x_rows + x_src[i]];
             if (q == 0 && p >= np) {                          // half a stage: what it lacks are zeros, of scale 1
 #pragma unroll
                 for (int o = 0; o < TO; ++o) d.ws[o] = ONE_WORD;
@@ -389,44 +432,8 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(Product a) {
         }
     }
 
-    // ---- Y: a lane holds, of each 32 x 32 block, token fr and outputs 8 q + 4 h .. + 3.  A wave turns 32 tokens x its outputs through LDS of
-    // its own and stores rows of 16 bytes a lane.
-    auto store = [&](auto tag) {
-        typedef decltype(tag) TY;
-        constexpr int N = 16 / sizeof(TY), COLS = TO * 32, PITCH = COLS * sizeof(TY) + 16, LANES = COLS / N, PER = 64 / LANES;
-        static_assert(NW * 32 * PITCH <= 2 * STAGE, "room");
-        typedef TY outv __attribute__((ext_vector_type(N)));
-        typedef TY quad __attribute__((ext_vector_type(4)));
-        const uint32_t mine = lds0 + wave * 32 * PITCH;
-#pragma unroll
-        for (int i = 0; i < TT; ++i) {
-#pragma unroll
-            for (int o = 0; o < TO; ++o)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    quad v;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) v[r] = static_cast<TY>(acc[o][i][4 * q + r]);
-                    lds_write(mine + fr * PITCH + (32 * o + 8 * q + 4 * fh) * sizeof(TY), v);
-                }
-            __builtin_amdgcn_wave_barrier();
-#pragma unroll
-            for (int r0 = 0; r0 < 32; r0 += PER) {
-                const int row = r0 + lane / LANES, col = (lane % LANES) * N;
-                const int64_t r = r_first + (wt * TT + i) * 32 + row, c = t.out0 + wo * COLS + col;
-                uint4v v = lds_read16(mine + row * PITCH + col * sizeof(TY));
-                if (r < gr.hi && c < a.out) {
-                    if (a.rows && source_row(a, r, gr.hi) < 0) v = uint4v{};
-                    Chunk<TY, N>::store(static_cast<TY*>(a.Y) + r * a.ldy + c, static_cast<int>(min(int64_t(N), a.out - c)),
-                                        __builtin_bit_cast(outv, v));
-                }
-            }
-            __builtin_amdgcn_wave_barrier();
-        }
-    };
-    if (a.y_type == ADADIM_TYPE_F16) store(_Float16{});
-    else if (a.y_type == ADADIM_TYPE_BF16) store(__bf16{});
-    else store(float{});
+    static_assert(NW * 32 * (TO * 32 * 4 + 16) <= 2 * STAGE, "room for the outputs");
+    store_tile<TO, TT, NW>(a, acc, lds0, wave, lane, r_first + wt * TT * 32, gr.hi, t.out0 + wo * TO * 32);
 }
 
 }  // namespace
