@@ -16,11 +16,9 @@ __device__ __forceinline__ uint32_t score_key(float f) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-template <class T>
-__device__ __forceinline__ float score(const T* p) { return static_cast<float>(*p); }
-
 constexpr int RT_TOKENS = 64;                     // tokens of a chunk: one bit each of an expert's mask
-constexpr int RT_WAVES = 8;
+constexpr int RT_THREADS = 1024;
+constexpr int RT_GROUPS = 256;                    // workgroups that place rows, at most
 
 struct Route {
     const void* logits;
@@ -29,129 +27,213 @@ struct Route {
     int32_t* chosen;
     float* weights;
     int32_t *offsets, *rows, *slots;
-    uint64_t* masks;                              // [chunks][experts]
-    int32_t* bases;                               // [chunks][experts]
+    uint64_t* masks;                              // [chunks][experts]: the tokens of the chunk that chose the expert
+    uint8_t* counts;                              // [chunks][experts, up to the next multiple of 4]: how many
 };
 
-// A wave per token: every lane holds the scores lane, lane + 64, ..; k times the largest one left.
-template <class T, int V>
-__global__ __launch_bounds__(64 * RT_WAVES) void route_choose(Route a) {
-    extern __shared__ uint32_t s_mask[];          // [experts][2]
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+    return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, 0xF, 0xF, false));
+}
+constexpr int QUAD_XOR1 = 0xB1, QUAD_XOR2 = 0x4E, HALF_MIRROR = 0x141, ROW_MIRROR = 0x140;
+// f over the W (8 or 16) lanes of a token, the result in all of them
+template <int W, class F>
+__device__ __forceinline__ uint32_t over_lanes(uint32_t v, F f) {
+    v = f(v, dpp<QUAD_XOR1>(v));
+    v = f(v, dpp<QUAD_XOR2>(v));
+    v = f(v, dpp<HALF_MIRROR>(v));
+    if constexpr (W == 16) v = f(v, dpp<ROW_MIRROR>(v));
+    return v;
+}
+
+// The sums of n (at most RT_THREADS) numbers in front of each, and of all; s_sum: RT_THREADS / 64 words.
+__device__ __forceinline__ int32_t sum_before(int32_t n, int32_t& all, int32_t* s_sum) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int i = threadIdx.x; i < 2 * a.experts; i += 64 * RT_WAVES) s_mask[i] = 0u;
+    int32_t sum = n;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int32_t o = __shfl_up(sum, d);
+        if (lane >= d) sum += o;
+    }
+    if (lane == 63) s_sum[wave] = sum;
     __syncthreads();
-    for (int tt = wave; tt < RT_TOKENS; tt += RT_WAVES) {
+    int32_t before = 0;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < RT_THREADS / 64; ++w) {
+        if (w < wave) before += s_sum[w];
+        all += s_sum[w];
+    }
+    return before + sum - n;
+}
+
+// The rows and slots of chunk c, whose rows of expert e begin at base[e].
+__device__ __forceinline__ void place_chunk(const Route& a, int64_t c, const uint64_t* mask, const int32_t* base) {
+    const int64_t t0 = c * RT_TOKENS;
+    const int n = static_cast<int>(min(int64_t(RT_TOKENS), a.tokens - t0)) * a.k;
+    for (int i = threadIdx.x; i < n; i += RT_THREADS) {
+        const int tt = i / a.k;
+        const int32_t e = a.chosen[t0 * a.k + i];
+        int32_t slot = -1;
+        if (e >= 0) {
+            slot = base[e] + __popcll(mask[e] & ((uint64_t(1) << tt) - 1));
+            a.rows[slot] = static_cast<int32_t>(t0 + tt);
+        }
+        a.slots[t0 * a.k + i] = slot;
+    }
+}
+
+// A chunk of 64 tokens.  W lanes a token, V consecutive scores each: k times the largest left, over a lane's own and then over the lanes by DPP,
+// its lowest index the same way.  Fewer lanes with more scores each would be less work still, but the loads would no longer be whole
+// lines.  Where the chunk is all there is, the rows are placed too, in the same launch.
+template <class T, int W, int V>
+__global__ __launch_bounds__(RT_THREADS) void route_choose(Route a) {
+    extern __shared__ uint64_t s_mask[];          // [experts], then int32 [experts]
+    __shared__ int32_t s_sum[RT_THREADS / 64];
+    const int sub = threadIdx.x % W;
+    for (int i = threadIdx.x; i < a.experts; i += RT_THREADS) s_mask[i] = 0u;
+    __syncthreads();
+    for (int tt = threadIdx.x / W; tt < RT_TOKENS; tt += RT_THREADS / W) {
         const int64_t t = int64_t(blockIdx.x) * RT_TOKENS + tt;
-        if (t >= a.tokens) break;
-        const T* l = static_cast<const T*>(a.logits) + t * a.ldl;
+        const bool real = t < a.tokens;           // (all lanes go through the moves between lanes)
         float f[V];
         uint32_t key[V];
+        const T* l = static_cast<const T*>(a.logits) + (real ? t : 0) * a.ldl + sub * V;
+        const int have = a.experts - sub * V;
+        typedef T vec __attribute__((ext_vector_type(V)));
+        if (have >= V) {
+            vec v;
+            __builtin_memcpy(&v, l, sizeof(v));
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int e = lane + 64 * v;
-            f[v] = e < a.experts ? score(l + e) : -INFINITY;
-            key[v] = score_key(f[v]);
+            for (int v_ = 0; v_ < V; ++v_) f[v_] = static_cast<float>(v[v_]);
+        } else {
+#pragma unroll
+            for (int v_ = 0; v_ < V; ++v_) f[v_] = v_ < have ? static_cast<float>(l[v_]) : -INFINITY;
         }
-        float top = 0.0f, sum = 0.0f;
-        float mine = 0.0f;                        // lane j: exp(l - max) of the j-th chosen
-        int32_t index = -1;
+#pragma unroll
+        for (int v = 0; v < V; ++v) key[v] = score_key(f[v]);
+        float top = 0.0f, sum = 0.0f, mine[2] = {};           // lane j (and j + W): exp(l - max) of the j-th chosen
+        int32_t index[2] = {-1, -1};
         for (int j = 0; j < a.k; ++j) {
             uint32_t best = 0u;
-            int at = 0x7fffffff;
+#pragma unroll
+            for (int v = 0; v < V; ++v) best = max(best, key[v]);
+            best = over_lanes<W>(best, [](uint32_t x, uint32_t y) { return max(x, y); });
+            uint32_t at = 0xffffffffu;
+#pragma unroll
+            for (int v = V - 1; v >= 0; --v)
+                if (key[v] == best) at = sub * V + v;
+            at = over_lanes<W>(at, [](uint32_t x, uint32_t y) { return min(x, y); });
+            if (__ballot(best != 0u) == 0) break;             // nothing left of any of the wave's tokens
 #pragma unroll
             for (int v = 0; v < V; ++v)
-                if (key[v] > best) {
-                    best = key[v];
-                    at = lane + 64 * v;
+                if (at == static_cast<uint32_t>(sub * V + v)) key[v] = 0u;
+            if (best != 0u) {
+                const uint32_t u = best & 0x80000000u ? best & 0x7fffffffu : ~best;            // back from the key
+                const float val = __uint_as_float(u);
+                if (j == 0) top = val;
+                const float p = val == top ? 1.0f : expf(val - top);
+                sum += p;
+                if (sub == j % W) {
+                    mine[W == 16 && j >= W] = p;
+                    index[W == 16 && j >= W] = static_cast<int32_t>(at);
                 }
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const uint32_t ob = __shfl_xor(best, d);
-                const int oa = __shfl_xor(at, d);
-                if (ob > best || (ob == best && oa < at)) {
-                    best = ob;
-                    at = oa;
-                }
+                if (sub == 0 && real) atomicOr(reinterpret_cast<unsigned long long*>(&s_mask[at]), 1ull << tt);
             }
-            if (best == 0u) break;                // nothing left (the same in every lane)
-            float val = 0.0f;
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (at == lane + 64 * v) {
-                    key[v] = 0u;
-                    val = f[v];
-                }
-            val = __shfl(val, at & 63);
-            if (j == 0) top = val;
-            const float p = val == top ? 1.0f : expf(val - top);
-            sum += p;
-            if (lane == j) {
-                mine = p;
-                index = at;
-            }
-            if (lane == 0) atomicOr(&s_mask[2 * at + (tt >> 5)], 1u << (tt & 31));
         }
         if (!a.renormalize) {
             sum = 0.0f;
 #pragma unroll
             for (int v = 0; v < V; ++v)
                 if (f[v] > -INFINITY) sum += f[v] == top ? 1.0f : expf(f[v] - top);
+            sum = __uint_as_float(over_lanes<W>(__float_as_uint(sum), [](uint32_t x, uint32_t y) {
+                return __float_as_uint(__uint_as_float(x) + __uint_as_float(y));
+            }));
+            sum = __shfl(sum, (threadIdx.x & 63) & ~(W - 1));         // (the lanes added in different orders)
+        }
 #pragma unroll
-            for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-        }
-        if (lane < a.k) {
-            a.chosen[t * a.k + lane] = index;
-            a.weights[t * a.k + lane] = index >= 0 ? mine / sum : 0.0f;
-        }
+        for (int h = 0; h < (W == 16 ? 2 : 1); ++h)
+            if (real && sub + h * W < a.k) {
+                a.chosen[t * a.k + sub + h * W] = index[h];
+                a.weights[t * a.k + sub + h * W] = index[h] >= 0 ? mine[h] / sum : 0.0f;
+            }
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < a.experts; e += 64 * RT_WAVES)
-        a.masks[int64_t(blockIdx.x) * a.experts + e] = uint64_t(s_mask[2 * e]) | uint64_t(s_mask[2 * e + 1]) << 32;
+    const int e = threadIdx.x;
+    const int32_t n = e < a.experts ? __popcll(s_mask[e]) : 0;
+    if (gridDim.x > 1) {
+        const int pitch = (a.experts + 3) & ~3;
+        if (e < a.experts) a.masks[int64_t(blockIdx.x) * a.experts + e] = s_mask[e];
+        if (e < pitch) a.counts[int64_t(blockIdx.x) * pitch + e] = static_cast<uint8_t>(n);
+        return;
+    }
+    int32_t all, *s_base = reinterpret_cast<int32_t*>(s_mask + a.experts);
+    const int32_t at = sum_before(n, all, s_sum);
+    if (e < a.experts) {
+        s_base[e] = at;
+        a.offsets[e] = at;
+        if (e == a.experts - 1) a.offsets[a.experts] = all;
+    }
+    __syncthreads();                              // (the choices above are visible to the workgroup, too)
+    place_chunk(a, 0, s_mask, s_base);
+    for (int64_t i = all + e; i < a.tokens * a.k; i += RT_THREADS) a.rows[i] = -1;
 }
 
-// One workgroup: the experts' totals and their sums, then where each chunk's rows of each expert begin.
-__global__ __launch_bounds__(1024) void route_bases(Route a, int64_t chunks) {
-    __shared__ int32_t s_sum[1024];
-    const int e = threadIdx.x;
-    int32_t n = 0;
-    if (e < a.experts)
-        for (int64_t c = 0; c < chunks; ++c) n += __popcll(a.masks[c * a.experts + e]);
-    s_sum[e] = n;
+// Several chunks: workgroup g places the rows of `per` of them.  It adds up the counts of all chunks (four experts to a word, the
+// rows of counts dealt to the threads), once for those in front of its own and once for all.
+__global__ __launch_bounds__(RT_THREADS) void route_place(Route a, int64_t chunks, int64_t per) {
+    extern __shared__ int32_t s_total[];          // [2][experts up to 4]: of all chunks, of those in front
+    __shared__ int32_t s_sum[RT_THREADS / 64];
+    const int pitch = (a.experts + 3) & ~3, words = pitch / 4;
+    int32_t* const s_before = s_total + pitch;
+    const int64_t first = blockIdx.x * per, last = min(first + per, chunks);
+    for (int i = threadIdx.x; i < 2 * pitch; i += RT_THREADS) s_total[i] = 0;
     __syncthreads();
-    for (int d = 1; d < 1024; d *= 2) {
-        const int32_t before = e >= d ? s_sum[e - d] : 0;
-        __syncthreads();
-        s_sum[e] += before;
-        __syncthreads();
-    }
-    if (e < a.experts) {
-        int32_t at = s_sum[e] - n;
-        if (e == 0) a.offsets[0] = 0;
-        a.offsets[e + 1] = s_sum[e];
-        for (int64_t c = 0; c < chunks; ++c) {
-            a.bases[c * a.experts + e] = at;
-            at += __popcll(a.masks[c * a.experts + e]);
+    const int lanes = RT_THREADS / words;         // rows of counts at a time (words <= 256)
+    if (static_cast<int>(threadIdx.x) < lanes * words) {
+        const int w = threadIdx.x % words;
+        const uint32_t* counts = reinterpret_cast<const uint32_t*>(a.counts) + w;
+        int32_t total[4] = {}, before[4] = {};
+        for (int64_t c0 = threadIdx.x / words; c0 < chunks; c0 += 8 * lanes) {
+            uint32_t q[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) q[u] = c0 + u * lanes < chunks ? counts[(c0 + u * lanes) * words] : 0u;
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const int32_t n = (q[u] >> (8 * b)) & 255u;
+                    total[b] += n;
+                    if (c0 + u * lanes < first) before[b] += n;
+                }
         }
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            atomicAdd(&s_total[4 * w + b], total[b]);         // (whole numbers: the order does not show)
+            atomicAdd(&s_before[4 * w + b], before[b]);
+        }
+    }
+    __syncthreads();
+    const int e = threadIdx.x;
+    int32_t all;
+    const int32_t at = sum_before(e < a.experts ? s_total[e] : 0, all, s_sum);
+    if (e < a.experts) {
+        s_before[e] += at;
+        if (blockIdx.x == 0) {
+            a.offsets[e] = at;
+            if (e == a.experts - 1) a.offsets[a.experts] = all;
+        }
+    }
+    __syncthreads();
+    for (int64_t c = first; c < last; ++c) {
+        place_chunk(a, c, a.masks + c * a.experts, s_before);
+        __syncthreads();
+        if (e < a.experts) s_before[e] += __popcll(a.masks[c * a.experts + e]);
+        __syncthreads();
     }
     // the places that no row takes
-    const int64_t all = a.tokens * a.k;
-    for (int64_t i = s_sum[1023] + int64_t(e); i < all; i += 1024) a.rows[i] = -1;
-}
-
-__global__ __launch_bounds__(256) void route_place(Route a) {
-    const int64_t t0 = int64_t(blockIdx.x) * RT_TOKENS;
-    const int n = static_cast<int>(min(int64_t(RT_TOKENS), a.tokens - t0)) * a.k;
-    for (int i = threadIdx.x; i < n; i += 256) {
-        const int tt = i / a.k;
-        const int32_t e = a.chosen[t0 * a.k + i];
-        int32_t slot = -1;
-        if (e >= 0) {
-            const int64_t at = int64_t(blockIdx.x) * a.experts + e;
-            slot = a.bases[at] + __popcll(a.masks[at] & ((uint64_t(1) << tt) - 1));
-            a.rows[slot] = static_cast<int32_t>(t0 + tt);
-        }
-        a.slots[t0 * a.k + i] = slot;
-    }
+    const int64_t end = min(last * RT_TOKENS, a.tokens) * a.k;
+    for (int64_t i = max(first * RT_TOKENS * a.k, int64_t(all)) + e; i < end; i += RT_THREADS) a.rows[i] = -1;
 }
 
 __global__ void route_none(int32_t* offsets, int experts) {
@@ -207,23 +289,29 @@ int launch_expert_route(adadim_ctx* ctx, const void* logits, int type, int64_t t
         ADADIM_LAUNCH_CHECK(ctx, "route_none");
         return ADADIM_OK;
     }
-    const int64_t chunks = (tokens + RT_TOKENS - 1) / RT_TOKENS;
-    char* ws = static_cast<char*>(adadim_workspace(ctx, WS_ROUTE, size_t(chunks) * size_t(experts) * 12));
-    if (!ws) return ADADIM_EHIP;
-    uint64_t* masks = reinterpret_cast<uint64_t*>(ws);
-    const Route a{logits, tokens, ldl, experts, k, renormalize, chosen, weights, offsets, rows, slots, masks,
-                  reinterpret_cast<int32_t*>(masks + chunks * experts)};
-    const dim3 grid(static_cast<unsigned>(chunks));
+    const int64_t chunks = (tokens + RT_TOKENS - 1) / RT_TOKENS, pitch = (experts + 3) & ~3;
+    Route a{logits, tokens, ldl, experts, k, renormalize, chosen, weights, offsets, rows, slots, nullptr, nullptr};
+    if (chunks > 1) {
+        char* ws = static_cast<char*>(adadim_workspace(ctx, WS_ROUTE, size_t(chunks) * size_t(experts * 8 + pitch)));
+        if (!ws) return ADADIM_EHIP;
+        a.masks = reinterpret_cast<uint64_t*>(ws);
+        a.counts = reinterpret_cast<uint8_t*>(ws + chunks * experts * 8);
+    }
     {
         ProfScope prof(ctx, "route_choose");
-        const size_t lds = size_t(experts) * 8;
-#define RT_GO(T, V) hipLaunchKernelGGL((route_choose<T, V>), grid, dim3(64 * RT_WAVES), lds, ctx->stream, a)
+        const dim3 grid(static_cast<unsigned>(chunks)), block(RT_THREADS);
+        const size_t lds = size_t(experts) * 12;
+#define RT_GO(T, W, V) hipLaunchKernelGGL((route_choose<T, W, V>), grid, block, lds, ctx->stream, a)
 #define RT_V(T)                                    \
     do {                                           \
-        if (experts <= 64) RT_GO(T, 1);            \
-        else if (experts <= 128) RT_GO(T, 2);      \
-        else if (experts <= 256) RT_GO(T, 4);      \
-        else RT_GO(T, 16);                         \
+        if (experts <= 8) RT_GO(T, 8, 1);          \
+        else if (experts <= 16) RT_GO(T, 16, 1);   \
+        else if (experts <= 32) RT_GO(T, 16, 2);   \
+        else if (experts <= 64) RT_GO(T, 16, 4);   \
+        else if (experts <= 128) RT_GO(T, 16, 8);  \
+        else if (experts <= 256) RT_GO(T, 16, 16); \
+        else if (experts <= 512) RT_GO(T, 16, 32); \
+        else RT_GO(T, 16, 64);                     \
     } while (0)
         if (type == ADADIM_TYPE_F16) RT_V(_Float16);
         else if (type == ADADIM_TYPE_BF16) RT_V(__bf16);
@@ -232,16 +320,12 @@ int launch_expert_route(adadim_ctx* ctx, const void* logits, int type, int64_t t
 #undef RT_GO
     }
     ADADIM_LAUNCH_CHECK(ctx, "route_choose");
-    {
-        ProfScope prof(ctx, "route_bases");
-        hipLaunchKernelGGL(route_bases, dim3(1), dim3(1024), 0, ctx->stream, a, chunks);
-    }
-    ADADIM_LAUNCH_CHECK(ctx, "route_bases");
-    {
+    if (chunks > 1) {
+        const int64_t per = (chunks + RT_GROUPS - 1) / RT_GROUPS;
         ProfScope prof(ctx, "route_place");
-        hipLaunchKernelGGL(route_place, grid, dim3(256), 0, ctx->stream, a);
+        hipLaunchKernelGGL(route_place, dim3(static_cast<unsigned>((chunks + per - 1) / per)), dim3(RT_THREADS), size_t(pitch) * 8, ctx->stream, a, chunks, per);
+        ADADIM_LAUNCH_CHECK(ctx, "route_place");
     }
-    ADADIM_LAUNCH_CHECK(ctx, "route_place");
     return ADADIM_OK;
 }
 
