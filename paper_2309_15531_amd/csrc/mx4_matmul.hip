@@ -75,7 +75,8 @@ __device__ __forceinline__ void piece16(const uint4v (&w)[NT], const uint32_t (&
     }
 }
 
-template <int XT, int NT, int MT>
+// SHIFT: rows of 16-bit X that begin in the middle of a word.  They are read from the word's begin on, one word more, and moved into place.
+template <int XT, int NT, int MT, bool SHIFT>
 __global__ __launch_bounds__(64 * RW_WAVES) void mx4_rows(Product a, float* __restrict__ part, unsigned* __restrict__ ticket) {
     constexpr int TILES = NT * MT, ROUND = TILES < 4 ? TILES : 4;                // tiles added up at a time
     __shared__ float4v s_part[RW_WAVES][ROUND][64];
@@ -98,14 +99,19 @@ __global__ __launch_bounds__(64 * RW_WAVES) void mx4_rows(Product a, float* __re
 
     for (int64_t r0 = gr.lo; r0 < gr.hi; r0 += 16 * MT) {
         const int64_t first = a.gather ? 0 : r0;              // the row of X that offsets are taken from
-        const char* const x_base = static_cast<const char*>(a.X) + first * x_pitch;
+        const char* x_base = static_cast<const char*>(a.X) + first * x_pitch;
+        uint32_t skew = 0;
+        if constexpr (SHIFT) {
+            skew = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(x_base) & 2u);
+            x_base -= skew;
+        }
         const auto x_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(x_base), 0, NO_ROW, 0x00027000);
         uint32_t xo[MT], xso[MT];
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             const int64_t src = source_row(a, r0 + 16 * m + (lane & 15), gr.hi);
             xso[m] = src < 0 ? 0u : static_cast<uint32_t>(src - first);
-            xo[m] = src < 0 ? NO_ROW : xso[m] * x_pitch + (XT == XMX4 ? 16 : 64) * g;
+            xo[m] = src < 0 ? NO_ROW : xso[m] * x_pitch + (XT == XMX4 ? 16 : 64) * g + skew;
         }
         float4v acc[NT][MT];
 #pragma unroll
@@ -127,6 +133,18 @@ __global__ __launch_bounds__(64 * RW_WAVES) void mx4_rows(Product a, float* __re
                 if constexpr (XT == XMX4) {
                     x[m].v[0] = __builtin_bit_cast(uint4v, __builtin_amdgcn_raw_buffer_load_b128(x_rsrc, xo[m], p * PIECE_BYTES, 0));
                     x[m].scale = (a.x_scales + int64_t(p) * a.x_rows + first)[xso[m]];
+                } else if constexpr (SHIFT) {
+                    const uint32_t at = xo[m] & ~3u, shift = 8 * (xo[m] & 2u);
+                    uint32_t d[17];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint4v q = __builtin_bit_cast(uint4v, __builtin_amdgcn_raw_buffer_load_b128(x_rsrc, at + 16 * i, p * (2 * PIECE), 0));
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) d[4 * i + j] = q[j];
+                    }
+                    d[16] = __builtin_amdgcn_raw_buffer_load_b32(x_rsrc, shift ? at + 64 : NO_ROW, p * (2 * PIECE), 0);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[m].v[i / 4][i % 4] = __builtin_amdgcn_alignbit(d[i + 1], d[i], shift);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
@@ -339,6 +357,7 @@ int launch_ring(adadim_ctx* ctx, const Product& a, int splits) {
 // ---- few rows
 template <int XT, int NT, int MT>
 int launch_rows(adadim_ctx* ctx, const Product& a, int splits) {
+    const bool shift = XT != XMX4 && ((reinterpret_cast<uintptr_t>(a.X) & 3u) != 0 || (a.ldx % 2 != 0 && a.tokens > 1));
     const int64_t tiles = (a.out + 16 * NT - 1) / (16 * NT);
     Shares sh{};
     if (splits > 1) {
@@ -346,8 +365,15 @@ int launch_rows(adadim_ctx* ctx, const Product& a, int splits) {
         if (rc != ADADIM_OK) return rc;
     }
     ProfScope prof(ctx, "mx4_rows");
-    hipLaunchKernelGGL((mx4_rows<XT, NT, MT>), dim3(static_cast<unsigned>(tiles), static_cast<unsigned>(a.experts), static_cast<unsigned>(splits)),
-                       dim3(64 * RW_WAVES), 0, ctx->stream, a, sh.part, sh.ticket);
+    const dim3 grid(static_cast<unsigned>(tiles), static_cast<unsigned>(a.experts), static_cast<unsigned>(splits)), block(64 * RW_WAVES);
+    if constexpr (XT != XMX4) {
+        if (shift) {
+            hipLaunchKernelGGL((mx4_rows<XT, NT, MT, true>), grid, block, 0, ctx->stream, a, sh.part, sh.ticket);
+            ADADIM_LAUNCH_CHECK(ctx, "mx4_rows");
+            return ADADIM_OK;
+        }
+    }
+    hipLaunchKernelGGL((mx4_rows<XT, NT, MT, false>), grid, block, 0, ctx->stream, a, sh.part, sh.ticket);
     ADADIM_LAUNCH_CHECK(ctx, "mx4_rows");
     return ADADIM_OK;
 }
@@ -404,12 +430,12 @@ hipError_t raise_lds() {
 template <int XT>
 int launch_product(adadim_ctx* ctx, Product a) {
     constexpr bool MX = XT == XMX4;
-    const Plan p = mx4_plan(a.n_rows, a.out, a.in, a.offsets ? a.experts : 0, MX);
-    const bool odd = !MX && (!aligned16(a.X) || (a.tokens > 1 && a.ldx % 8 != 0) || (p.form != Form::rows && a.in % 8 != 0));
+    const bool odd = !MX && (!aligned16(a.X) || (a.tokens > 1 && a.ldx % 8 != 0) || a.in % 8 != 0);
+    const Plan p = mx4_plan(a.n_rows, a.out, a.in, a.offsets ? a.experts : 0, MX, odd);
     // offsets are taken from token 0 where rows[] is given, from a tile's first row otherwise
     const int64_t pitch = MX ? pieces(a.in) * PIECE_BYTES : 2 * a.ldx;
     const bool far = (a.gather ? a.tokens : min(a.n_rows, int64_t(256))) * pitch >= int64_t(NO_ROW);
-    if (odd || (far && (a.gather || !MX))) {
+    if ((odd && p.form != Form::rows) || (far && (a.gather || !MX))) {
         const int64_t to_pitch = MX ? pitch : pieces(a.in) * (2 * PIECE), blocks = (a.n_rows * to_pitch / 16 + 255) / 256;
         if (blocks > INT32_MAX) return adadim_fail(ctx, ADADIM_EINVAL, "mx4 product: X too large to be copied");
         const size_t codes = size_t(a.n_rows) * size_t(to_pitch);

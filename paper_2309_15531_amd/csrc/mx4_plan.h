@@ -32,25 +32,31 @@ struct TileForm {
     float fill;                    // workgroups that run at once, over 256
     float steps;                   // how far a last round that is not full counts as one: 1 wholly, 0 by its share
     float share;                   // us: of adding up
+    float read;                    // MB/us: operands through the L2
 };
 constexpr TileForm TILE_FORMS_16[] = {
-    {Form::ring32, 32, 256, 1, true, 1.50f, 3.49f, 0.694f, 0.94f, 0.86f, 1.3f}, {Form::ring64, 64, 64, 1, true, 2.18f, 2.81f, 0.585f, 1.34f, 0.19f, 1.5f},
-    {Form::ring64w, 64, 128, 1, true, 3.42f, 2.24f, 0.765f, 1.20f, 0.19f, 2.4f}, {Form::mid, 128, 128, 1, true, 2.60f, 3.25f, 0.931f, 0.80f, 0.0f, 2.4f},
-    {Form::wide, 128, 256, 1, true, 5.20f, 1.41f, 1.348f, 0.88f, 1.0f, 4.0f},    {Form::big, 256, 256, 1, false, 2.76f, 6.00f, 2.596f, 0.81f, 0.68f, 0.0f}};
+    {Form::ring32, 32, 256, 1, true, 1.50f, 3.68f, 0.706f, 1.00f, 0.92f, 1.5f, 7.3f},
+    {Form::ring64, 64, 64, 1, true, 2.44f, 2.57f, 0.571f, 1.31f, 0.17f, 1.8f, 21.1f},
+    {Form::ring64w, 64, 128, 1, true, 2.88f, 2.82f, 0.743f, 1.20f, 0.19f, 2.9f, 27.0f},
+    {Form::mid, 128, 128, 1, true, 1.50f, 4.51f, 0.944f, 1.00f, 0.97f, 2.6f, 7.9f},
+    {Form::wide, 128, 256, 1, true, 1.50f, 5.49f, 1.347f, 1.00f, 1.00f, 4.0f, 6.0f},
+    {Form::big, 256, 256, 1, false, 8.00f, 0.91f, 2.575f, 1.80f, 0.97f, 0.0f, 4.3f}};
 constexpr TileForm TILE_FORMS_MX[] = {
-    {Form::ring32, 32, 128, 1, true, 3.14f, 1.33f, 0.233f, 0.94f, 0.52f, 1.4f},  {Form::ring64, 64, 64, 1, true, 2.91f, 1.42f, 0.217f, 1.44f, 0.56f, 1.3f},
-    {Form::ring64w, 64, 128, 1, true, 3.63f, 1.07f, 0.253f, 0.95f, 0.54f, 2.3f}, {Form::mid, 128, 128, 2, false, 1.64f, 3.74f, 0.642f, 1.0f, 0.14f, 0.0f},
-    {Form::big, 256, 256, 2, false, 1.50f, 5.04f, 1.515f, 0.82f, 1.0f, 0.0f}};
+    {Form::ring32, 32, 128, 1, true, 2.46f, 2.15f, 0.239f, 1.15f, 0.40f, 1.5f, 12.2f},
+    {Form::ring64, 64, 64, 1, true, 3.28f, 1.15f, 0.198f, 1.25f, 0.42f, 1.5f, 27.9f},
+    {Form::ring64w, 64, 128, 1, true, 3.52f, 1.41f, 0.238f, 1.00f, 0.47f, 2.6f, 25.1f},
+    {Form::mid, 128, 128, 2, false, 2.67f, 2.92f, 0.587f, 1.00f, 0.46f, 0.0f, 23.9f},
+    {Form::big, 256, 256, 2, false, 1.50f, 6.04f, 1.561f, 1.00f, 1.00f, 0.0f, 8.3f}};
 struct RowForm {
     int out_tiles;
     float start, pass, piece, rows;   // us: of the launch, of a pass over the contraction, of a wave's piece, and of 16 rows of X with it
     float fill, share;
 };
-constexpr RowForm ROW_FORMS_16[] = {{1, 3.87f, 0.66f, 0.03f, 1.12f, 0.84f, 0.7f}, {2, 3.98f, 0.89f, 0.11f, 1.53f, 0.8f, 0.6f}, {4, 4.14f, 0.88f, 0.49f, 2.31f, 0.8f, 0.6f}};
-constexpr RowForm ROW_FORMS_MX[] = {{1, 3.08f, 0.36f, 0.14f, 0.32f, 0.8f, 1.1f}, {2, 3.32f, 0.23f, 0.27f, 0.63f, 0.81f, 0.8f}, {4, 3.07f, 0.57f, 0.68f, 1.35f, 0.8f, 0.8f}};
+constexpr RowForm ROW_FORMS_16[] = {{1, 3.93f, 0.54f, 0.13f, 0.95f, 0.90f, 0.8f}, {2, 3.65f, 0.87f, 0.41f, 1.13f, 0.96f, 0.8f}, {4, 3.55f, 1.12f, 0.72f, 1.60f, 0.86f, 1.0f}};
+constexpr RowForm ROW_FORMS_MX[] = {{1, 3.01f, 0.35f, 0.21f, 0.25f, 0.95f, 1.2f}, {2, 3.02f, 0.43f, 0.38f, 0.42f, 1.05f, 1.0f}, {4, 2.56f, 0.91f, 0.80f, 0.75f, 0.87f, 1.3f}};
 
-// experts 0: one weight.
-inline Plan mx4_plan(int64_t n_rows, int64_t out, int64_t in, int experts, bool mx) {
+// experts 0: one weight.  copy: X has to be copied for all forms but rows (a launch more).
+inline Plan mx4_plan(int64_t n_rows, int64_t out, int64_t in, int experts, bool mx, bool copy) {
     const double np = double((in + 127) / 128);
     const double active = experts ? double(std::min<int64_t>(experts, n_rows)) : 1.0;         // groups that may have rows
     const double weight = active * double(out) * np * 68.0;                                   // bytes of W
@@ -69,7 +75,7 @@ inline Plan mx4_plan(int64_t n_rows, int64_t out, int64_t in, int experts, bool 
     const int64_t per_group = experts ? (n_rows + experts - 1) / experts : n_rows;
     if (per_group <= 96) {
         const int rt = per_group <= 16 ? 1 : per_group <= 32 ? 2 : 4;
-        const double loops = std::max(1.0, (experts ? 2.0 : 1.0) * avg / (16 * rt));          // of the longest group
+        const double loops = std::max(1.0, (experts ? 3.0 : 1.0) * avg / (16 * rt));          // of the longest group
         for (const RowForm& f : mx ? ROW_FORMS_MX : ROW_FORMS_16) {
             const double tiles = up(double(out) / (16 * f.out_tiles));
             for (int s = 1; s <= 8; s *= 2) {
@@ -88,8 +94,8 @@ inline Plan mx4_plan(int64_t n_rows, int64_t out, int64_t in, int experts, bool 
             if (s > 1 && (s > np || tiles * s > MOST_SHARED)) break;
             const double full = std::max(1.0, tiles * s / (256 * f.fill)), rounds = f.steps * up(full - 1e-9) + (1.0 - f.steps) * full;
             double t = f.start + rounds * (f.tile + up(np / (s * f.pieces)) * f.stage);
-            t = std::max(t, f.start + weight / 5.0e6) + (s > 1 ? f.share + s * part / 6.0e6 : 0.0);
-            take(t, Plan{f.form, s, 0, 0});
+            t = std::max({t, f.start + weight / 5.0e6, f.start + tiles * np * (f.bm * (mx ? 64.0 : 256.0) + f.bn * 64.0) / (f.read * 1e6)}) + (s > 1 ? f.share + s * part / 6.0e6 : 0.0);
+            take(t + (copy ? 4.0 + double(n_rows) * double(in) * 4.0 / 5.0e6 : 0.0), Plan{f.form, s, 0, 0});
         }
     };
     if (mx)
