@@ -66,7 +66,7 @@ static int product_checked(adadim_ctx* ctx, const char* me, int x_type, const mx
         return adadim_fail(ctx, ADADIM_EINVAL, "%s: x_type must be F16, BF16 or MX4, got %d", me, x_type);
     if (!is_float_type(a.y_type)) return adadim_fail(ctx, ADADIM_EINVAL, "%s: y_type must be F16, BF16 or F32, got %d", me, a.y_type);
     if (a.tokens < 0 || a.n_rows < 0 || a.out <= 0 || a.in <= 0 || a.tokens > MOST_ROWS || a.n_rows > MOST_ROWS || a.out > MOST_COLS ||
-        a.in > MOST_COLS || (x_type != ADADIM_TYPE_MX4 && a.ldx < a.in) || a.ldy < a.out)
+        a.in > MOST_COLS || (x_type != ADADIM_TYPE_MX4 && (a.ldx < a.in || a.ldx > INT32_MAX)) || a.ldy < a.out || a.ldy > INT32_MAX)
         return adadim_fail(ctx, ADADIM_EINVAL,
                            "%s: need rows >= 0, out, in > 0 in range, ldx >= in, ldy >= out (tokens=%lld rows=%lld out=%lld in=%lld "
                            "ldx=%lld ldy=%lld)",

@@ -26,6 +26,34 @@ struct Product {
     int64_t ldy;
 };
 
+// The same as a kernel's argument: up to 112 bytes a launch costs the host 2.7 us, beyond 3.4.  (The host has checked that the sizes fit.)
+struct ProductArgs {
+    const void* X;
+    const uint32_t* x_scales;
+    const int32_t *rows, *offsets;
+    const uint8_t* codes;
+    const uint32_t* scales;
+    void* Y;
+    int32_t tokens, ldx, x_rows, n_rows, out, in, ldy;
+    uint16_t experts;
+    uint8_t y_type, gather;
+
+    explicit ProductArgs(const Product& a)
+        : X(a.X), x_scales(a.x_scales), rows(a.rows), offsets(a.offsets), codes(a.codes), scales(a.scales), Y(a.Y),
+          tokens(static_cast<int32_t>(a.tokens)), ldx(static_cast<int32_t>(a.ldx)), x_rows(static_cast<int32_t>(a.x_rows)),
+          n_rows(static_cast<int32_t>(a.n_rows)), out(static_cast<int32_t>(a.out)), in(static_cast<int32_t>(a.in)),
+          ldy(static_cast<int32_t>(a.ldy)), experts(static_cast<uint16_t>(a.experts)), y_type(static_cast<uint8_t>(a.y_type)), gather(a.gather) {}
+    __device__ __forceinline__ Product open() const {
+        return Product{X, x_scales, tokens, ldx, x_rows, rows, gather != 0, offsets, n_rows, experts, codes, scales, out, in, Y, y_type, ldy};
+    }
+};
+static_assert(sizeof(ProductArgs) <= 104, "a pointer more");
+
+// Where the workgroups that share a contraction leave their sums: a counter for each output tile, zero between launches, then the sums.
+constexpr int SHARE_TICKETS = 1024;
+__device__ __forceinline__ unsigned* tickets_of(void* shared) { return static_cast<unsigned*>(shared); }
+__device__ __forceinline__ float* parts_of(void* shared) { return static_cast<float*>(shared) + SHARE_TICKETS; }
+
 struct Group {
     int64_t lo, hi;
     const uint8_t* codes;

@@ -77,7 +77,10 @@ __device__ __forceinline__ void piece16(const uint4v (&w)[NT], const uint32_t (&
 
 // SHIFT: rows of 16-bit X that begin in the middle of a word.  They are read from the word's begin on, one word more, and moved into place.
 template <int XT, int NT, int MT, bool SHIFT>
-__global__ __launch_bounds__(64 * RW_WAVES) void mx4_rows(Product a, float* __restrict__ part, unsigned* __restrict__ ticket) {
+__global__ __launch_bounds__(64 * RW_WAVES) void mx4_rows(ProductArgs args, void* shared) {
+    const Product a = args.open();
+    float* const part = parts_of(shared);
+    unsigned* const ticket = tickets_of(shared);
     constexpr int TILES = NT * MT, ROUND = TILES < 4 ? TILES : 4;                // tiles added up at a time
     __shared__ float4v s_part[RW_WAVES][ROUND][64];
     __shared__ unsigned s_ticket;
@@ -263,7 +266,8 @@ __global__ __launch_bounds__(64 * RW_WAVES) void mx4_rows(Product a, float* __re
 // X in the order of Y's rows, for kernels that read 16 bytes at a time and reach rows by 32-bit offsets: copied where it does not lie so.
 // 16-bit rows become whole pieces, filled up with zeros.  PITCH: bytes of a row.
 template <bool MX>
-__global__ __launch_bounds__(256) void mx4_copy_rows(Product a, int64_t pitch, uint8_t* __restrict__ to, uint32_t* __restrict__ to_scales) {
+__global__ __launch_bounds__(256) void mx4_copy_rows(ProductArgs args, int64_t pitch, uint8_t* __restrict__ to, uint32_t* __restrict__ to_scales) {
+    const Product a = args.open();
     const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 16, row = i / pitch, c = i % pitch;
     if (row >= a.n_rows) return;
     const int64_t src = source_row(a, row, a.n_rows);
@@ -285,21 +289,15 @@ __global__ __launch_bounds__(256) void mx4_copy_rows(Product a, int64_t pitch, u
 
 namespace {
 
-// Where the workgroups that share a contraction leave their sums: counters of the output tiles, zero between launches, then `bytes` of sums.
-constexpr int TICKETS = MOST_SHARED;
+static_assert(MOST_SHARED <= SHARE_TICKETS, "a counter for each tile that is shared");
 __global__ void mx4_zero_tickets(unsigned* ticket) { ticket[threadIdx.x] = 0u; }
 
-struct Shares {
-    float* part;
-    unsigned* ticket;
-};
-int shares(adadim_ctx* ctx, size_t bytes, Shares& s) {
-    char* slot = static_cast<char*>(adadim_workspace(ctx, WS_MX4_PART, TICKETS * 4 + bytes));
-    if (!slot) return ADADIM_EHIP;
-    s.ticket = reinterpret_cast<unsigned*>(slot);
-    s.part = reinterpret_cast<float*>(slot + TICKETS * 4);
+// The counters and room for `bytes` of sums.
+int shares(adadim_ctx* ctx, size_t bytes, void*& shared) {
+    shared = adadim_workspace(ctx, WS_MX4_PART, SHARE_TICKETS * 4 + bytes);
+    if (!shared) return ADADIM_EHIP;
     if (ctx->mx4_ready_bytes != ctx->ws_bytes[WS_MX4_PART]) {
-        hipLaunchKernelGGL(mx4_zero_tickets, dim3(1), dim3(TICKETS), 0, ctx->stream, s.ticket);
+        hipLaunchKernelGGL(mx4_zero_tickets, dim3(1), dim3(SHARE_TICKETS), 0, ctx->stream, static_cast<unsigned*>(shared));
         ADADIM_LAUNCH_CHECK(ctx, "mx4_zero_tickets");
         // a clearing that is only recorded has not happened yet for the calls outside the graph
         if (!ctx->capturing) ctx->mx4_ready_bytes = ctx->ws_bytes[WS_MX4_PART];
@@ -328,7 +326,7 @@ int launch_tiles(adadim_ctx* ctx, const Product& a) {
     if (tiles > INT32_MAX - 8) return adadim_fail(ctx, ADADIM_EINVAL, "mx4 product: more tiles than a launch has workgroups");
     ProfScope prof(ctx, "mx4_tiles");
     hipLaunchKernelGGL((mx4_tiles<XT, BM, BN, WT, WO>), dim3(static_cast<unsigned>((tiles + 7) / 8 * 8)), dim3(64 * WT * WO),
-                       (tile_lds<XT, BM, BN, WT, WO>()), ctx->stream, a);
+                       (tile_lds<XT, BM, BN, WT, WO>()), ctx->stream, ProductArgs(a));
     ADADIM_LAUNCH_CHECK(ctx, "mx4_tiles");
     return ADADIM_OK;
 }
@@ -342,14 +340,14 @@ template <int XT, int BM, int BN, int WT, int WO, int NS>
 int launch_ring(adadim_ctx* ctx, const Product& a, int splits) {
     const int64_t tiles = most_row_tiles(a, BM) * ((a.out + BN - 1) / BN), grid = (tiles + 7) / 8 * 8;
     if (tiles > INT32_MAX - 8) return adadim_fail(ctx, ADADIM_EINVAL, "mx4 product: more tiles than a launch has workgroups");
-    Shares sh{};
+    void* shared = nullptr;
     if (splits > 1) {
-        const int rc = shares(ctx, size_t(splits) * size_t(grid) * BM * BN * 4, sh);
+        const int rc = shares(ctx, size_t(splits) * size_t(grid) * BM * BN * 4, shared);
         if (rc != ADADIM_OK) return rc;
     }
     ProfScope prof(ctx, "mx4_ring");
     hipLaunchKernelGGL((mx4_ring<XT, BM, BN, WT, WO, NS>), dim3(static_cast<unsigned>(grid), static_cast<unsigned>(splits)), dim3(64 * WT * WO),
-                       (Ring<XT, BM, BN, WT, WO, NS>::LDS), ctx->stream, a, sh.part, sh.ticket);
+                       (Ring<XT, BM, BN, WT, WO, NS>::LDS), ctx->stream, ProductArgs(a), shared);
     ADADIM_LAUNCH_CHECK(ctx, "mx4_ring");
     return ADADIM_OK;
 }
@@ -359,21 +357,21 @@ template <int XT, int NT, int MT>
 int launch_rows(adadim_ctx* ctx, const Product& a, int splits) {
     const bool shift = XT != XMX4 && ((reinterpret_cast<uintptr_t>(a.X) & 3u) != 0 || (a.ldx % 2 != 0 && a.tokens > 1));
     const int64_t tiles = (a.out + 16 * NT - 1) / (16 * NT);
-    Shares sh{};
+    void* shared = nullptr;
     if (splits > 1) {
-        const int rc = shares(ctx, size_t(splits) * size_t(a.n_rows) * size_t(a.out) * 4, sh);
+        const int rc = shares(ctx, size_t(splits) * size_t(a.n_rows) * size_t(a.out) * 4, shared);
         if (rc != ADADIM_OK) return rc;
     }
     ProfScope prof(ctx, "mx4_rows");
     const dim3 grid(static_cast<unsigned>(tiles), static_cast<unsigned>(a.experts), static_cast<unsigned>(splits)), block(64 * RW_WAVES);
     if constexpr (XT != XMX4) {
         if (shift) {
-            hipLaunchKernelGGL((mx4_rows<XT, NT, MT, true>), grid, block, 0, ctx->stream, a, sh.part, sh.ticket);
+            hipLaunchKernelGGL((mx4_rows<XT, NT, MT, true>), grid, block, 0, ctx->stream, ProductArgs(a), shared);
             ADADIM_LAUNCH_CHECK(ctx, "mx4_rows");
             return ADADIM_OK;
         }
     }
-    hipLaunchKernelGGL((mx4_rows<XT, NT, MT, false>), grid, block, 0, ctx->stream, a, sh.part, sh.ticket);
+    hipLaunchKernelGGL((mx4_rows<XT, NT, MT, false>), grid, block, 0, ctx->stream, ProductArgs(a), shared);
     ADADIM_LAUNCH_CHECK(ctx, "mx4_rows");
     return ADADIM_OK;
 }
@@ -443,7 +441,7 @@ int launch_product(adadim_ctx* ctx, Product a) {
         if (!to) return ADADIM_EHIP;
         uint32_t* to_scales = reinterpret_cast<uint32_t*>(to + codes);
         ProfScope prof(ctx, "mx4_copy_rows");
-        hipLaunchKernelGGL((mx4_copy_rows<MX>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, ctx->stream, a, to_pitch, to, to_scales);
+        hipLaunchKernelGGL((mx4_copy_rows<MX>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, ctx->stream, ProductArgs(a), to_pitch, to, to_scales);
         ADADIM_LAUNCH_CHECK(ctx, "mx4_copy_rows");
         a.X = to;
         a.gather = false;

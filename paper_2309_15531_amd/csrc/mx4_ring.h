@@ -36,7 +36,8 @@ struct Ring {
 constexpr int wait_vm_lgkm0(int n) { return (n & 15) | ((n >> 4) << 14) | 0x0070; }
 
 template <int XT, int BM, int BN, int WT, int WO, int NS>
-__global__ __launch_bounds__(64 * WT * WO) void mx4_ring(Product a, float* __restrict__ part, unsigned* __restrict__ ticket) {
+__global__ __launch_bounds__(64 * WT * WO) void mx4_ring(ProductArgs args, void* shared) {
+    const Product a = args.open();
     using namespace tiles;
     using R = Ring<XT, BM, BN, WT, WO, NS>;
     constexpr bool MX = R::MX;
@@ -299,6 +300,8 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_ring(Product a, float* __res
     }
 
     if (gridDim.y > 1) {
+        float* const part = parts_of(shared);
+        unsigned* const ticket = tickets_of(shared);
         // this share's sums, a lane's four consecutive outputs at a time, in the order in which the lanes hold them: whoever adds them up
         // holds the same places
         float* mine = part + (int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * (BM * BN) + tid;

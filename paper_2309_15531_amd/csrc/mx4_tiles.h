@@ -161,7 +161,8 @@ __device__ __forceinline__ void store_tile(const Product& a, const float16v (&ac
 // need them; instruction j takes values 64 h + 8 j .. + 7.
 // Two stages of LDS: one is computed while the other arrives.
 template <int XT, int BM, int BN, int WT, int WO>
-__global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(Product a) {
+__global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(ProductArgs args) {
+    const Product a = args.open();
     using namespace tiles;
     constexpr bool MX = XT == XMX4;
     constexpr int NW = WT * WO, TT = BM / WT / 32, TO = BN / WO / 32;
