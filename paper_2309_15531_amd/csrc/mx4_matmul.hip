@@ -397,7 +397,7 @@ int launch_form(adadim_ctx* ctx, const Product& a, Plan p) {
             if constexpr (MX) return launch_ring<XT, 32, 128, 1, 4, 6>(ctx, a, p.shares);
             else return launch_ring<XT, 32, 256, 1, 8, 4>(ctx, a, p.shares);
         case Form::ring64: return launch_ring<XT, 64, 64, 2, 2, MX ? 4 : 3>(ctx, a, p.shares);
-        case Form::ring64w: return launch_ring<XT, 64, 128, 2, 2, MX ? 4 : 3>(ctx, a, p.shares);
+        case Form::ring64w: return launch_ring<XT, 64, 128, MX ? 2 : 1, MX ? 2 : 4, MX ? 4 : 3>(ctx, a, p.shares);
         case Form::mid:
             if constexpr (MX) return launch_tiles<XT, 128, 128, 2, 2>(ctx, a);
             else return launch_ring<XT, 128, 128, 2, 4, 3>(ctx, a, p.shares);
@@ -413,7 +413,7 @@ hipError_t raise_lds() {
     constexpr bool MX = XT == XMX4;
     hipError_t e = raise_tiles<XT, 256, 256, 2, 4>();
     if (e == hipSuccess) e = raise_ring<XT, 64, 64, 2, 2, MX ? 4 : 3>();
-    if (e == hipSuccess) e = raise_ring<XT, 64, 128, 2, 2, MX ? 4 : 3>();
+    if (e == hipSuccess) e = raise_ring<XT, 64, 128, MX ? 2 : 1, MX ? 2 : 4, MX ? 4 : 3>();
     if constexpr (MX) {
         if (e == hipSuccess) e = raise_tiles<XT, 128, 128, 2, 2>();
         if (e == hipSuccess) e = raise_ring<XT, 32, 128, 1, 4, 6>();

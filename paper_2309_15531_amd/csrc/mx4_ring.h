@@ -158,47 +158,8 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_ring(ProductArgs args, void*
         xa[j] = lds0 + (wt * TT * 32 + fr) * ROWB + (static_cast<uint32_t>(chunk_of(CH, fr, j + STEPS * fh)) << 4);
         if constexpr (MX) wa[j] = w_at + ((static_cast<uint32_t>(j + 2 * fh) ^ w_swz) << 4);
     }
-    struct Frags {
-        uint4v w[TO], x[TT];
-    };
-    bool wide = false;
-    float sc[MX ? 1 : TO][2];
-    auto scales_of = [&](const Side& d, bool real) {
-        if constexpr (!MX) {
-#pragma unroll
-            for (int o = 0; o < TO; ++o)
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const uint32_t byte = (d.ws[o] >> (8 * b)) & 255u;
-                    sc[o][b] = scale_operand(byte);
-                    wide |= real && beyond_f16(byte);
-                }
-        }
-    };
-    auto read_one = [&](Frags& f, const Side& d, uint32_t slot, int step, int k) {
-        if (k >= TO) f.x[k - TO] = lds_read16(xa[step] + slot + (k - TO) * 32 * ROWB);
-        else if constexpr (MX) f.w[k] = lds_read16(wa[step] + slot + k * 32 * 64);
-        else if constexpr (XT == XF16) f.w[k] = __builtin_bit_cast(uint4v, values8_f16(d.w[k][step >> 2][step & 3], sc[k][step >> 2]));
-        else f.w[k] = __builtin_bit_cast(uint4v, values8_bf16(d.w[k][step >> 2][step & 3], sc[k][step >> 2]));
-    };
-    auto mma = [&](auto step_tag, const Frags& f, const Side& d, int m) {
-        constexpr int J = decltype(step_tag)::value;
-        const int o = m / TT, i = m % TT;
-        if constexpr (MX) acc[o][i] = mma_mx4<J & 3>(f.w[o], d.ws[o], f.x[i], d.xs[i], acc[o][i]);
-        else if constexpr (XT == XF16)
-            acc[o][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8v, f.w[o]), __builtin_bit_cast(half8v, f.x[i]), acc[o][i], 0, 0, 0);
-        else
-            acc[o][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8v, f.w[o]), __builtin_bit_cast(bf8v, f.x[i]), acc[o][i], 0, 0, 0);
-    };
-    constexpr int M = TO * TT, RD = TO + TT, BOTH = M > RD ? M : RD;
-    auto step = [&](auto step_tag, const Frags& f, const Side& d, Frags& nf, uint32_t slot, int nstep) {
-#pragma unroll
-        for (int m = 0; m < BOTH; ++m) {
-            if (m < RD) read_one(nf, d, slot, nstep, m);
-            if (m < M) mma(step_tag, f, d, m);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    };
+    bool wide = false;                                        // fp16 X: a weight has gone by that no fp16 number holds
+    constexpr int M = TO * TT;
 
     // ---- stage 0: the chunks it lacks are zeros (16-bit X; mx4 rows are whole pieces)
     {
@@ -219,42 +180,125 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_ring(ProductArgs args, void*
     __builtin_amdgcn_s_waitcnt(wait_vm_lgkm0((NS - 1) * R::LOADS < 63 ? (NS - 1) * R::LOADS : 63));
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    Frags f0, f1;
-    Side now = side_of(0);
-    scales_of(now, true);
-#pragma unroll
-    for (int k = 0; k < RD; ++k) read_one(f0, now, 0, 0, k);
     uint32_t slot = 0;
-    for (int q = 0; q < n_st; ++q) {
-        auto pair = [&](auto tag) {                           // steps J (even) and J + 1, unless that is the stage's last
-            constexpr int J = decltype(tag)::value;
-            step(std::integral_constant<int, J>{}, f0, now, f1, slot, J + 1);
-            if constexpr (J + 2 < STEPS) step(std::integral_constant<int, J + 1>{}, f1, now, f0, slot, J + 2);
-        };
-        pair(std::integral_constant<int, 0>{});
-        if constexpr (STEPS == 8) {
-            pair(std::integral_constant<int, 2>{});
-            pair(std::integral_constant<int, 4>{});
-            pair(std::integral_constant<int, 6>{});
-        }
-        // the next stage has arrived, this one's reads have ended in every wave: its slot is free
+    auto after = [](uint32_t s) { return s == (NS - 1) * SLOT ? 0u : s + SLOT; };
+    // The stage behind the one at hand has arrived, and every wave has read what it needs of the one at hand: its slot is free.
+    auto meet = [&]() {
         __builtin_amdgcn_s_waitcnt(wait_vm_lgkm0((NS - 2) * R::LOADS));
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
-        const uint32_t next_slot = slot == (NS - 1) * SLOT ? 0u : slot + SLOT;
         next_fetch();
-        const Side next = side_of(next_slot);
-        scales_of(next, q + 1 < n_st);
+    };
+    if constexpr (MX) {
+        // Little to compute a stage: all of the next stage is read while one is computed from registers.
+        struct Stage {
+            Side side;
+            uint4v w[2][TO], x[2][TT];
+        };
+        constexpr int READS = 2 * (TO + TT);
+        auto read_one = [&](Stage& st, uint32_t at, int k) {
+            const int j = k / (TO + TT), n = k % (TO + TT);
+            if (n < TO) st.w[j][n] = lds_read16(wa[j] + at + n * 32 * 64);
+            else st.x[j][n - TO] = lds_read16(xa[j] + at + (n - TO) * 32 * ROWB);
+        };
+        Stage s0, s1;
+        s0.side = side_of(0);
 #pragma unroll
-        for (int m = 0; m < BOTH; ++m) {
-            if (m < RD) read_one(f0, next, next_slot, 0, m);
+        for (int k = 0; k < READS; ++k) read_one(s0, 0, k);
+        auto body = [&](const Stage& st, Stage& next) {
+            meet();
+            const uint32_t next_slot = after(slot);
+            next.side = side_of(next_slot);
 #pragma unroll
-            for (int i = m * R::LOADS / BOTH; i < (m + 1) * R::LOADS / BOTH; ++i) fetch_one(slot, i);
-            if (m < M) mma(std::integral_constant<int, STEPS - 1>{}, f1, now, m);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int m = 0; m < 2 * M; ++m) {
+#pragma unroll
+                for (int k = m * READS / (2 * M); k < (m + 1) * READS / (2 * M); ++k) read_one(next, next_slot, k);
+#pragma unroll
+                for (int i = m * R::LOADS / (2 * M); i < (m + 1) * R::LOADS / (2 * M); ++i) fetch_one(slot, i);
+                const int j = m / M, o = m % M / TT, i = m % TT;
+                if (j == 0) acc[o][i] = mma_mx4<0>(st.w[0][o], st.side.ws[o], st.x[0][i], st.side.xs[i], acc[o][i]);
+                else acc[o][i] = mma_mx4<1>(st.w[1][o], st.side.ws[o], st.x[1][i], st.side.xs[i], acc[o][i]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            slot = next_slot;
+        };
+        for (int q = 0; q < n_st; q += 2) {                   // (the surplus stage of an odd number multiplies zeros)
+            body(s0, s1);
+            body(s1, s0);
         }
-        now = next;
-        slot = next_slot;
+    } else {
+        // X is read two steps ahead, W's codes become numbers one step ahead.  The waves meet two steps before a stage's end, so that
+        // what is read of the next stage has two steps' instructions to arrive.
+        uint4v xf[4][TT], wf[2][TO];
+        float sc[TO][2];
+        auto scales_of = [&](const Side& d, bool real) {
+#pragma unroll
+            for (int o = 0; o < TO; ++o)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const uint32_t byte = (d.ws[o] >> (8 * b)) & 255u;
+                    sc[o][b] = scale_operand(byte);
+                    wide |= real && beyond_f16(byte);
+                }
+        };
+        auto read_x = [&](int b, uint32_t at, int step, int i) { xf[b][i] = lds_read16(xa[step] + at + i * 32 * ROWB); };
+        auto number_w = [&](int b, const Side& d, int step, int o) {
+            if constexpr (XT == XF16) wf[b][o] = __builtin_bit_cast(uint4v, values8_f16(d.w[o][step >> 2][step & 3], sc[o][step >> 2]));
+            else wf[b][o] = __builtin_bit_cast(uint4v, values8_bf16(d.w[o][step >> 2][step & 3], sc[o][step >> 2]));
+        };
+        auto mma = [&](int step, int m) {
+            const int o = m / TT, i = m % TT;
+            if constexpr (XT == XF16)
+                acc[o][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8v, wf[step & 1][o]), __builtin_bit_cast(half8v, xf[step & 3][i]), acc[o][i], 0, 0, 0);
+            else
+                acc[o][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8v, wf[step & 1][o]), __builtin_bit_cast(bf8v, xf[step & 3][i]), acc[o][i], 0, 0, 0);
+        };
+        constexpr int SLOTS = M > TT ? (M > TO ? M : TO) : (TT > TO ? TT : TO);
+        Side now = side_of(0);
+        scales_of(now, true);
+#pragma unroll
+        for (int i = 0; i < TT; ++i) {
+            read_x(0, 0, 0, i);
+            read_x(1, 0, 1, i);
+        }
+#pragma unroll
+        for (int o = 0; o < TO; ++o) number_w(0, now, 0, o);
+        for (int q = 0; q < n_st; ++q) {
+#pragma unroll
+            for (int j = 0; j < 6; ++j)
+#pragma unroll
+                for (int m = 0; m < SLOTS; ++m) {
+                    if (m < TT) read_x((j + 2) & 3, slot, j + 2, m);
+                    if (m < M) mma(j, m);
+                    if (m < TO) number_w((j + 1) & 1, now, j + 1, m);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            meet();
+            const uint32_t next_slot = after(slot);
+            const Side next = side_of(next_slot);
+#pragma unroll
+            for (int m = 0; m < SLOTS; ++m) {
+                if (m < TT) read_x(0, next_slot, 0, m);
+#pragma unroll
+                for (int i = m * R::LOADS / (2 * SLOTS); i < (m + 1) * R::LOADS / (2 * SLOTS); ++i) fetch_one(slot, i);
+                if (m < M) mma(6, m);
+                if (m < TO) number_w(1, now, 7, m);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int m = 0; m < SLOTS; ++m) {
+                if (m < TT) read_x(1, next_slot, 1, m);
+#pragma unroll
+                for (int i = (SLOTS + m) * R::LOADS / (2 * SLOTS); i < (SLOTS + m + 1) * R::LOADS / (2 * SLOTS); ++i) fetch_one(slot, i);
+                if (m < M) mma(7, m);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            scales_of(next, q + 1 < n_st);
+#pragma unroll
+            for (int o = 0; o < TO; ++o) number_w(0, next, 0, o);
+            now = next;
+            slot = next_slot;
+        }
     }
     __builtin_amdgcn_s_waitcnt(WAIT_ALL);                     // no transfer may outlive the workgroup, or meet what follows in LDS
     __syncthreads();
