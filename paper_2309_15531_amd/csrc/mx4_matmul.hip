@@ -305,14 +305,9 @@ int shares(adadim_ctx* ctx, size_t bytes, void*& shared) {
     return ADADIM_OK;
 }
 
-template <int XT, int BM, int BN, int WT, int WO>
-constexpr int tile_lds() {
-    return 2 * (BM * (XT == XMX4 ? 128 : 256) + (XT == XMX4 ? BN * 128 : 0));
-}
-
-template <int XT, int BM, int BN, int WT, int WO>
+template <int BM, int BN, int WT, int WO>
 hipError_t raise_tiles() {
-    return hipFuncSetAttribute(reinterpret_cast<const void*>(&mx4_tiles<XT, BM, BN, WT, WO>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_lds<XT, BM, BN, WT, WO>());
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(&mx4_tiles<BM, BN, WT, WO>), hipFuncAttributeMaxDynamicSharedMemorySize, Tiles<BM, BN, WT, WO>::LDS);
 }
 
 // Row tiles that the launch has to have workgroups for: each group may end in a tile of its own.
@@ -320,13 +315,13 @@ inline int64_t most_row_tiles(const Product& a, int bm) {
     return a.offsets ? a.n_rows / bm + min(int64_t(a.experts), a.n_rows) : (a.n_rows + bm - 1) / bm;
 }
 
-template <int XT, int BM, int BN, int WT, int WO>
+template <int BM, int BN, int WT, int WO>
 int launch_tiles(adadim_ctx* ctx, const Product& a) {
     const int64_t tiles = most_row_tiles(a, BM) * ((a.out + BN - 1) / BN);
     if (tiles > INT32_MAX - 8) return adadim_fail(ctx, ADADIM_EINVAL, "mx4 product: more tiles than a launch has workgroups");
     ProfScope prof(ctx, "mx4_tiles");
-    hipLaunchKernelGGL((mx4_tiles<XT, BM, BN, WT, WO>), dim3(static_cast<unsigned>((tiles + 7) / 8 * 8)), dim3(64 * WT * WO),
-                       (tile_lds<XT, BM, BN, WT, WO>()), ctx->stream, ProductArgs(a));
+    hipLaunchKernelGGL((mx4_tiles<BM, BN, WT, WO>), dim3(static_cast<unsigned>((tiles + 7) / 8 * 8)), dim3(64 * WT * WO),
+                       (Tiles<BM, BN, WT, WO>::LDS), ctx->stream, ProductArgs(a));
     ADADIM_LAUNCH_CHECK(ctx, "mx4_tiles");
     return ADADIM_OK;
 }
@@ -377,48 +372,43 @@ int launch_rows(adadim_ctx* ctx, const Product& a, int splits) {
 }
 
 
+template <int XT, int NT>
+int launch_rows_of(adadim_ctx* ctx, const Product& a, const Plan& p) {
+    if constexpr (NT < 4) {
+        if (p.row_tiles == 4) return launch_rows<XT, NT, 4>(ctx, a, p.shares);
+        if (p.row_tiles == 2) return launch_rows<XT, NT, 2>(ctx, a, p.shares);
+    }
+    return launch_rows<XT, NT, 1>(ctx, a, p.shares);
+}
 
 // The kernel of a form.
 template <int XT>
-int launch_form(adadim_ctx* ctx, const Product& a, Plan p) {
+int launch_form(adadim_ctx* ctx, const Product& a, const Plan& p) {
     constexpr bool MX = XT == XMX4;
     switch (p.form) {
-        case Form::rows: {
-#define MX4_ROWS(NT)                                                     \
-    return p.row_tiles == 1   ? launch_rows<XT, NT, 1>(ctx, a, p.shares) \
-           : p.row_tiles == 2 ? launch_rows<XT, NT, 2>(ctx, a, p.shares) \
-                              : launch_rows<XT, NT, 4>(ctx, a, p.shares)
-            if (p.out_tiles == 1) MX4_ROWS(1);
-            if (p.out_tiles == 2) MX4_ROWS(2);
-            MX4_ROWS(4);
-#undef MX4_ROWS
-        }
-        case Form::ring32:
-            if constexpr (MX) return launch_ring<XT, 32, 128, 1, 4, 6>(ctx, a, p.shares);
-            else return launch_ring<XT, 32, 256, 1, 8, 4>(ctx, a, p.shares);
+        case Form::rows: return p.out_tiles == 1 ? launch_rows_of<XT, 1>(ctx, a, p) : p.out_tiles == 2 ? launch_rows_of<XT, 2>(ctx, a, p) : launch_rows_of<XT, 4>(ctx, a, p);
+        case Form::ring32: return launch_ring<XT, 32, MX ? 128 : 256, 1, MX ? 4 : 8, MX ? 6 : 4>(ctx, a, p.shares);
         case Form::ring64: return launch_ring<XT, 64, 64, 2, 2, MX ? 4 : 3>(ctx, a, p.shares);
         case Form::ring64w: return launch_ring<XT, 64, 128, MX ? 2 : 1, MX ? 2 : 4, MX ? 4 : 3>(ctx, a, p.shares);
         case Form::mid:
-            if constexpr (MX) return launch_tiles<XT, 128, 128, 2, 2>(ctx, a);
+            if constexpr (MX) return launch_tiles<128, 128, 2, 2>(ctx, a);
             else return launch_ring<XT, 128, 128, 2, 4, 3>(ctx, a, p.shares);
-        case Form::wide:
-            if constexpr (!MX) return launch_ring<XT, 128, 256, 2, 4, 3>(ctx, a, p.shares);
-            [[fallthrough]];
-        default: return launch_tiles<XT, 256, 256, 2, 4>(ctx, a);
+        default:                                              // big
+            if constexpr (MX) return launch_tiles<256, 256, 2, 4>(ctx, a);
+            else return launch_ring<XT, 128, 256, 2, 4, 3>(ctx, a, p.shares);
     }
 }
 
 template <int XT>
 hipError_t raise_lds() {
     constexpr bool MX = XT == XMX4;
-    hipError_t e = raise_tiles<XT, 256, 256, 2, 4>();
+    hipError_t e = raise_ring<XT, 32, MX ? 128 : 256, 1, MX ? 4 : 8, MX ? 6 : 4>();
     if (e == hipSuccess) e = raise_ring<XT, 64, 64, 2, 2, MX ? 4 : 3>();
     if (e == hipSuccess) e = raise_ring<XT, 64, 128, MX ? 2 : 1, MX ? 2 : 4, MX ? 4 : 3>();
     if constexpr (MX) {
-        if (e == hipSuccess) e = raise_tiles<XT, 128, 128, 2, 2>();
-        if (e == hipSuccess) e = raise_ring<XT, 32, 128, 1, 4, 6>();
+        if (e == hipSuccess) e = raise_tiles<128, 128, 2, 2>();
+        if (e == hipSuccess) e = raise_tiles<256, 256, 2, 4>();
     } else {
-        if (e == hipSuccess) e = raise_ring<XT, 32, 256, 1, 8, 4>();
         if (e == hipSuccess) e = raise_ring<XT, 128, 128, 2, 4, 3>();
         if (e == hipSuccess) e = raise_ring<XT, 128, 256, 2, 4, 3>();
     }

@@ -3,8 +3,8 @@
 // The kernels differ in how much of Y a workgroup owns.  Large tiles read each operand less often; small ones are more, start sooner and
 // leave fewer compute units idle, and where even they are few the contraction is shared.  Which is ahead depends on all of rows, outputs,
 // contraction, X's type and the groups, so each form's time is estimated and the shortest taken.  The estimates are fits to the
-// kernels' times over shapes drawn at random (1 to 8192 rows, 64 to 28672 outputs, 64 to 11008 deep; 4 to 64 experts): mean error 8 to 20 % a form, and
-// the form chosen is 2 % (one weight) and 5 % (experts) slower in the geometric mean than the best of them all.
+// kernels' times over shapes drawn at random (1 to 8192 rows, 64 to 28672 outputs, 64 to 11008 deep; 4 to 64 experts): mean error 9 to 20 % a form, and
+// the form chosen is 2 % (one weight) and 6 % (experts) slower in the geometric mean than the best of them all.
 #pragma once
 
 #include <algorithm>
@@ -13,8 +13,8 @@
 namespace mx4 {
 
 // rows: 16 out_tiles outputs, a wave a share of the pieces.  The others by their tile (rows x outputs): ring32 32 x 256 (mx4 X: 32 x 128), ring64
-// 64 x 64, ring64w 64 x 128, mid 128 x 128, wide 128 x 256 (16-bit X only), big 256 x 256.
-enum class Form { rows, ring32, ring64, ring64w, mid, wide, big };
+// 64 x 64, ring64w 64 x 128, mid 128 x 128, big 128 x 256 (mx4 X: 256 x 256).
+enum class Form { rows, ring32, ring64, ring64w, mid, big };
 
 struct Plan {
     Form form;
@@ -35,25 +35,24 @@ struct TileForm {
     float read;                    // MB/us: operands through the L2
 };
 constexpr TileForm TILE_FORMS_16[] = {
-    {Form::ring32, 32, 256, 1, true, 1.50f, 3.68f, 0.706f, 1.00f, 0.92f, 1.5f, 7.3f},
-    {Form::ring64, 64, 64, 1, true, 2.44f, 2.57f, 0.571f, 1.31f, 0.17f, 1.8f, 21.1f},
-    {Form::ring64w, 64, 128, 1, true, 2.88f, 2.82f, 0.743f, 1.20f, 0.19f, 2.9f, 27.0f},
-    {Form::mid, 128, 128, 1, true, 1.50f, 4.51f, 0.944f, 1.00f, 0.97f, 2.6f, 7.9f},
-    {Form::wide, 128, 256, 1, true, 1.50f, 5.49f, 1.347f, 1.00f, 1.00f, 4.0f, 6.0f},
-    {Form::big, 256, 256, 1, false, 8.00f, 0.91f, 2.575f, 1.80f, 0.97f, 0.0f, 4.3f}};
+    {Form::ring32, 32, 256, 1, true, 1.50f, 3.52f, 0.610f, 1.00f, 0.98f, 1.6f, 8.0f},
+    {Form::ring64, 64, 64, 1, true, 2.35f, 2.36f, 0.450f, 1.21f, 0.24f, 1.9f, 12.6f},
+    {Form::ring64w, 64, 128, 1, true, 3.37f, 2.16f, 0.548f, 1.01f, 0.41f, 3.0f, 24.4f},
+    {Form::mid, 128, 128, 1, true, 1.50f, 4.35f, 0.860f, 1.00f, 1.00f, 2.7f, 8.4f},
+    {Form::big, 128, 256, 1, true, 6.72f, 0.20f, 1.217f, 1.01f, 1.00f, 4.0f, 5.8f}};
 constexpr TileForm TILE_FORMS_MX[] = {
-    {Form::ring32, 32, 128, 1, true, 2.46f, 2.15f, 0.239f, 1.15f, 0.40f, 1.5f, 12.2f},
-    {Form::ring64, 64, 64, 1, true, 3.28f, 1.15f, 0.198f, 1.25f, 0.42f, 1.5f, 27.9f},
-    {Form::ring64w, 64, 128, 1, true, 3.52f, 1.41f, 0.238f, 1.00f, 0.47f, 2.6f, 25.1f},
-    {Form::mid, 128, 128, 2, false, 2.67f, 2.92f, 0.587f, 1.00f, 0.46f, 0.0f, 23.9f},
-    {Form::big, 256, 256, 2, false, 1.50f, 6.04f, 1.561f, 1.00f, 1.00f, 0.0f, 8.3f}};
+    {Form::ring32, 32, 128, 1, true, 2.45f, 2.25f, 0.212f, 1.12f, 0.43f, 1.4f, 21.2f},
+    {Form::ring64, 64, 64, 1, true, 3.12f, 1.26f, 0.189f, 1.25f, 0.48f, 1.6f, 15.9f},
+    {Form::ring64w, 64, 128, 1, true, 3.38f, 1.63f, 0.243f, 1.05f, 0.48f, 2.7f, 19.7f},
+    {Form::mid, 128, 128, 2, false, 2.52f, 2.97f, 0.594f, 1.00f, 0.48f, 0.0f, 13.0f},
+    {Form::big, 256, 256, 2, false, 1.50f, 5.69f, 1.598f, 1.00f, 1.00f, 0.0f, 8.2f}};
 struct RowForm {
     int out_tiles;
     float start, pass, piece, rows;   // us: of the launch, of a pass over the contraction, of a wave's piece, and of 16 rows of X with it
     float fill, share;
 };
-constexpr RowForm ROW_FORMS_16[] = {{1, 3.93f, 0.54f, 0.13f, 0.95f, 0.90f, 0.8f}, {2, 3.65f, 0.87f, 0.41f, 1.13f, 0.96f, 0.8f}, {4, 3.55f, 1.12f, 0.72f, 1.60f, 0.86f, 1.0f}};
-constexpr RowForm ROW_FORMS_MX[] = {{1, 3.01f, 0.35f, 0.21f, 0.25f, 0.95f, 1.2f}, {2, 3.02f, 0.43f, 0.38f, 0.42f, 1.05f, 1.0f}, {4, 2.56f, 0.91f, 0.80f, 0.75f, 0.87f, 1.3f}};
+constexpr RowForm ROW_FORMS_16[] = {{1, 3.80f, 0.50f, 0.12f, 0.88f, 0.85f, 0.8f}, {2, 3.52f, 0.84f, 0.42f, 1.07f, 0.96f, 0.8f}, {4, 3.49f, 1.03f, 0.72f, 1.52f, 0.86f, 1.0f}};
+constexpr RowForm ROW_FORMS_MX[] = {{1, 2.76f, 0.34f, 0.20f, 0.24f, 0.92f, 1.2f}, {2, 2.74f, 0.39f, 0.42f, 0.39f, 1.03f, 1.0f}, {4, 2.38f, 0.85f, 0.79f, 0.71f, 0.87f, 1.3f}};
 
 // experts 0: one weight.  copy: X has to be copied for all forms but rows (a launch more).
 inline Plan mx4_plan(int64_t n_rows, int64_t out, int64_t in, int experts, bool mx, bool copy) {
@@ -77,6 +76,7 @@ inline Plan mx4_plan(int64_t n_rows, int64_t out, int64_t in, int experts, bool 
         const int rt = per_group <= 16 ? 1 : per_group <= 32 ? 2 : 4;
         const double loops = std::max(1.0, (experts ? 3.0 : 1.0) * avg / (16 * rt));          // of the longest group
         for (const RowForm& f : mx ? ROW_FORMS_MX : ROW_FORMS_16) {
+            if (f.out_tiles == 4 && rt > 1) break;             // (the estimates rarely had it ahead)
             const double tiles = up(double(out) / (16 * f.out_tiles));
             for (int s = 1; s <= 8; s *= 2) {
                 if (s > 1 && (experts || n_rows > 64 || s > np || tiles > MOST_SHARED)) break;

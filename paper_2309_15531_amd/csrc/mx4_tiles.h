@@ -1,4 +1,4 @@
-// Product tiles of microscaled 4-bit weights on the matrix cores, for many rows.  Included by mx4_matmul.hip.
+// What the product kernels with tiles of both operands share, and the one for many rows of mx4 X.  Included by mx4_matmul.hip.
 #pragma once
 
 #include "mx4_matmul.h"
@@ -31,10 +31,9 @@ __device__ __forceinline__ void lds_write(uint32_t addr, const V& v) {
     *reinterpret_cast<lds_ptr>(uintptr_t(addr)) = v;
 }
 
-// Rows of 128 bytes (8 chunks of 16) or 256 bytes (16 chunks) in LDS; chunk c of row r lies at slot c ^ swizzle(r), so that
-// a fragment read (32 consecutive rows, one chunk each) touches every bank evenly.  The same for rows 32 apart.
-template <int CHUNKS>
-__device__ __forceinline__ int swizzle(int row) { return CHUNKS == 8 ? (row & 7) ^ ((row >> 3) & 3) : row & 15; }
+// Rows of 128 bytes (8 chunks of 16) in LDS; chunk c of row r lies at slot c ^ swizzle(r), so that a fragment read
+// (32 consecutive rows, one chunk each) touches every bank evenly.  The same for rows 32 apart.
+__device__ __forceinline__ int swizzle(int row) { return (row & 7) ^ ((row >> 3) & 3); }
 
 template <int J>
 __device__ __forceinline__ float16v mma_mx4(uint4v w, uint32_t ws, uint4v x, uint32_t xs, float16v acc) {
@@ -151,34 +150,38 @@ __device__ __forceinline__ void store_tile(const Product& a, const float16v (&ac
 
 }  // namespace tiles
 
-// Y tile of BM rows x BN outputs by WT x WO waves (along the rows, along the outputs).
+// Y tile of BM rows x BN outputs by WT x WO waves (along the rows, along the outputs), X in mx4.
 //
-// mx4 X: a stage is 256 k, 128 bytes of every row of both operands, brought to LDS by DMA; the lane (row r, half h) of the
-// 32x32x64 instruction number j takes chunk j + 4 h, so that its scale is byte j of one word: half 0 works through the stage's first
-// piece while half 1 works through the second.
-// 16-bit X: a stage is 128 k, 256 bytes of every row of X; the weights' codes go straight to registers (32 bytes a lane and row tile: half
-// h takes blocks 2 h and 2 h + 1) and become 16-bit numbers there, two a conversion, next to the 32x32x16 instructions that
-// need them; instruction j takes values 64 h + 8 j .. + 7.
-// Two stages of LDS: one is computed while the other arrives.
-template <int XT, int BM, int BN, int WT, int WO>
+// A stage is 256 k, 128 bytes of every row of both operands, brought to LDS by DMA; the lane (row r, half h) of the 32x32x64 instruction
+// number j takes chunk j + 4 h, so that its scale is byte j of one word: half 0 works through the stage's first piece while half 1
+// works through the second.  Two stages of LDS: one is computed while the other arrives.
+template <int BM, int BN, int WT, int WO>
+struct Tiles {
+    static constexpr int NW = WT * WO, TT = BM / WT / 32, TO = BN / WO / 32;
+    static constexpr int CH = 8, ROWB = 16 * CH, ROWS_PER = 64 / CH, STEPS = CH / 2;      // chunks and bytes of a row, rows of a transfer, steps of a stage
+    static constexpr int X_BYTES = BM * ROWB, STAGE = X_BYTES + BN * ROWB, LDS = 2 * STAGE;
+    static constexpr int XL = BM / ROWS_PER / NW, WL = BN / ROWS_PER / NW;                // transfers of a wave and stage
+    static_assert(BM % (ROWS_PER * NW) == 0 && BN % (ROWS_PER * NW) == 0, "transfers");
+    static_assert(NW % 4 == 0, "the swizzle is the same for all transfers of a wave");
+    static_assert(NW * 32 * (TO * 32 * 4 + 16) <= LDS, "room for the outputs");
+};
+
+template <int BM, int BN, int WT, int WO>
 __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(ProductArgs args) {
     const Product a = args.open();
     using namespace tiles;
-    constexpr bool MX = XT == XMX4;
-    constexpr int NW = WT * WO, TT = BM / WT / 32, TO = BN / WO / 32;
-    constexpr int CH = MX ? 8 : 16, ROWB = 16 * CH, ROWS_PER = 64 / CH;           // chunks and bytes of a row, rows of a transfer
-    constexpr int X_BYTES = BM * ROWB, STAGE = X_BYTES + (MX ? BN * ROWB : 0);
-    constexpr int XL = BM / ROWS_PER / NW, WL = MX ? BN / ROWS_PER / NW : 0;       // transfers of a wave and stage
-    static_assert(BM % (ROWS_PER * NW) == 0 && (!MX || BN % (ROWS_PER * NW) == 0), "transfers");
+    using S = Tiles<BM, BN, WT, WO>;
+    constexpr int NW = S::NW, TT = S::TT, TO = S::TO, CH = S::CH, ROWB = S::ROWB, ROWS_PER = S::ROWS_PER, STEPS = S::STEPS;
+    constexpr int X_BYTES = S::X_BYTES, STAGE = S::STAGE, XL = S::XL, WL = S::WL;
     extern __shared__ __align__(16) char smem[];
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
     Tile t;
     if (!tile_of<BM, BN>(a, t)) return;
-    Group gr = group_of(a, t.expert);
+    const Group gr = group_of(a, t.expert);
     const int64_t r_first = gr.lo + t.row0, np = pieces(a.in);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wt = wave / WO, wo = wave % WO, fr = lane & 31, fh = lane >> 5;
-    const int n_st = static_cast<int>(MX ? (np + 1) / 2 : np);
+    const int n_st = static_cast<int>((np + 1) / 2);
 
     // a row of X to read in place of one that does not exist: its products are not stored, or stored as zeros
     auto x_row = [&](int i) {
@@ -187,10 +190,9 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(ProductArgs args) {
     };
     // Transfers.  Number i of a wave takes ROWS_PER rows; every lane has the same chunk in all of them.  They are given as 32-bit offsets
     // from a row that all share: the tile's first (W; X in Y's order) or that of token 0, which the host holds within 4 GB.
-    static_assert(NW % 4 == 0, "the swizzle is the same for all transfers of a wave");
-    const int t_row = ROWS_PER * wave + lane / CH, t_chunk = (lane % CH) ^ swizzle<CH>(t_row);
-    const int64_t x_pitch = MX ? np * PIECE_BYTES : 2 * a.ldx, x_first = a.gather ? 0 : r_first;
-    uint32_t xo[XL], wofs[MX ? WL : 1];
+    const int t_row = ROWS_PER * wave + lane / CH, t_chunk = (lane % CH) ^ swizzle(t_row);
+    const int64_t x_pitch = np * PIECE_BYTES, x_first = a.gather ? 0 : r_first;
+    uint32_t xo[XL], wofs[WL];
     const char* x_base = uniform(static_cast<const char*>(a.X) + x_first * x_pitch);
     const char* w_base = uniform(gr.codes + t.out0 * np * PIECE_BYTES);
 #pragma unroll
@@ -198,16 +200,14 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(ProductArgs args) {
         const int row = t_row + ROWS_PER * NW * i;
         xo[i] = static_cast<uint32_t>((a.gather ? x_row(row) : min(int64_t(row), gr.hi - 1 - r_first)) * x_pitch + 16 * t_chunk);
     }
-    if constexpr (MX) {
 #pragma unroll
-        for (int i = 0; i < WL; ++i)
-            wofs[i] = static_cast<uint32_t>(min(int64_t(t_row + ROWS_PER * NW * i), a.out - 1 - t.out0) * np * PIECE_BYTES + 16 * t_chunk);
-    }
+    for (int i = 0; i < WL; ++i)
+        wofs[i] = static_cast<uint32_t>(min(int64_t(t_row + ROWS_PER * NW * i), a.out - 1 - t.out0) * np * PIECE_BYTES + 16 * t_chunk);
     // The last stage along k, which may be shorter, is computed first: stage q > 0 in the order of computation is number q - 1 along k.
     // The chunks that stage 0 lacks, and all of the stages behind the last (nothing branches on them), read zeros.
     auto fetch_first = [&]() {
         const int64_t k = n_st - 1;
-        const int n = static_cast<int>(MX ? min(int64_t(8), 4 * (np - 2 * k)) : min(int64_t(16), (a.in - PIECE * k + 7) / 8));
+        const int n = static_cast<int>(min(int64_t(CH), 4 * (np - 2 * k)));
         const char* none = reinterpret_cast<const char*>(&zero_chunk);
         const uint32_t to = lds0 + wave * 1024;
 #pragma unroll
@@ -218,7 +218,7 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(ProductArgs args) {
     auto fetch_one = [&](const char* xb, const char* wb, uint32_t mask, int buf, int i) {
         const uint32_t to = lds0 + buf * STAGE + wave * 1024;
         if (i < XL) g2l16_s(xb, xo[i < XL ? i : 0] & mask, to + NW * i * 1024);
-        else if constexpr (MX) g2l16_s(wb, wofs[i < XL ? 0 : i - XL] & mask, to + X_BYTES + NW * (i - XL) * 1024);
+        else g2l16_s(wb, wofs[i < XL ? 0 : i - XL] & mask, to + X_BYTES + NW * (i - XL) * 1024);
     };
 
     int64_t w_row[TO];
@@ -233,95 +233,60 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(ProductArgs args) {
 
     // ---- what a wave needs of a stage besides LDS, fetched one stage ahead
     struct Side {
-        uint32_t ws[TO], xs[MX ? TT : 1];
-        uint4v w[MX ? 1 : TO][2];
+        uint32_t ws[TO], xs[TT];
     };
-    int64_t x_src[MX ? TT : 1];
-    if constexpr (MX) {
+    int64_t x_src[TT];
 #pragma unroll
-        for (int i = 0; i < TT; ++i) x_src[i] = x_row((wt * TT + i) * 32 + fr);
-    }
+    for (int i = 0; i < TT; ++i) x_src[i] = x_row((wt * TT + i) * 32 + fr);
     auto side = [&](int q) {
         const int s = q == 0 ? n_st - 1 : min(q, n_st) - 1;
+        const int64_t p = 2 * int64_t(s) + fh, at = min(p, np - 1);
         Side d;
-        if constexpr (MX) {
-            const int64_t p = 2 * int64_t(s) + fh, at = min(p, np - 1);
 #pragma unroll
-            for (int o = 0; o < TO; ++o) d.ws[o] = gr.scales[at * a.out + w_row[o]];
+        for (int o = 0; o < TO; ++o) d.ws[o] = gr.scales[at * a.out + w_row[o]];
 #pragma unroll
-            for (int i = 0; i < TT; ++i) d.xs[i] = a.x_scales[at * a.x_rows + x_src[i]];
-            if (q == 0 && p >= np) {                          // half a stage: what it lacks are zeros, of scale 1
+        for (int i = 0; i < TT; ++i) d.xs[i] = a.x_scales[at * a.x_rows + x_src[i]];
+        if (q == 0 && p >= np) {                              // half a stage: what it lacks are zeros, of scale 1
 #pragma unroll
-                for (int o = 0; o < TO; ++o) d.ws[o] = ONE_WORD;
+            for (int o = 0; o < TO; ++o) d.ws[o] = ONE_WORD;
 #pragma unroll
-                for (int i = 0; i < TT; ++i) d.xs[i] = ONE_WORD;
-            }
-        } else {
-#pragma unroll
-            for (int o = 0; o < TO; ++o) {
-                d.ws[o] = gr.scales[s * a.out + w_row[o]] >> (16 * fh);
-                const uint4v* p = reinterpret_cast<const uint4v*>(gr.codes + (w_row[o] * np + s) * PIECE_BYTES + 32 * fh);
-                d.w[o][0] = p[0];
-                d.w[o][1] = p[1];
-            }
+            for (int i = 0; i < TT; ++i) d.xs[i] = ONE_WORD;
         }
         return d;
     };
 
     // Fragment addresses: step j of half h reads chunk j + CH / 2 * h of its row.  They move between the two stages: those of step 0 a
     // step before the others, since a stage's first operands are read during the last step of the one before.
-    constexpr int STEPS = CH / 2;
-    uint32_t xa[STEPS], wa[MX ? STEPS : 1];
+    uint32_t xa[STEPS], wa[STEPS];
 #pragma unroll
     for (int j = 0; j < STEPS; ++j) {
-        const uint32_t slot = static_cast<uint32_t>((j + STEPS * fh) ^ swizzle<CH>(fr)) << 4;
+        const uint32_t slot = static_cast<uint32_t>((j + STEPS * fh) ^ swizzle(fr)) << 4;
         xa[j] = lds0 + (wt * TT * 32 + fr) * ROWB + slot;
-        if constexpr (MX) wa[j] = lds0 + X_BYTES + (wo * TO * 32 + fr) * ROWB + slot;
+        wa[j] = lds0 + X_BYTES + (wo * TO * 32 + fr) * ROWB + slot;
     }
 
-    // ---- the pipeline.  A stage is CH / 2 steps of TO x TT matrix instructions; a step's operands are read (and, for 16-bit X, its
-    // weights converted) during the step before.  Before the last step of a stage all its reads have ended: there the wave waits for
-    // the next stage's transfers, meets the others, reads the next stage's first operands and sends for the one after it, into
-    // the buffer that has become free.
+    // ---- the pipeline.  A stage is four steps of TO x TT matrix instructions; a step's operands are read during the step before.
+    // Before the last step of a stage all its reads have ended: there the wave waits for the next stage's transfers, meets the others,
+    // reads the next stage's first operands and sends for the one after it, into the buffer that has become free.
     struct Frags {
         uint4v w[TO], x[TT];
     };
-    bool wide = false;                                        // fp16 X: a weight has gone by that no fp16 number holds
-    float sc[MX ? 1 : TO][2];
-    auto scales_of = [&](const Side& d) {
-        if constexpr (!MX) {
-#pragma unroll
-            for (int o = 0; o < TO; ++o)
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const uint32_t byte = (d.ws[o] >> (8 * b)) & 255u;
-                    sc[o][b] = scale_operand(byte);
-                    wide |= beyond_f16(byte);
-                }
-        }
-    };
     // operand number k of a step: TO of W, then TT of X
-    auto read_one = [&](Frags& f, const Side& d, int step, int k) {
+    auto read_one = [&](Frags& f, int step, int k) {
         if (k >= TO) f.x[k - TO] = lds_read16(xa[step] + (k - TO) * 32 * ROWB);
-        else if constexpr (MX) f.w[k] = lds_read16(wa[step] + k * 32 * ROWB);
-        else if constexpr (XT == XF16) f.w[k] = __builtin_bit_cast(uint4v, values8_f16(d.w[k][step >> 2][step & 3], sc[k][step >> 2]));
-        else f.w[k] = __builtin_bit_cast(uint4v, values8_bf16(d.w[k][step >> 2][step & 3], sc[k][step >> 2]));
+        else f.w[k] = lds_read16(wa[step] + k * 32 * ROWB);
     };
     auto mma = [&](auto step_tag, const Frags& f, const Side& d, int m) {
         constexpr int J = decltype(step_tag)::value;
         const int o = m / TT, i = m % TT;
-        if constexpr (MX) acc[o][i] = mma_mx4<J & 3>(f.w[o], d.ws[o], f.x[i], d.xs[i], acc[o][i]);
-        else if constexpr (XT == XF16)
-            acc[o][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8v, f.w[o]), __builtin_bit_cast(half8v, f.x[i]), acc[o][i], 0, 0, 0);
-        else
-            acc[o][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8v, f.w[o]), __builtin_bit_cast(bf8v, f.x[i]), acc[o][i], 0, 0, 0);
+        acc[o][i] = mma_mx4<J>(f.w[o], d.ws[o], f.x[i], d.xs[i], acc[o][i]);
     };
     constexpr int M = TO * TT, R = TO + TT, F = XL + WL;
     // a step: its instructions with the next step's operands read between them, in this order
     auto step = [&](auto step_tag, const Frags& f, const Side& d, Frags& nf, int nstep) {
 #pragma unroll
         for (int m = 0; m < (M > R ? M : R); ++m) {
-            if (m < R) read_one(nf, d, nstep, m);
+            if (m < R) read_one(nf, nstep, m);
             if (m < M) mma(step_tag, f, d, m);
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -332,11 +297,10 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(ProductArgs args) {
     __builtin_amdgcn_s_waitcnt(WAIT_VM0);
     __syncthreads();
     Frags f0, f1;
-    scales_of(now);
 #pragma unroll
-    for (int k = 0; k < R; ++k) read_one(f0, now, 0, k);
+    for (int k = 0; k < R; ++k) read_one(f0, 0, k);
     xa[0] += STAGE;
-    if constexpr (MX) wa[0] += STAGE;
+    wa[0] += STAGE;
     const char *xb = x_base, *wb = w_base;
     uint32_t mask = ~0u;
     int to_fetch = 1;
@@ -356,25 +320,16 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(ProductArgs args) {
         const int buf = q & 1;
         Side next = side(q + 1);
         __builtin_amdgcn_sched_barrier(0);
-        auto pair = [&](auto tag) {                           // steps J (even) and J + 1, unless that is the stage's last
-            constexpr int J = decltype(tag)::value;
-            step(std::integral_constant<int, J>{}, f0, now, f1, J + 1);
-            if constexpr (J + 2 < STEPS) step(std::integral_constant<int, J + 1>{}, f1, now, f0, J + 2);
-        };
-        pair(std::integral_constant<int, 0>{});
-        pair(std::integral_constant<int, 2>{});
-        if constexpr (STEPS == 8) {
-            pair(std::integral_constant<int, 4>{});
-            pair(std::integral_constant<int, 6>{});
-        }
+        step(std::integral_constant<int, 0>{}, f0, now, f1, 1);
+        step(std::integral_constant<int, 1>{}, f1, now, f0, 2);
+        step(std::integral_constant<int, 2>{}, f0, now, f1, 3);
         __builtin_amdgcn_s_waitcnt(WAIT_ALL);
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         next_fetch();
-        scales_of(next);
 #pragma unroll
         for (int m = 0; m < (M > R ? M : R); ++m) {
-            if (m < R) read_one(f0, next, 0, m);
+            if (m < R) read_one(f0, 0, m);
 #pragma unroll
             for (int i = m * F / M; i < (m < M ? (m + 1) * F / M : 0); ++i) fetch_one(xb, wb, mask, buf, i);
             if (m < M) mma(std::integral_constant<int, STEPS - 1>{}, f1, now, m);
@@ -384,56 +339,12 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(ProductArgs args) {
 #pragma unroll
         for (int j = 0; j < STEPS; ++j) {
             xa[j] += j ? move : -move;
-            if constexpr (MX) wa[j] += j ? move : -move;
+            wa[j] += j ? move : -move;
         }
         now = next;
     }
     __builtin_amdgcn_s_waitcnt(WAIT_ALL);
     __syncthreads();
-    if constexpr (XT == XF16) {
-        if (__syncthreads_or(wide)) {
-            // The tile once more with both operands in bf16, X in two parts.  Rare: a stage at a time.
-#pragma unroll
-            for (int o = 0; o < TO; ++o)
-#pragma unroll
-                for (int i = 0; i < TT; ++i) acc[o][i] = float16v{};
-            x_base -= int64_t(to_fetch - 1) * ROWB;
-            uint32_t x0[STEPS];
-#pragma unroll
-            for (int j = 0; j < STEPS; ++j)
-                x0[j] = lds0 + (wt * TT * 32 + fr) * ROWB + (static_cast<uint32_t>((j + STEPS * fh) ^ swizzle<CH>(fr)) << 4);
-            for (int q = 0; q < n_st; ++q) {
-                if (q == 0) fetch_first();
-                else {
-#pragma unroll
-                    for (int i = 0; i < XL; ++i) fetch_one(x_base + int64_t(q - 1) * ROWB, nullptr, ~0u, 0, i);
-                }
-                const Side d = side(q);
-                __builtin_amdgcn_s_waitcnt(WAIT_VM0);
-                __syncthreads();
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    bf8v w[TO];
-#pragma unroll
-                    for (int o = 0; o < TO; ++o) w[o] = values8_bf16(d.w[o][j >> 2][j & 3], scale_operand((d.ws[o] >> (8 * (j >> 2))) & 255u));
-#pragma unroll
-                    for (int i = 0; i < TT; ++i) {
-                        bf8v hi, lo;
-                        split_f16(__builtin_bit_cast(half8v, lds_read16(x0[j] + i * 32 * ROWB)), hi, lo);
-#pragma unroll
-                        for (int o = 0; o < TO; ++o) {
-                            acc[o][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[o], hi, acc[o][i], 0, 0, 0);
-                            acc[o][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[o], lo, acc[o][i], 0, 0, 0);
-                        }
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-                }
-                __syncthreads();
-            }
-        }
-    }
-
-    static_assert(NW * 32 * (TO * 32 * 4 + 16) <= 2 * STAGE, "room for the outputs");
     store_tile<TO, TT, NW>(a, acc, lds0, wave, lane, r_first + wt * TT * 32, gr.hi, t.out0 + wo * TO * 32);
 }
 
