@@ -292,15 +292,6 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(ProductArgs args) {
         }
     };
 
-    Side now = side(0);
-    fetch_first();
-    __builtin_amdgcn_s_waitcnt(WAIT_VM0);
-    __syncthreads();
-    Frags f0, f1;
-#pragma unroll
-    for (int k = 0; k < R; ++k) read_one(f0, 0, k);
-    xa[0] += STAGE;
-    wa[0] += STAGE;
     const char *xb = x_base, *wb = w_base;
     uint32_t mask = ~0u;
     int to_fetch = 1;
@@ -313,6 +304,29 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(ProductArgs args) {
         x_base += ROWB;
         w_base += ROWB;
     };
+    fetch_first();
+    if (r_first + wt * TT * 32 >= gr.hi || t.out0 + wo * TO * 32 >= a.out) {
+        // A wave beyond the group's last row or the last output only brings its part of the operands: what shares its SIMD has the matrix cores
+        // to itself.
+        __builtin_amdgcn_s_waitcnt(WAIT_VM0);
+        __syncthreads();
+        for (int q = 0; q <= n_st; ++q) {
+            next_fetch();
+#pragma unroll
+            for (int i = 0; i < F; ++i) fetch_one(xb, wb, mask, (q + 1) & 1, i);
+            __builtin_amdgcn_s_waitcnt(WAIT_ALL);
+            __builtin_amdgcn_s_barrier();
+        }
+        return;
+    }
+    Side now = side(0);
+    __builtin_amdgcn_s_waitcnt(WAIT_VM0);
+    __syncthreads();
+    Frags f0, f1;
+#pragma unroll
+    for (int k = 0; k < R; ++k) read_one(f0, 0, k);
+    xa[0] += STAGE;
+    wa[0] += STAGE;
     next_fetch();
 #pragma unroll
     for (int i = 0; i < F; ++i) fetch_one(xb, wb, mask, 1, i);
