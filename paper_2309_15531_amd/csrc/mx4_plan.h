@@ -4,7 +4,7 @@
 // leave fewer compute units idle, and where even they are few the contraction is shared.  Which is ahead depends on all of rows, outputs,
 // contraction, X's type and the groups, so each form's time is estimated and the shortest taken.  The estimates are fits to the
 // kernels' times over shapes drawn at random (1 to 8192 rows, 64 to 28672 outputs, 64 to 11008 deep; 4 to 64 experts): mean error 9 to 20 % a form, and
-// the form chosen is 2 % (one weight) and 6 % (experts) slower in the geometric mean than the best of them all.
+// the form chosen is 2 % (one weight) and 5 % (experts) slower in the geometric mean than the best of them all.
 #pragma once
 
 #include <algorithm>
@@ -49,10 +49,16 @@ constexpr TileForm TILE_FORMS_MX[] = {
 struct RowForm {
     int out_tiles;
     float start, pass, piece, rows;   // us: of the launch, of a pass over the contraction, of a wave's piece, and of 16 rows of X with it
-    float fill, share;
+    float fill, share, more;          // (as above; us of adding up for 16 rows, and for each 16 more)
 };
-constexpr RowForm ROW_FORMS_16[] = {{1, 3.80f, 0.50f, 0.12f, 0.88f, 0.85f, 0.8f}, {2, 3.52f, 0.84f, 0.42f, 1.07f, 0.96f, 0.8f}, {4, 3.49f, 1.03f, 0.72f, 1.52f, 0.86f, 1.0f}};
-constexpr RowForm ROW_FORMS_MX[] = {{1, 2.76f, 0.34f, 0.20f, 0.24f, 0.92f, 1.2f}, {2, 2.74f, 0.39f, 0.42f, 0.39f, 1.03f, 1.0f}, {4, 2.38f, 0.85f, 0.79f, 0.71f, 0.87f, 1.3f}};
+constexpr RowForm ROW_FORMS_16[] = {
+    {1, 3.88f, 0.47f, 0.13f, 0.77f, 0.80f, 0.60f, 0.53f},
+    {2, 3.65f, 0.77f, 0.43f, 0.87f, 0.90f, 0.56f, 0.93f},
+    {4, 3.71f, 0.89f, 0.73f, 1.24f, 0.80f, 0.78f, 1.52f}};
+constexpr RowForm ROW_FORMS_MX[] = {
+    {1, 2.80f, 0.33f, 0.20f, 0.22f, 0.89f, 0.98f, 0.22f},
+    {2, 2.83f, 0.29f, 0.45f, 0.28f, 0.90f, 0.72f, 0.72f},
+    {4, 2.44f, 0.77f, 0.86f, 0.53f, 0.83f, 1.02f, 1.34f}};
 
 // experts 0: one weight.  copy: X has to be copied for all forms but rows (a launch more).
 inline Plan mx4_plan(int64_t n_rows, int64_t out, int64_t in, int experts, bool mx, bool copy) {
@@ -70,9 +76,10 @@ inline Plan mx4_plan(int64_t n_rows, int64_t out, int64_t in, int experts, bool 
             best = p;
         }
     };
-    // few rows: at most six passes of 64 over a group
+    // few rows, in passes over the contraction.  Beyond 32 a group the groups' lengths, which the host does not know, differ too much for
+    // the estimate: with tiles there the chosen form was 5 % slower than the best, with these 7 %.
     const int64_t per_group = experts ? (n_rows + experts - 1) / experts : n_rows;
-    if (per_group <= 96) {
+    if (per_group <= (experts ? 32 : 96)) {
         const int rt = per_group <= 16 ? 1 : per_group <= 32 ? 2 : 4;
         const double loops = std::max(1.0, (experts ? 3.0 : 1.0) * avg / (16 * rt));          // of the longest group
         for (const RowForm& f : mx ? ROW_FORMS_MX : ROW_FORMS_16) {
@@ -82,7 +89,7 @@ inline Plan mx4_plan(int64_t n_rows, int64_t out, int64_t in, int experts, bool 
                 if (s > 1 && (experts || n_rows > 64 || s > np || tiles > MOST_SHARED)) break;
                 const double rounds = std::max(1.0, active * tiles * s / (256 * f.fill)), rows = std::min(avg / loops, 16.0 * rt);
                 double t = f.start + rounds * loops * (f.pass + up(np / (8 * s)) * (f.piece + f.rows * rows / 16.0));
-                t = std::max(t, f.start + weight / 5.2e6) + (s > 1 ? f.share : 0.0);
+                t = std::max(t, f.start + weight / 5.2e6) + (s > 1 ? f.share + f.more * (rt - 1) : 0.0);
                 take(t, Plan{Form::rows, s, f.out_tiles, rt});
             }
         }
