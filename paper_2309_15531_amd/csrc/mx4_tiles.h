@@ -47,6 +47,7 @@ __device__ __forceinline__ float16v mma_mx4(uint4v w, uint32_t ws, uint4v x, uin
 }
 
 __device__ const uint4v zero_chunk = {0u, 0u, 0u, 0u};   // what the transfers of chunks that do not exist read
+__device__ const uint32_t one_word = ONE_WORD;            // ... and of their scales
 
 constexpr int WAIT_VM0 = 0x0F70, WAIT_ALL = 0x0070;       // s_waitcnt vmcnt(0); vmcnt(0) lgkmcnt(0)
 
@@ -159,8 +160,9 @@ template <int BM, int BN, int WT, int WO>
 struct Tiles {
     static constexpr int NW = WT * WO, TT = BM / WT / 32, TO = BN / WO / 32;
     static constexpr int CH = 8, ROWB = 16 * CH, ROWS_PER = 64 / CH, STEPS = CH / 2;      // chunks and bytes of a row, rows of a transfer, steps of a stage
-    static constexpr int X_BYTES = BM * ROWB, STAGE = X_BYTES + BN * ROWB, LDS = 2 * STAGE;
-    static constexpr int XL = BM / ROWS_PER / NW, WL = BN / ROWS_PER / NW;                // transfers of a wave and stage
+    static constexpr int X_BYTES = BM * ROWB, W_BYTES = BN * ROWB, S_BYTES = 2 * (BM + BN) * 4, STAGE = X_BYTES + W_BYTES + S_BYTES, LDS = 2 * STAGE;
+    static constexpr int XL = BM / ROWS_PER / NW, WL = BN / ROWS_PER / NW;                // transfers of a wave and stage, and two of scales
+    static_assert(BM % 64 == 0 && BM + BN == 64 * NW, "a wave brings the scales of 64 rows, a transfer for each of the stage's pieces");
     static_assert(BM % (ROWS_PER * NW) == 0 && BN % (ROWS_PER * NW) == 0, "transfers");
     static_assert(NW % 4 == 0, "the swizzle is the same for all transfers of a wave");
     static_assert(NW * 32 * (TO * 32 * 4 + 16) <= LDS, "room for the outputs");
@@ -172,7 +174,7 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(ProductArgs args) {
     using namespace tiles;
     using S = Tiles<BM, BN, WT, WO>;
     constexpr int NW = S::NW, TT = S::TT, TO = S::TO, CH = S::CH, ROWB = S::ROWB, ROWS_PER = S::ROWS_PER, STEPS = S::STEPS;
-    constexpr int X_BYTES = S::X_BYTES, STAGE = S::STAGE, XL = S::XL, WL = S::WL;
+    constexpr int X_BYTES = S::X_BYTES, W_BYTES = S::W_BYTES, STAGE = S::STAGE, XL = S::XL, WL = S::WL;
     extern __shared__ __align__(16) char smem[];
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
     Tile t;
@@ -203,6 +205,15 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(ProductArgs args) {
 #pragma unroll
     for (int i = 0; i < WL; ++i)
         wofs[i] = static_cast<uint32_t>(min(int64_t(t_row + ROWS_PER * NW * i), a.out - 1 - t.out0) * np * PIECE_BYTES + 16 * t_chunk);
+    const bool s_of_x = wave < BM / 64;
+    const int s_row = 64 * wave + lane - (s_of_x ? 0 : BM);
+    const uint32_t so = static_cast<uint32_t>(4 * (!s_of_x ? min(int64_t(s_row), a.out - 1 - t.out0)
+                                                  : a.gather ? x_row(s_row) : min(int64_t(s_row), gr.hi - 1 - r_first)));
+    const int64_t s_pitch = 4 * (s_of_x ? a.x_rows : a.out);
+    const char* s_base = uniform(s_of_x ? a.x_scales + x_first : gr.scales + t.out0);
+    auto g2l4_s = [](const char* sbase, uint32_t voff, uint32_t lds) {
+        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(voff), "s"(sbase) : "memory", "m0");
+    };
     // The last stage along k, which may be shorter, is computed first: stage q > 0 in the order of computation is number q - 1 along k.
     // The chunks that stage 0 lacks, and all of the stages behind the last (nothing branches on them), read zeros.
     auto fetch_first = [&]() {
@@ -214,16 +225,19 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(ProductArgs args) {
         for (int i = 0; i < XL; ++i) g2l16(t_chunk < n ? x_base + xo[i] + k * ROWB : none, to + NW * i * 1024);
 #pragma unroll
         for (int i = 0; i < WL; ++i) g2l16(t_chunk < n ? w_base + wofs[i] + k * ROWB : none, to + X_BYTES + NW * i * 1024);
+        const bool whole = 2 * k + 1 < np;                    // of the piece that stage 0 may lack: scales 1
+        const uint32_t s_to = lds0 + X_BYTES + W_BYTES + wave * 256;
+        g2l4_s(uniform(s_base + 2 * k * s_pitch), so, s_to);
+        g2l4_s(uniform(whole ? s_base + (2 * k + 1) * s_pitch : reinterpret_cast<const char*>(&one_word)), whole ? so : 0u, s_to + (BM + BN) * 4);
     };
-    auto fetch_one = [&](const char* xb, const char* wb, uint32_t mask, int buf, int i) {
+    const char *xb, *wb, *sb;
+    uint32_t mask = ~0u;
+    auto fetch_one = [&](int buf, int i) {
         const uint32_t to = lds0 + buf * STAGE + wave * 1024;
         if (i < XL) g2l16_s(xb, xo[i < XL ? i : 0] & mask, to + NW * i * 1024);
-        else g2l16_s(wb, wofs[i < XL ? 0 : i - XL] & mask, to + X_BYTES + NW * (i - XL) * 1024);
+        else if (i < XL + WL) g2l16_s(wb, wofs[i < XL || i >= XL + WL ? 0 : i - XL] & mask, to + X_BYTES + NW * (i - XL) * 1024);
+        else g2l4_s(i == XL + WL ? sb : uniform(sb + (mask ? s_pitch : 0)), so & mask, lds0 + buf * STAGE + X_BYTES + W_BYTES + wave * 256 + (i - XL - WL) * (BM + BN) * 4);
     };
-
-    int64_t w_row[TO];
-#pragma unroll
-    for (int o = 0; o < TO; ++o) w_row[o] = min(t.out0 + (wo * TO + o) * 32 + fr, a.out - 1);
 
     float16v acc[TO][TT];
 #pragma unroll
@@ -231,28 +245,18 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(ProductArgs args) {
 #pragma unroll
         for (int i = 0; i < TT; ++i) acc[o][i] = float16v{};
 
-    // ---- what a wave needs of a stage besides LDS, fetched one stage ahead
+    // ---- the scales of a wave's rows in a stage, a word for its half's piece
     struct Side {
         uint32_t ws[TO], xs[TT];
     };
-    int64_t x_src[TT];
-#pragma unroll
-    for (int i = 0; i < TT; ++i) x_src[i] = x_row((wt * TT + i) * 32 + fr);
-    auto side = [&](int q) {
-        const int s = q == 0 ? n_st - 1 : min(q, n_st) - 1;
-        const int64_t p = 2 * int64_t(s) + fh, at = min(p, np - 1);
-        Side d;
-#pragma unroll
-        for (int o = 0; o < TO; ++o) d.ws[o] = gr.scales[at * a.out + w_row[o]];
-#pragma unroll
-        for (int i = 0; i < TT; ++i) d.xs[i] = a.x_scales[at * a.x_rows + x_src[i]];
-        if (q == 0 && p >= np) {                              // half a stage: what it lacks are zeros, of scale 1
-#pragma unroll
-            for (int o = 0; o < TO; ++o) d.ws[o] = ONE_WORD;
-#pragma unroll
-            for (int i = 0; i < TT; ++i) d.xs[i] = ONE_WORD;
-        }
-        return d;
+    uint32_t s_at = lds0 + X_BYTES + W_BYTES + 4 * (fh * (BM + BN) + fr);
+    auto lds_read4 = [](uint32_t addr) {
+        typedef uint32_t __attribute__((address_space(3))) * lds_ptr;
+        return *reinterpret_cast<lds_ptr>(uintptr_t(addr));
+    };
+    auto read_scale = [&](Side& d, int k) {
+        if (k < TO) d.ws[k] = lds_read4(s_at + 4 * (BM + 32 * (wo * TO + k)));
+        else d.xs[k - TO] = lds_read4(s_at + 4 * 32 * (wt * TT + k - TO));
     };
 
     // Fragment addresses: step j of half h reads chunk j + CH / 2 * h of its row.  They move between the two stages: those of step 0 a
@@ -281,7 +285,7 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(ProductArgs args) {
         const int o = m / TT, i = m % TT;
         acc[o][i] = mma_mx4<J>(f.w[o], d.ws[o], f.x[i], d.xs[i], acc[o][i]);
     };
-    constexpr int M = TO * TT, R = TO + TT, F = XL + WL;
+    constexpr int M = TO * TT, R = TO + TT, F = XL + WL + 2;
     // a step: its instructions with the next step's operands read between them, in this order
     auto step = [&](auto step_tag, const Frags& f, const Side& d, Frags& nf, int nstep) {
 #pragma unroll
@@ -292,17 +296,18 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(ProductArgs args) {
         }
     };
 
-    const char *xb = x_base, *wb = w_base;
-    uint32_t mask = ~0u;
     int to_fetch = 1;
     auto next_fetch = [&]() {                                 // where the next stage's transfers come from
         const bool real = to_fetch < n_st;
-        xb = uniform(real ? x_base : reinterpret_cast<const char*>(&zero_chunk));
-        wb = uniform(real ? w_base : reinterpret_cast<const char*>(&zero_chunk));
+        const char* none = reinterpret_cast<const char*>(&zero_chunk);
+        xb = uniform(real ? x_base : none);
+        wb = uniform(real ? w_base : none);
+        sb = uniform(real ? s_base : none);
         mask = real ? ~0u : 0u;
         ++to_fetch;
         x_base += ROWB;
         w_base += ROWB;
+        s_base += 2 * s_pitch;
     };
     fetch_first();
     if (r_first + wt * TT * 32 >= gr.hi || t.out0 + wo * TO * 32 >= a.out) {
@@ -313,27 +318,28 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(ProductArgs args) {
         for (int q = 0; q <= n_st; ++q) {
             next_fetch();
 #pragma unroll
-            for (int i = 0; i < F; ++i) fetch_one(xb, wb, mask, (q + 1) & 1, i);
+            for (int i = 0; i < F; ++i) fetch_one((q + 1) & 1, i);
             __builtin_amdgcn_s_waitcnt(WAIT_ALL);
             __builtin_amdgcn_s_barrier();
         }
         return;
     }
-    Side now = side(0);
     __builtin_amdgcn_s_waitcnt(WAIT_VM0);
     __syncthreads();
+    Side now, next;
     Frags f0, f1;
+#pragma unroll
+    for (int k = 0; k < R; ++k) read_scale(now, k);
 #pragma unroll
     for (int k = 0; k < R; ++k) read_one(f0, 0, k);
     xa[0] += STAGE;
     wa[0] += STAGE;
+    s_at += STAGE;
     next_fetch();
 #pragma unroll
-    for (int i = 0; i < F; ++i) fetch_one(xb, wb, mask, 1, i);
+    for (int i = 0; i < F; ++i) fetch_one(1, i);
     for (int q = 0; q < n_st; ++q) {
         const int buf = q & 1;
-        Side next = side(q + 1);
-        __builtin_amdgcn_sched_barrier(0);
         step(std::integral_constant<int, 0>{}, f0, now, f1, 1);
         step(std::integral_constant<int, 1>{}, f1, now, f0, 2);
         step(std::integral_constant<int, 2>{}, f0, now, f1, 3);
@@ -343,13 +349,17 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(ProductArgs args) {
         next_fetch();
 #pragma unroll
         for (int m = 0; m < (M > R ? M : R); ++m) {
-            if (m < R) read_one(f0, 0, m);
+            if (m < R) {
+                read_one(f0, 0, m);
+                read_scale(next, m);
+            }
 #pragma unroll
-            for (int i = m * F / M; i < (m < M ? (m + 1) * F / M : 0); ++i) fetch_one(xb, wb, mask, buf, i);
+            for (int i = m * F / M; i < (m < M ? (m + 1) * F / M : 0); ++i) fetch_one(buf, i);
             if (m < M) mma(std::integral_constant<int, STEPS - 1>{}, f1, now, m);
             __builtin_amdgcn_sched_barrier(0);
         }
         const uint32_t move = buf ? -STAGE : STAGE;
+        s_at -= move;
 #pragma unroll
         for (int j = 0; j < STEPS; ++j) {
             xa[j] += j ? move : -move;
