@@ -3,8 +3,8 @@
 // The kernels differ in how much of Y a workgroup owns.  Large tiles read each operand less often; small ones are more, start sooner and
 // leave fewer compute units idle, and where even they are few the contraction is shared.  Which is ahead depends on all of rows, outputs,
 // contraction, X's type and the groups, so each form's time is estimated and the shortest taken.  The estimates are fits to the
-// kernels' times over shapes drawn at random (1 to 8192 rows, 64 to 28672 outputs, 64 to 11008 deep; 4 to 64 experts): mean error 9 to 20 % a form, and
-// the form chosen is 2 % (one weight) and 5 % (experts) slower in the geometric mean than the best of them all.
+// kernels' times over shapes drawn at random (1 to 8192 rows, 64 to 28672 outputs, 64 to 28672 deep; 4 to 128 experts): mean error 9 to 15 % a form, and
+// the form chosen is 2 % (one weight) and 4 % (experts) slower in the geometric mean than the best of them all.
 #pragma once
 
 #include <algorithm>
@@ -35,30 +35,32 @@ struct TileForm {
     float read;                    // MB/us: operands through the L2
 };
 constexpr TileForm TILE_FORMS_16[] = {
-    {Form::ring32, 32, 256, 1, true, 1.50f, 3.52f, 0.610f, 1.00f, 0.98f, 1.6f, 8.0f},
-    {Form::ring64, 64, 64, 1, true, 2.35f, 2.36f, 0.450f, 1.21f, 0.24f, 1.9f, 12.6f},
-    {Form::ring64w, 64, 128, 1, true, 3.37f, 2.16f, 0.548f, 1.01f, 0.41f, 3.0f, 24.4f},
-    {Form::mid, 128, 128, 1, true, 1.50f, 4.35f, 0.860f, 1.00f, 1.00f, 2.7f, 8.4f},
-    {Form::big, 128, 256, 1, true, 6.72f, 0.20f, 1.217f, 1.01f, 1.00f, 4.0f, 5.8f}};
+    {Form::ring32, 32, 256, 1, true, 1.50f, 3.39f, 0.598f, 1.00f, 1.00f, 2.0f, 8.1f},
+    {Form::ring64, 64, 64, 1, true, 3.25f, 1.53f, 0.422f, 1.09f, 0.25f, 2.1f, 12.6f},
+    {Form::ring64w, 64, 128, 1, true, 3.73f, 1.68f, 0.544f, 1.03f, 0.46f, 3.5f, 31.4f},
+    {Form::mid, 128, 128, 1, true, 1.53f, 4.24f, 0.808f, 1.00f, 0.99f, 3.2f, 8.5f},
+    {Form::big, 128, 256, 1, true, 1.50f, 4.66f, 1.367f, 1.01f, 1.00f, 4.0f, 8.6f}};
 constexpr TileForm TILE_FORMS_MX[] = {
-    {Form::ring32, 32, 128, 1, true, 2.45f, 2.25f, 0.212f, 1.12f, 0.43f, 1.4f, 21.2f},
-    {Form::ring64, 64, 64, 1, true, 3.12f, 1.26f, 0.189f, 1.25f, 0.48f, 1.6f, 15.9f},
-    {Form::ring64w, 64, 128, 1, true, 3.38f, 1.63f, 0.243f, 1.05f, 0.48f, 2.7f, 19.7f},
-    {Form::mid, 128, 128, 2, false, 2.52f, 2.97f, 0.594f, 1.00f, 0.48f, 0.0f, 13.0f},
-    {Form::big, 256, 256, 2, false, 1.50f, 5.69f, 1.598f, 1.00f, 1.00f, 0.0f, 8.2f}};
+    {Form::ring32, 32, 128, 1, true, 3.33f, 1.32f, 0.206f, 1.01f, 0.80f, 1.7f, 10.7f},
+    {Form::ring64, 64, 64, 1, true, 3.67f, 0.68f, 0.188f, 1.19f, 0.60f, 1.9f, 29.4f},
+    {Form::ring64w, 64, 128, 1, true, 4.34f, 0.60f, 0.234f, 1.01f, 0.65f, 3.4f, 20.7f},
+    {Form::mid, 128, 128, 2, false, 3.50f, 1.88f, 0.602f, 1.03f, 0.41f, 0.0f, 34.9f},
+    {Form::big, 256, 256, 2, false, 1.50f, 4.94f, 1.471f, 1.01f, 1.00f, 0.0f, 8.5f}};
 struct RowForm {
     int out_tiles;
     float start, pass, piece, rows;   // us: of the launch, of a pass over the contraction, of a wave's piece, and of 16 rows of X with it
-    float fill, share, more;          // (as above; us of adding up for 16 rows, and for each 16 more)
+    float fill, steps;                // as above
+    float share, more;                // us: of adding up for 16 rows, and for each 16 more
+    float read;                       // MB/us: of W, most of it from memory
 };
 constexpr RowForm ROW_FORMS_16[] = {
-    {1, 3.88f, 0.47f, 0.13f, 0.77f, 0.80f, 0.60f, 0.53f},
-    {2, 3.65f, 0.77f, 0.43f, 0.87f, 0.90f, 0.56f, 0.93f},
-    {4, 3.71f, 0.89f, 0.73f, 1.24f, 0.80f, 0.78f, 1.52f}};
+    {1, 3.22f, 0.45f, 0.26f, 0.87f, 1.02f, 0.72f, 1.05f, 0.49f, 4.3f},
+    {2, 3.10f, 0.71f, 0.46f, 0.94f, 0.96f, 0.52f, 0.96f, 0.80f, 5.0f},
+    {4, 3.25f, 0.94f, 0.76f, 1.24f, 0.99f, 0.87f, 1.07f, 1.44f, 4.9f}};
 constexpr RowForm ROW_FORMS_MX[] = {
-    {1, 2.80f, 0.33f, 0.20f, 0.22f, 0.89f, 0.98f, 0.22f},
-    {2, 2.83f, 0.29f, 0.45f, 0.28f, 0.90f, 0.72f, 0.72f},
-    {4, 2.44f, 0.77f, 0.86f, 0.53f, 0.83f, 1.02f, 1.34f}};
+    {1, 2.50f, 0.29f, 0.25f, 0.25f, 1.02f, 0.79f, 1.31f, 0.18f, 7.0f},
+    {2, 2.70f, 0.26f, 0.39f, 0.36f, 1.05f, 0.94f, 1.01f, 0.63f, 6.5f},
+    {4, 2.19f, 0.78f, 0.84f, 0.61f, 0.99f, 0.81f, 1.42f, 1.26f, 5.0f}};
 
 // experts 0: one weight.  copy: X has to be copied for all forms but rows (a launch more).
 inline Plan mx4_plan(int64_t n_rows, int64_t out, int64_t in, int experts, bool mx, bool copy) {
@@ -87,20 +89,21 @@ inline Plan mx4_plan(int64_t n_rows, int64_t out, int64_t in, int experts, bool 
             const double tiles = up(double(out) / (16 * f.out_tiles));
             for (int s = 1; s <= 8; s *= 2) {
                 if (s > 1 && (experts || n_rows > 64 || s > np || tiles > MOST_SHARED)) break;
-                const double rounds = std::max(1.0, active * tiles * s / (256 * f.fill)), rows = std::min(avg / loops, 16.0 * rt);
+                const double full = std::max(1.0, active * tiles * s / (256 * f.fill)), rounds = f.steps * up(full - 1e-9) + (1.0 - f.steps) * full, rows = std::min(avg / loops, 16.0 * rt);
                 double t = f.start + rounds * loops * (f.pass + up(np / (8 * s)) * (f.piece + f.rows * rows / 16.0));
-                t = std::max(t, f.start + weight / 5.2e6) + (s > 1 ? f.share + f.more * (rt - 1) : 0.0);
+                t = std::max(t, f.start + weight / (f.read * 1e6)) + (s > 1 ? f.share + f.more * (rt - 1) : 0.0);
                 take(t, Plan{Form::rows, s, f.out_tiles, rt});
             }
         }
     }
     auto tile = [&](const TileForm& f) {
+        if (!experts && n_rows * 4 <= f.bm && f.bm > 64) return;  // (24 rows of 8320 -> 27392 took 1.3 times as long by 128 as by 32)
         const double rt = experts ? std::max(active, double(n_rows) / f.bm + 0.5 * active) : up(double(n_rows) / f.bm);
         const double tiles = rt * up(double(out) / f.bn);
         for (int s = 1; s <= (f.shares && !experts ? 8 : 1); s *= 2) {
             if (s > 1 && (s > np || tiles * s > MOST_SHARED)) break;
             const double full = std::max(1.0, tiles * s / (256 * f.fill)), rounds = f.steps * up(full - 1e-9) + (1.0 - f.steps) * full;
-            double t = f.start + rounds * (f.tile + up(np / (s * f.pieces)) * f.stage);
+            double t = f.start + rounds * (f.tile + up(np / (s * f.pieces)) * f.stage) + double(n_rows) * double(out) * 2.0 / 5.0e6;      // (Y's way out)
             t = std::max({t, f.start + weight / 5.0e6, f.start + tiles * np * (f.bm * (mx ? 64.0 : 256.0) + f.bn * 64.0) / (f.read * 1e6)}) + (s > 1 ? f.share + s * part / 6.0e6 : 0.0);
             take(t + (copy ? 4.0 + double(n_rows) * double(in) * 4.0 / 5.0e6 : 0.0), Plan{f.form, s, 0, 0});
         }

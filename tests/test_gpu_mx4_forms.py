@@ -8,6 +8,7 @@ import torch
 
 from mx4_forms import MX4_FORMS
 from paper_2309_15531_amd import binding as B
+from test_gpu_mx4 import check_experts
 
 pytestmark = pytest.mark.gpu
 
@@ -167,3 +168,12 @@ def test_rows_of_x_beyond_4_gb(ctx):
         offsets = torch.tensor([0, len(rows)], dtype=torch.int32, device="cuda")
         ctx.adadim_mx4_matmul_experts(X, codes[None], scales[None], offsets, Y, rows=rows)
         check(Y, X[rows.long()].float(), wv)
+
+
+@pytest.mark.parametrize("x,y", [("f16", "f16"), ("bf16", "f32"), ("mx4", "bf16")])
+@pytest.mark.parametrize("places", [(0,), (129,), (3, 64), (63, 64, 65), (1, 1, 127, 128, 128, 129), (5,) * 20])
+def test_fewer_rows_than_experts(ctx, places, x, y):
+    """Groups with rows are found among many empty ones; rows in front of the first and behind the last stay."""
+    sizes = [places.count(e) for e in range(130)]
+    check_experts(ctx, sizes, 70, 260, x, y, lead=2, tail=1)
+    check_experts(ctx, sizes, 70, 260, x, y, seed=1)
