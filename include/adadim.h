@@ -387,6 +387,7 @@ int adadim_mx4_dequantize(adadim_ctx* ctx, const uint8_t* codes, const uint8_t* 
  *   Y       [tokens, out] of y_type F16, BF16 or F32, pitch ldy
  * Products are exact (a weight outside fp16's range meets fp16 activations as bf16 in two parts), sums are fp32 on the
  * matrix cores in a fixed order (the same bits every run; the order depends on the sizes), rounded once.  tokens may be 0.
+ * Row pitches up to 2^31 - 1 elements.
  */
 int adadim_mx4_matmul(adadim_ctx* ctx, const void* X, const uint8_t* x_scales, int x_type, int64_t tokens, int64_t ldx,
                       const uint8_t* codes, const uint8_t* scales, int64_t out, int64_t in, void* Y, int y_type, int64_t ldy);

