@@ -161,8 +161,9 @@ __device__ __forceinline__ void store_tile(const Product& a, const float16v (&ac
 // of 55 at 8192 deep).  256 x 256: 8192 x 8192 x 8192 248 us (4.43 PFLOP/s; instructions on registers alone reach 6.4 with such operands),
 // 8192 x 8192 -> 28672 868 to 903 us, 4096 tokens x 2 of 16 experts, 5120 -> 4096, 139 to 152 us.  128 x 128: 2048 x 4096 -> 4096 24.6 us.  Between them, 128 x 256
 // and 256 x 128 by four waves took 1.2 to 1.4 times 256 x 256: LDS gives them too few operands.  Scales read from memory by each wave took
-// 3 to 10 % longer than those brought to LDS with the codes.  Prefetching a stage further into the L2 took 5 % longer; a workgroup that goes on to
-// further tiles, the next one's first stage under the output of the last, took 10 % longer (its addresses spill).
+// 3 to 10 % longer than those brought to LDS with the codes.  Prefetching a stage further into the L2 took 5 % longer.  Workgroups that go on to
+// further tiles, the next one's first stage under the output of the last, gained nothing (258 us both; the experts 152 against 144): the time saved goes
+// into a lower clock.
 template <int BM, int BN, int WT, int WO>
 struct Tiles {
     static constexpr int NW = WT * WO, TT = BM / WT / 32, TO = BN / WO / 32;
