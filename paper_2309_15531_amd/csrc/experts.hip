@@ -9,12 +9,28 @@
 
 namespace {
 
-// Larger number, larger key; -infinity and NaN have key 0 and never win.  (-0 and +0 are equal scores.)
-__device__ __forceinline__ uint32_t score_key(float f) {
-    if (!(f > -INFINITY)) return 0u;
-    const uint32_t u = __float_as_uint(f + 0.0f);
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
-}
+// Larger number, larger key; -infinity and NaN have key 0 and never win.  (-0 and +0 are equal scores.)  A 16-bit score's key has its place
+// below it, the lower the larger: one comparison finds both.
+template <class T>
+struct Keys {
+    static constexpr bool WITH_PLACE = sizeof(T) == 2;
+    static __device__ __forceinline__ uint32_t of(float f, uint32_t place) {
+        if (!(f > -INFINITY)) return 0u;
+        if constexpr (WITH_PLACE) {
+            const uint32_t u = __builtin_bit_cast(uint16_t, static_cast<T>(f + 0.0f));
+            return (u & 0x8000u ? ~u : u | 0x8000u) << 16 | (0xffffu - place);
+        } else {
+            const uint32_t u = __float_as_uint(f + 0.0f);
+            return u & 0x80000000u ? ~u : u | 0x80000000u;
+        }
+    }
+    static __device__ __forceinline__ float score(uint32_t key) {
+        if constexpr (WITH_PLACE) {
+            const uint32_t u = key >> 16;
+            return static_cast<float>(__builtin_bit_cast(T, static_cast<uint16_t>(u & 0x8000u ? u & 0x7fffu : ~u)));
+        } else return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
+    }
+};
 
 constexpr int RT_TOKENS = 64;                     // tokens of a chunk: one bit each of an expert's mask
 constexpr int RT_THREADS = 1024;
@@ -112,7 +128,7 @@ __global__ __launch_bounds__(RT_THREADS) void route_choose(Route a) {
             for (int v_ = 0; v_ < V; ++v_) f[v_] = v_ < have ? static_cast<float>(l[v_]) : -INFINITY;
         }
 #pragma unroll
-        for (int v = 0; v < V; ++v) key[v] = score_key(f[v]);
+        for (int v = 0; v < V; ++v) key[v] = Keys<T>::of(f[v], sub * V + v);
         float top = 0.0f, sum = 0.0f, mine[2] = {};           // lane j (and j + W): exp(l - max) of the j-th chosen
         int32_t index[2] = {-1, -1};
         for (int j = 0; j < a.k; ++j) {
@@ -120,18 +136,24 @@ __global__ __launch_bounds__(RT_THREADS) void route_choose(Route a) {
 #pragma unroll
             for (int v = 0; v < V; ++v) best = max(best, key[v]);
             best = over_lanes<W>(best, [](uint32_t x, uint32_t y) { return max(x, y); });
-            uint32_t at = 0xffffffffu;
-#pragma unroll
-            for (int v = V - 1; v >= 0; --v)
-                if (key[v] == best) at = sub * V + v;
-            at = over_lanes<W>(at, [](uint32_t x, uint32_t y) { return min(x, y); });
             if (__ballot(best != 0u) == 0) break;             // nothing left of any of the wave's tokens
+            uint32_t at = 0xffffu - (best & 0xffffu);
+            if constexpr (Keys<T>::WITH_PLACE) {
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (at == static_cast<uint32_t>(sub * V + v)) key[v] = 0u;
+                for (int v = 0; v < V; ++v)
+                    if (key[v] == best) key[v] = 0u;
+            } else {
+                at = 0xffffffffu;
+#pragma unroll
+                for (int v = V - 1; v >= 0; --v)
+                    if (key[v] == best) at = sub * V + v;
+                at = over_lanes<W>(at, [](uint32_t x, uint32_t y) { return min(x, y); });
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    if (at == static_cast<uint32_t>(sub * V + v)) key[v] = 0u;
+            }
             if (best != 0u) {
-                const uint32_t u = best & 0x80000000u ? best & 0x7fffffffu : ~best;            // back from the key
-                const float val = __uint_as_float(u);
+                const float val = Keys<T>::score(best);
                 if (j == 0) top = val;
                 const float p = val == top ? 1.0f : expf(val - top);
                 sum += p;
