@@ -25,7 +25,7 @@ constexpr int XF16 = ADADIM_TYPE_F16, XBF16 = ADADIM_TYPE_BF16, XMX4 = ADADIM_TY
 //
 // Eight waves, so that a wave has few pieces one after the other (4 at 4096 deep); NT by the estimates of mx4_plan.h: more outputs of a
 // workgroup read X less often, fewer give more workgroups.  With weights that come from memory: 1 token, 28672 -> 8192, mx4 X 24.6 us
-// (5.1 TB/s), 8192 -> 28672 fp16 31 us (4.0 TB/s), 4096 -> 11008 8.9 us (2.7 TB/s: a launch's start is 3 us of it); 16 tokens x 2 of 8
+// (5.1 TB/s), 8192 -> 28672 fp16 30 us (4.1 TB/s), 4096 -> 11008 8.2 us (2.9 TB/s: a launch's start is 3 us of it); 16 tokens x 2 of 8
 // experts, 4096 -> 11008 fp16 45 us (4.2 TB/s).  Deeper unrolling, a second set of registers for the next piece, and X turned in LDS gained
 // nothing.
 constexpr int RW_WAVES = 8;

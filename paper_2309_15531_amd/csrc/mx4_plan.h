@@ -55,12 +55,12 @@ struct RowForm {
 };
 constexpr RowForm ROW_FORMS_16[] = {
     {1, 3.22f, 0.45f, 0.26f, 0.87f, 1.02f, 0.72f, 1.05f, 0.49f, 4.3f},
-    {2, 3.10f, 0.71f, 0.46f, 0.94f, 0.96f, 0.52f, 0.96f, 0.80f, 5.0f},
-    {4, 3.25f, 0.94f, 0.76f, 1.24f, 0.99f, 0.87f, 1.07f, 1.44f, 4.9f}};
+    {2, 3.10f, 0.71f, 0.46f, 0.94f, 0.96f, 0.52f, 0.96f, 0.80f, 4.6f},
+    {4, 3.25f, 0.94f, 0.76f, 1.24f, 0.99f, 0.87f, 1.07f, 0.0f, 5.2f}};
 constexpr RowForm ROW_FORMS_MX[] = {
     {1, 2.50f, 0.29f, 0.25f, 0.25f, 1.02f, 0.79f, 1.31f, 0.18f, 7.0f},
     {2, 2.70f, 0.26f, 0.39f, 0.36f, 1.05f, 0.94f, 1.01f, 0.63f, 6.5f},
-    {4, 2.19f, 0.78f, 0.84f, 0.61f, 0.99f, 0.81f, 1.42f, 1.26f, 5.0f}};
+    {4, 2.19f, 0.78f, 0.84f, 0.61f, 0.99f, 0.81f, 1.42f, 0.0f, 5.0f}};
 
 // experts 0: one weight.  copy: X has to be copied for all forms but rows (a launch more).
 inline Plan mx4_plan(int64_t n_rows, int64_t out, int64_t in, int experts, bool mx, bool copy) {
@@ -91,7 +91,8 @@ inline Plan mx4_plan(int64_t n_rows, int64_t out, int64_t in, int experts, bool 
                 if (s > 1 && (experts || n_rows > 64 || s > np || tiles > MOST_SHARED)) break;
                 const double full = std::max(1.0, active * tiles * s / (256 * f.fill)), rounds = f.steps * up(full - 1e-9) + (1.0 - f.steps) * full, rows = std::min(avg / loops, 16.0 * rt);
                 double t = f.start + rounds * loops * (f.pass + up(np / (8 * s)) * (f.piece + f.rows * rows / 16.0));
-                t = std::max(t, f.start + weight / (f.read * 1e6)) + (s > 1 ? f.share + f.more * (rt - 1) : 0.0);
+                // (a workgroup of few reads 28 GB/s: 64 to 128 of four output tiles 1.9 to 3.1 TB/s)
+                t = std::max(t, f.start + weight / std::min(f.read * 1e6, active * tiles * s * 28e3)) + (s > 1 ? f.share + f.more * (rt - 1) : 0.0);
                 take(t, Plan{Form::rows, s, f.out_tiles, rt});
             }
         }
@@ -104,7 +105,7 @@ inline Plan mx4_plan(int64_t n_rows, int64_t out, int64_t in, int experts, bool 
             if (s > 1 && (s > np || tiles * s > MOST_SHARED)) break;
             const double full = std::max(1.0, tiles * s / (256 * f.fill)), rounds = f.steps * up(full - 1e-9) + (1.0 - f.steps) * full;
             double t = f.start + rounds * (f.tile + up(np / (s * f.pieces)) * f.stage) + double(n_rows) * double(out) * 2.0 / 5.0e6;      // (Y's way out)
-            t = std::max({t, f.start + weight / 5.0e6, f.start + tiles * np * (f.bm * (mx ? 64.0 : 256.0) + f.bn * 64.0) / (f.read * 1e6)}) + (s > 1 ? f.share + s * part / 6.0e6 : 0.0);
+            t = std::max({t, f.start + weight / 4.6e6, f.start + tiles * np * (f.bm * (mx ? 64.0 : 256.0) + f.bn * 64.0) / (f.read * 1e6)}) + (s > 1 ? f.share + s * part / 6.0e6 : 0.0);
             take(t + (copy ? 4.0 + double(n_rows) * double(in) * 4.0 / 5.0e6 : 0.0), Plan{f.form, s, 0, 0});
         }
     };
