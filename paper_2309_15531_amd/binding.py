@@ -18,7 +18,6 @@ DIM_OC, DIM_IC = 0, 1
 DW_F32, DW_F16, DW_F16_SCALED = 0, 1, 2
 TYPE_F16, TYPE_BF16, TYPE_F32, TYPE_MX4 = 0, 1, 2, 3
 _TYPES = {"torch.float16": TYPE_F16, "torch.bfloat16": TYPE_BF16, "torch.float32": TYPE_F32}
-_DTYPES: dict = {}      # element type -> (its name, its TYPE_ number or None), filled as types are met
 
 EXPORTS = (
     "adadim_create", "adadim_destroy", "adadim_last_error", "adadim_version", "adadim_score_elems",
@@ -208,21 +207,22 @@ def mx4_shapes(rows: int, cols: int):
     return (rows, 64 * pieces), (pieces, rows, 4)
 
 
-def _dtype(t):
-    """(name, TYPE_ number or None) of a tensor's element type."""
-    d = t.dtype
-    try:
-        return _DTYPES[d]
-    except KeyError:
+class _Dtypes(dict):
+    """(name, TYPE_ number or None) by element type, filled in as types are met."""
+
+    def __missing__(self, d):
         name = str(d)
-        _DTYPES[d] = r = (name, _TYPES.get(name))
+        self[d] = r = (name, _TYPES.get(name))
         return r
+
+
+_DTYPES = _Dtypes()
 
 
 # The calls of a decode step take a few microseconds on the GPU: what follows looks at each tensor no more often than it must.
 def _array(t, what: str, dtype: str, shape) -> int:
     """Address of a contiguous device tensor of that element type and shape."""
-    if t.shape != shape or not t.is_contiguous() or not t.is_cuda or _dtype(t)[0] != dtype:
+    if t.shape != shape or not t.is_contiguous() or not t.is_cuda or _DTYPES[t.dtype][0] != dtype:
         _need(t, what, dtype[6:])
         raise ValueError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
     return t.data_ptr()
@@ -234,7 +234,7 @@ def _matrix(t, what: str):
     shape = t.shape
     if len(shape) != 2:
         raise ValueError(f"{what}: expected two axes, got shape {tuple(shape)}")
-    kind = _dtype(t)[1]
+    kind = _DTYPES[t.dtype][1]
     if kind is None:
         raise TypeError(f"{what}: expected float16, bfloat16 or float32, got {t.dtype}")
     rows, cols = shape
@@ -474,7 +474,7 @@ class Context:
     def _mx4_input(self, X, x_scales, in_f):
         """(address, scales' address, type, tokens, in, pitch) of a product's left operand; mx4 codes are told by their type
         and need in_f."""
-        if _dtype(X)[0] == "torch.uint8":
+        if _DTYPES[X.dtype][0] == "torch.uint8":
             if in_f is None or x_scales is None:
                 raise ValueError("X in mx4 needs in_f and x_scales")
             tokens = X.shape[0]
