@@ -108,3 +108,41 @@ fake.fake_reset()
 assert product(ctx, *SHARED) == OK and not launched("mx4_zero_tickets")
 lib.adadim_graph_destroy(g)
 """)
+
+
+def test_failures_of_the_other_calls_fail_no_later_one(run):  # noqa: F811
+    """An allocation or a launch that fails is reported by its own call and by no other; the next one does all its work."""
+    run(MATMUL + """
+def odd(ctx):                                                  # rows that have to be copied for the tiles
+    return lib.adadim_mx4_matmul(ctx, A, None, 0, c_int64(700), c_int64(333), A, A, c_int64(512), c_int64(333), A, 2, c_int64(512))
+def route(ctx, tokens=700):
+    return lib.adadim_expert_route(ctx, A, 2, c_int64(tokens), c_int64(16), 16, 2, 1, A, A, A, A, A)
+def experts(ctx):
+    return lib.adadim_mx4_matmul_experts(ctx, A, None, 1, c_int64(8), c_int64(256), A, c_int64(16), A, 64, A, A, c_int64(96), c_int64(256), A, 1, c_int64(96))
+def combine(ctx):
+    return lib.adadim_expert_combine(ctx, A, 1, c_int64(16), c_int64(96), c_int64(96), A, A, c_int64(8), 2, A, 1, c_int64(96))
+def quantize(ctx):
+    return lib.adadim_mx4_quantize(ctx, A, 1, c_int64(8), c_int64(96), c_int64(96), A, A, None, 0, None)
+def dequantize(ctx):
+    return lib.adadim_mx4_dequantize(ctx, A, A, c_int64(8), c_int64(96), A, 1, c_int64(96))
+for call, kernels, allocates in ((odd, ["mx4_copy_rows", "mx4_ring"], True), (route, ["route_choose", "route_place"], True),
+                                 (lambda c: route(c, 5), ["route_choose"], False), (lambda c: route(c, 0), ["route_none"], False),
+                                 (experts, ["mx4_rows"], False), (combine, ["combine_rows"], False),
+                                 (quantize, ["mx4_quantize_rows"], False), (dequantize, ["mx4_dequantize_rows"], False)):
+    for what in kernels + ["hipMalloc"] * allocates:
+        ctx = context()
+        fake.fake_reset()
+        fake.fake_fail(what.encode(), 1)
+        assert call(ctx) == EHIP, what
+        assert product(ctx, *PLAIN) == OK, what
+        fake.fake_reset()
+        assert call(ctx) == OK, lib.adadim_last_error(ctx)
+        order = [c.split()[1] for c in calls() if c.startswith("launch")]
+        assert len(order) == len(kernels) and all(k in o for k, o in zip(kernels, order)), order
+        lib.adadim_destroy(ctx)
+# workgroups of the few-row kernel: for as many groups as there are rows
+ctx = context()
+fake.fake_reset()
+assert experts(ctx) == OK
+assert launched("mx4_rows")[0].split()[3] == "16", launched("mx4_rows")
+""")
