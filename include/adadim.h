@@ -399,6 +399,7 @@ int adadim_mx4_matmul(adadim_ctx* ctx, const void* X, const uint8_t* x_scales, i
  *   offsets  int32 [experts + 1], device: not decreasing, inside [0, n_rows] (values outside are taken as the nearer end).
  *            Groups may be empty.  Rows of Y in no group are not written.
  *   rows     int32 [n_rows], device, or NULL: row r of X (then tokens == n_rows).  An entry outside [0, tokens) stands for a row of zeros.
+ *            Without tokens X and x_scales may be NULL: rows[] names none then.
  *   experts  1..1024
  */
 int adadim_mx4_matmul_experts(adadim_ctx* ctx, const void* X, const uint8_t* x_scales, int x_type, int64_t tokens, int64_t ldx,

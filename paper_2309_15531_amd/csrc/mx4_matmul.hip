@@ -288,7 +288,8 @@ __global__ __launch_bounds__(64 * RW_WAVES) void mx4_rows(ProductArgs args, void
     }
 }
 
-// X in the order of Y's rows, for kernels that read 16 bytes at a time and reach rows by 32-bit offsets: copied where it does not lie so.
+// X in the order of Y's rows, for kernels that read 16 bytes at a time, reach rows by 32-bit offsets and read another row in place of one that
+// does not exist: copied where it does not lie so.
 // 16-bit rows become whole pieces, filled up with zeros.  PITCH: bytes of a row.
 template <bool MX>
 __global__ __launch_bounds__(256) void mx4_copy_rows(ProductArgs args, int64_t pitch, uint8_t* __restrict__ to, uint32_t* __restrict__ to_scales) {
@@ -448,7 +449,9 @@ int launch_product(adadim_ctx* ctx, Product a) {
     // offsets are taken from token 0 where rows[] is given, from a tile's first row otherwise
     const int64_t pitch = MX ? pieces(a.in) * PIECE_BYTES : 2 * a.ldx;
     const bool far = (a.gather ? a.tokens : min(a.n_rows, int64_t(256))) * pitch >= int64_t(NO_ROW);
-    if ((odd && p.form != Form::rows) || (far && (a.gather || !MX))) {
+    // Without tokens there is no row 0 for the kernels to read in place of those that rows[] does not name: the copy is made of zeros alone.
+    const bool none = a.tokens == 0;
+    if ((odd && p.form != Form::rows) || (far && (a.gather || !MX)) || none) {
         const int64_t to_pitch = MX ? pitch : pieces(a.in) * (2 * PIECE), blocks = (a.n_rows * to_pitch / 16 + 255) / 256;
         if (blocks > INT32_MAX) return adadim_fail(ctx, ADADIM_EINVAL, "mx4 product: X too large to be copied");
         const size_t codes = size_t(a.n_rows) * size_t(to_pitch);

@@ -1,0 +1,61 @@
+"""The host path of the microscaled operators: memory that a kernel would read where there is none, without a GPU."""
+import os
+import shutil
+import subprocess
+import sys
+import textwrap
+
+import pytest
+
+from paper_2309_15531_amd import binding as B
+from test_host_path_cpu import PREAMBLE
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+CALLS = """
+def matmul(ctx, rows, out, inn):
+    return lib.adadim_mx4_matmul(ctx, A, None, 0, c_int64(rows), c_int64(inn), A, A, c_int64(out), c_int64(inn), A, 2, c_int64(out))
+def experts(ctx, x_type, tokens, rows, out, inn, n=8, X=A, xs=A):
+    return lib.adadim_mx4_matmul_experts(ctx, X, xs, x_type, c_int64(tokens), c_int64(inn), A, c_int64(rows), A, n, A, A, c_int64(out),
+                                         c_int64(inn), A, 2, c_int64(out))
+def names():
+    return [c.split()[1] for c in calls() if c.startswith("launch")]
+"""
+
+
+@pytest.fixture(scope="module")
+def run(tmp_path_factory):
+    if shutil.which("g++") is None:
+        pytest.skip("no host compiler")
+    if not os.path.exists(B.LIB_PATH):
+        from paper_2309_15531_amd.build import build
+        build(verbose=False)
+    fake = tmp_path_factory.mktemp("fake") / "libfake_hip.so"
+    subprocess.run(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", os.path.join(ROOT, "tests", "host", "fake_hip_memory.cpp"), "-o",
+                    str(fake)], check=True)
+
+    def go(body):
+        res = subprocess.run([sys.executable, "-c", PREAMBLE + CALLS + textwrap.dedent(body), str(fake), B.LIB_PATH],
+                             capture_output=True, text=True, timeout=120)
+        assert res.returncode == 0, res.stdout + res.stderr
+        return res.stdout
+    return go
+
+
+@pytest.mark.parametrize("x_type", [B.TYPE_F16, B.TYPE_BF16, B.TYPE_MX4])
+@pytest.mark.parametrize("rows,out,inn,kernel", [(3, 96, 256, "mx4_rows"), (619, 4312, 136, None), (1999, 837, 160, None), (5000, 4096, 1024, None)])
+def test_without_tokens_no_kernel_reads_x(run, x_type, rows, out, inn, kernel):
+    """No row of X exists, so rows[] can name none: rows of zeros.  X and its scales may be NULL then; what a kernel reads in place of a
+    row that does not exist has to be memory of the library's own."""
+    run(f"""
+    ctx = context()
+    for X in (None, A):
+        fake.fake_reset()
+        assert experts(ctx, {x_type}, 0, {rows}, {out}, {inn}, X=X, xs=X) == OK, lib.adadim_last_error(ctx)
+        order = names()
+        assert len(order) == 2 and "mx4_copy_rows" in order[0], order
+        assert {kernel!r} is None or {kernel!r} in order[1], order
+        given = dict(c.split() for c in calls() if c.startswith("x"))
+        assert int(given["x"], 16) not in (0, A.value), given
+        assert {x_type} != {B.TYPE_MX4} or int(given["x_scales"], 16) not in (0, A.value), given
+    """)
