@@ -39,6 +39,7 @@ void* adadim_workspace(adadim_ctx* ctx, int slot, size_t bytes) {
         }
         ctx->ws[slot] = nullptr;
         ctx->ws_bytes[slot] = 0;
+        ctx->ws_cleared[slot] = false;                        // whatever comes next is other memory, of the same size or not
     }
     size_t want = (bytes + 255) & ~size_t(255);
     void* p = nullptr;

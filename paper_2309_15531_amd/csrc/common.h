@@ -64,9 +64,7 @@ struct adadim_ctx {
     char err[512];
     void* ws[WS_COUNT];
     size_t ws_bytes[WS_COUNT];
-    size_t zero_ready_bytes;         // size of WS_ZERO when it was last cleared
-    size_t mx4_ready_bytes;          // size of WS_MX4_PART when its counters were last cleared
-    size_t gemv_ready_bytes;         // size of WS_GEMV_PART when its counters were last cleared
+    bool ws_cleared[WS_COUNT];       // the slot's memory holds the zeros that its kernels count on (WS_ZERO all of it, others their counters)
     // Gram launch plans already chosen, keyed by (token count, tile count, whether whole tiles may store): choosing
     // one simulates the launch's schedule (milliseconds of host time), and a model driver alternates between a few
     // input widths

@@ -358,11 +358,11 @@ int launch_gemv_ic(adadim_ctx* ctx, const uint32_t* packed, const void* scales, 
     if (!slot) return ADADIM_EHIP;
     unsigned int* ticket = reinterpret_cast<unsigned int*>(slot);
     float* part = reinterpret_cast<float*>(slot + GV_COUNTERS);
-    if (sh.chunks > 1 && ctx->gemv_ready_bytes != ctx->ws_bytes[WS_GEMV_PART]) {
+    if (sh.chunks > 1 && !ctx->ws_cleared[WS_GEMV_PART]) {
         hipLaunchKernelGGL(gemv_zero, dim3(1), dim3(GV_SLOTS), 0, ctx->stream, ticket);
         ADADIM_LAUNCH_CHECK(ctx, "gemv_zero");
         // a clearing that is only recorded has not happened yet for the calls outside the graph
-        if (!ctx->capturing) ctx->gemv_ready_bytes = ctx->ws_bytes[WS_GEMV_PART];
+        if (!ctx->capturing) ctx->ws_cleared[WS_GEMV_PART] = true;
     }
     const int64_t n_words = out * bits / 32;
     const dim3 grid(static_cast<unsigned>(sh.tiles), static_cast<unsigned>(sh.chunks));

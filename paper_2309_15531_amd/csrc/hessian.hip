@@ -446,12 +446,12 @@ size_t part_bytes_of(const GramPlan& plan, int bt) {
 int zero_rows(adadim_ctx* ctx, int64_t ldx, void** zero16) {
     *zero16 = adadim_workspace(ctx, WS_ZERO, size_t(32) * size_t(ldx) * 2 + 512);
     if (!*zero16) return ADADIM_EHIP;
-    if (ctx->zero_ready_bytes != ctx->ws_bytes[WS_ZERO]) {
+    if (!ctx->ws_cleared[WS_ZERO]) {
         const int64_t n = static_cast<int64_t>(ctx->ws_bytes[WS_ZERO] / 4);
         hipLaunchKernelGGL(zero_f32, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, ctx->stream,
                            static_cast<float*>(*zero16), n);
         ADADIM_LAUNCH_CHECK(ctx, "zero_f32");
-        ctx->zero_ready_bytes = ctx->ws_bytes[WS_ZERO];
+        ctx->ws_cleared[WS_ZERO] = true;
     }
     return ADADIM_OK;
 }
@@ -640,12 +640,12 @@ extern "C" int adadim_probe_gram_timeline(adadim_ctx* ctx, const void* X, int64_
     float* part = static_cast<float*>(adadim_workspace(ctx, WS_HESS_PART, size_t(slots) * BT * BT * sizeof(float)));
     void* zero16 = adadim_workspace(ctx, WS_ZERO, size_t(32) * size_t(ldx) * 2 + 512);
     if (!part || !zero16) return ADADIM_EHIP;
-    if (ctx->zero_ready_bytes != ctx->ws_bytes[WS_ZERO]) {
+    if (!ctx->ws_cleared[WS_ZERO]) {
         const int64_t n = static_cast<int64_t>(ctx->ws_bytes[WS_ZERO] / 4);
         hipLaunchKernelGGL(zero_f32, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, ctx->stream,
                            static_cast<float*>(zero16), n);
         ADADIM_LAUNCH_CHECK(ctx, "zero_f32");
-        ctx->zero_ready_bytes = ctx->ws_bytes[WS_ZERO];
+        ctx->ws_cleared[WS_ZERO] = true;
     }
     static PerDeviceOnce once;
     ADADIM_HIP_TRY(ctx, once.run([] {

@@ -597,13 +597,13 @@ int launch_layer_error(adadim_ctx* ctx, int n, const void* const* dW, int dW_dty
     void* zero16 = adadim_workspace(ctx, WS_ZERO, 256);
     if (!zero16) return ADADIM_EHIP;
     sc.zero16 = zero16;
-    if (ctx->zero_ready_bytes != ctx->ws_bytes[WS_ZERO]) {
+    if (!ctx->ws_cleared[WS_ZERO]) {
         // a fill kernel rather than a memset node, so that the call stays safe to capture in a graph
         const int64_t nz = static_cast<int64_t>(ctx->ws_bytes[WS_ZERO] / 4);
         hipLaunchKernelGGL(fill_zero_f32, dim3(static_cast<unsigned>((nz + 255) / 256)), dim3(256), 0, ctx->stream,
                            static_cast<float*>(zero16), nz);
         ADADIM_LAUNCH_CHECK(ctx, "fill_zero_f32");
-        ctx->zero_ready_bytes = ctx->ws_bytes[WS_ZERO];
+        ctx->ws_cleared[WS_ZERO] = true;
     }
     int rc = set_error_attr(ctx);
     if (rc != ADADIM_OK) return rc;

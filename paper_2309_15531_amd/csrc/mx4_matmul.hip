@@ -322,11 +322,11 @@ __global__ void mx4_zero_tickets(unsigned* ticket) { ticket[threadIdx.x] = 0u; }
 int shares(adadim_ctx* ctx, size_t bytes, void*& shared) {
     shared = adadim_workspace(ctx, WS_MX4_PART, SHARE_TICKETS * 4 + bytes);
     if (!shared) return ADADIM_EHIP;
-    if (ctx->mx4_ready_bytes != ctx->ws_bytes[WS_MX4_PART]) {
+    if (!ctx->ws_cleared[WS_MX4_PART]) {
         hipLaunchKernelGGL(mx4_zero_tickets, dim3(1), dim3(SHARE_TICKETS), 0, ctx->stream, static_cast<unsigned*>(shared));
         ADADIM_LAUNCH_CHECK(ctx, "mx4_zero_tickets");
         // a clearing that is only recorded has not happened yet for the calls outside the graph
-        if (!ctx->capturing) ctx->mx4_ready_bytes = ctx->ws_bytes[WS_MX4_PART];
+        if (!ctx->capturing) ctx->ws_cleared[WS_MX4_PART] = true;
     }
     return ADADIM_OK;
 }

@@ -59,3 +59,31 @@ def test_without_tokens_no_kernel_reads_x(run, x_type, rows, out, inn, kernel):
         assert int(given["x"], 16) not in (0, A.value), given
         assert {x_type} != {B.TYPE_MX4} or int(given["x_scales"], 16) not in (0, A.value), given
     """)
+
+
+@pytest.mark.parametrize("small,large,clear,kernel", [
+    ("matmul(ctx, 12, 96, 8192)", "matmul(ctx, 40, 1500, 8192)", "mx4_zero_tickets", "mx4_rows"),
+    ("gemv(ctx, 1024, 1024)", "gemv(ctx, 28672, 8192)", "gemv_zero", "gemv_ic_tiles"),
+    # (the same columns at a larger pitch: nothing but the zeros behind the last token row grows)
+    ("hessian(ctx, 4096)", "hessian(ctx, 16384)", "zero_f32", "gram_tiles")])
+def test_memory_of_the_size_before_a_failed_growth_is_cleared_again(run, small, large, clear, kernel):
+    """Growing frees a slot before it allocates.  Where the allocation fails, a call that needs what there was before gets new memory of the
+    old size: the counters and zeros in it are not those that were cleared."""
+    run(f"""
+    def hessian(ctx, ldx):
+        return lib.adadim_hessian(ctx, A, c_int64(4096), c_int64(4096), c_int64(ldx), A, 0)
+    ctx = context()
+    assert {small} == OK, lib.adadim_last_error(ctx)
+    assert sum({clear!r} in c for c in names()) == 1, names()
+    fake.fake_reset()
+    assert {small} == OK and not any({clear!r} in c for c in names()), names()
+    fake.fake_reset()
+    fake.fake_fail(b"hipMalloc", 1)
+    assert {large} == EHIP
+    assert [c.split()[0] for c in calls() if c.startswith(("have", "free"))] == ["free"], calls()
+    for again in range(2):
+        fake.fake_reset()
+        assert {small} == OK, lib.adadim_last_error(ctx)
+        order = [c for c in names() if {clear!r} in c or {kernel!r} in c]
+        assert [{clear!r} in c for c in order] == ([True, False] if again == 0 else [False]), order
+    """)
