@@ -93,6 +93,10 @@ bool adadim_side_stream(adadim_ctx* ctx);
 
 // Returns a device buffer of at least `bytes` for `slot`, or nullptr (error recorded).
 void* adadim_workspace(adadim_ctx* ctx, int slot, size_t bytes);
+// A launch that clears the slot has been made.  One that is only recorded has not run yet for the calls outside the graph.
+inline void adadim_workspace_cleared(adadim_ctx* ctx, int slot) {
+    if (!ctx->capturing) ctx->ws_cleared[slot] = true;
+}
 
 #define ADADIM_HIP_TRY(ctx, expr)                                                          \
     do {                                                                                   \

@@ -361,8 +361,7 @@ int launch_gemv_ic(adadim_ctx* ctx, const uint32_t* packed, const void* scales, 
     if (sh.chunks > 1 && !ctx->ws_cleared[WS_GEMV_PART]) {
         hipLaunchKernelGGL(gemv_zero, dim3(1), dim3(GV_SLOTS), 0, ctx->stream, ticket);
         ADADIM_LAUNCH_CHECK(ctx, "gemv_zero");
-        // a clearing that is only recorded has not happened yet for the calls outside the graph
-        if (!ctx->capturing) ctx->ws_cleared[WS_GEMV_PART] = true;
+        adadim_workspace_cleared(ctx, WS_GEMV_PART);
     }
     const int64_t n_words = out * bits / 32;
     const dim3 grid(static_cast<unsigned>(sh.tiles), static_cast<unsigned>(sh.chunks));

@@ -451,7 +451,7 @@ int zero_rows(adadim_ctx* ctx, int64_t ldx, void** zero16) {
         hipLaunchKernelGGL(zero_f32, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, ctx->stream,
                            static_cast<float*>(*zero16), n);
         ADADIM_LAUNCH_CHECK(ctx, "zero_f32");
-        ctx->ws_cleared[WS_ZERO] = true;
+        adadim_workspace_cleared(ctx, WS_ZERO);
     }
     return ADADIM_OK;
 }
@@ -645,7 +645,7 @@ extern "C" int adadim_probe_gram_timeline(adadim_ctx* ctx, const void* X, int64_
         hipLaunchKernelGGL(zero_f32, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, ctx->stream,
                            static_cast<float*>(zero16), n);
         ADADIM_LAUNCH_CHECK(ctx, "zero_f32");
-        ctx->ws_cleared[WS_ZERO] = true;
+        adadim_workspace_cleared(ctx, WS_ZERO);
     }
     static PerDeviceOnce once;
     ADADIM_HIP_TRY(ctx, once.run([] {

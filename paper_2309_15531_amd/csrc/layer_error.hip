@@ -603,7 +603,7 @@ int launch_layer_error(adadim_ctx* ctx, int n, const void* const* dW, int dW_dty
         hipLaunchKernelGGL(fill_zero_f32, dim3(static_cast<unsigned>((nz + 255) / 256)), dim3(256), 0, ctx->stream,
                            static_cast<float*>(zero16), nz);
         ADADIM_LAUNCH_CHECK(ctx, "fill_zero_f32");
-        ctx->ws_cleared[WS_ZERO] = true;
+        adadim_workspace_cleared(ctx, WS_ZERO);
     }
     int rc = set_error_attr(ctx);
     if (rc != ADADIM_OK) return rc;

@@ -325,8 +325,7 @@ int shares(adadim_ctx* ctx, size_t bytes, void*& shared) {
     if (!ctx->ws_cleared[WS_MX4_PART]) {
         hipLaunchKernelGGL(mx4_zero_tickets, dim3(1), dim3(SHARE_TICKETS), 0, ctx->stream, static_cast<unsigned*>(shared));
         ADADIM_LAUNCH_CHECK(ctx, "mx4_zero_tickets");
-        // a clearing that is only recorded has not happened yet for the calls outside the graph
-        if (!ctx->capturing) ctx->ws_cleared[WS_MX4_PART] = true;
+        adadim_workspace_cleared(ctx, WS_MX4_PART);
     }
     return ADADIM_OK;
 }

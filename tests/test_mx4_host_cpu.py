@@ -87,3 +87,23 @@ def test_memory_of_the_size_before_a_failed_growth_is_cleared_again(run, small, 
         order = [c for c in names() if {clear!r} in c or {kernel!r} in c]
         assert [{clear!r} in c for c in order] == ([True, False] if again == 0 else [False]), order
     """)
+
+
+def test_zeros_whose_clearing_was_only_recorded_are_cleared_again(run):
+    """The clearing launch fails, and the next call is recorded: what it records has not run for the calls outside the graph."""
+    run("""
+    def hessian(ctx):
+        return lib.adadim_hessian(ctx, A, c_int64(4096), c_int64(4096), c_int64(4096), A, 0)
+    ctx = context()
+    fake.fake_fail(b"zero_f32", 1)
+    assert hessian(ctx) == EHIP
+    g = c_void_p()
+    assert lib.adadim_capture_begin(ctx) == OK
+    assert hessian(ctx) == OK, lib.adadim_last_error(ctx)
+    assert lib.adadim_capture_end(ctx, byref(g)) == OK
+    for again in range(2):
+        fake.fake_reset()
+        assert hessian(ctx) == OK
+        assert sum("zero_f32" in c for c in names()) == (again == 0), names()
+    lib.adadim_graph_destroy(g)
+    """)
