@@ -624,14 +624,14 @@ int launch_layer_error(adadim_ctx* ctx, int n, const void* const* dW, int dW_dty
         // scratch of the final reduction: per candidate one double per 256 rows; then the tickets
         const unsigned fin_blocks = static_cast<unsigned>((out + 255) / 256);
         const size_t fin_bytes = size_t(edma::MAX_BATCH) * fin_blocks * sizeof(double) + 256;
-        const bool fin_fresh = ctx->ws_bytes[WS_ERR_FIN] < fin_bytes;
         sc.block_tot = static_cast<double*>(adadim_workspace(ctx, WS_ERR_FIN, fin_bytes));
         if (!sc.block_tot) return ADADIM_EHIP;
         sc.ticket = reinterpret_cast<unsigned int*>(sc.block_tot + (ctx->ws_bytes[WS_ERR_FIN] - 256) / sizeof(double));
-        if (fin_fresh) {
+        if (!ctx->ws_cleared[WS_ERR_FIN]) {
             hipLaunchKernelGGL(fill_zero_f32, dim3(1), dim3(64), 0, ctx->stream, reinterpret_cast<float*>(sc.ticket),
                                int64_t(64));
             ADADIM_LAUNCH_CHECK(ctx, "fill_zero_f32");
+            adadim_workspace_cleared(ctx, WS_ERR_FIN);
         }
         sc.dW16 = nullptr;
         if (dW_dtype != ADADIM_DW_F16_SCALED) {

@@ -107,3 +107,19 @@ def test_zeros_whose_clearing_was_only_recorded_are_cleared_again(run):
         assert sum("zero_f32" in c for c in names()) == (again == 0), names()
     lib.adadim_graph_destroy(g)
     """)
+
+
+def test_tickets_of_the_loss_whose_clearing_failed_are_cleared_by_the_next_call(run):
+    """The workgroup that finds itself last writes the loss: with other than zeros to count from there may be none."""
+    run("""
+    def loss(ctx):
+        arr = (c_void_p * 1)(A)
+        return lib.adadim_layer_error_batch(ctx, 1, arr, 2, c_int64(512), c_int64(512), A, A, None, A)
+    ctx = context()
+    fake.fake_fail(b"fill_zero_f32", 2)                            # (the first clears the zeros behind the operands)
+    assert loss(ctx) == EHIP
+    for again in range(2):
+        fake.fake_reset()
+        assert loss(ctx) == OK, lib.adadim_last_error(ctx)
+        assert sum("fill_zero_f32" in c for c in names()) == (again == 0), names()
+    """)
