@@ -24,7 +24,10 @@ int adadim_fail(adadim_ctx* ctx, int code, const char* fmt, ...) {
 
 void* adadim_workspace(adadim_ctx* ctx, int slot, size_t bytes) {
     if (bytes == 0) bytes = 256;
-    if (ctx->ws_bytes[slot] >= bytes) return ctx->ws[slot];
+    if (ctx->ws_bytes[slot] >= bytes) {
+        if (ctx->capturing) ctx->ws_recorded[slot] = true;
+        return ctx->ws[slot];
+    }
     if (ctx->capturing) {
         adadim_fail(ctx, ADADIM_EINVAL,
                     "scratch slot %d would have to grow while a graph is being recorded: make the same call once "
@@ -32,8 +35,17 @@ void* adadim_workspace(adadim_ctx* ctx, int slot, size_t bytes) {
         return nullptr;
     }
     if (ctx->ws[slot]) {
-        // Earlier kernels on the stream may still read the old buffer.
-        if (hipStreamSynchronize(ctx->stream) != hipSuccess || hipFree(ctx->ws[slot]) != hipSuccess) {
+        if (ctx->ws_recorded[slot]) {
+            // A graph holds the old buffer's address and may be launched at any time: it stays.
+            adadim_retired* r = new (std::nothrow) adadim_retired{ctx->ws[slot], ctx->retired};
+            if (!r) {
+                adadim_fail(ctx, ADADIM_EINVAL, "scratch slot %d: out of host memory", slot);
+                return nullptr;
+            }
+            ctx->retired = r;
+            ctx->ws_recorded[slot] = false;
+        } else if (hipStreamSynchronize(ctx->stream) != hipSuccess || hipFree(ctx->ws[slot]) != hipSuccess) {
+            // (earlier kernels on the stream may still read the old buffer)
             adadim_fail(ctx, ADADIM_EHIP, "releasing scratch slot %d failed", slot);
             return nullptr;
         }
@@ -214,12 +226,17 @@ void adadim_destroy(adadim_ctx* ctx) {
         (void)hipStreamSynchronize(ctx->stream);
         (void)hipHostFree(ctx->host_best);
     }
-    bool any = false;
+    bool any = ctx->retired != nullptr;
     for (int i = 0; i < WS_COUNT; ++i) any = any || ctx->ws[i];
     if (any) {
         (void)hipStreamSynchronize(ctx->stream);
         for (int i = 0; i < WS_COUNT; ++i)
             if (ctx->ws[i]) (void)hipFree(ctx->ws[i]);
+        while (adadim_retired* r = ctx->retired) {
+            ctx->retired = r->next;
+            (void)hipFree(r->p);
+            delete r;
+        }
     }
     if (ctx->prof.start) {
         for (int i = 0; i < ctx->prof.n_events; ++i) {

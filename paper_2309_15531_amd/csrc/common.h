@@ -59,12 +59,20 @@ struct adadim_prof {
     char only[32];                   // when not empty: the one kernel that is bracketed
 };
 
+// Scratch that a recorded graph still points into, outgrown by a later call.
+struct adadim_retired {
+    void* p;
+    adadim_retired* next;
+};
+
 struct adadim_ctx {
     hipStream_t stream;
     char err[512];
     void* ws[WS_COUNT];
     size_t ws_bytes[WS_COUNT];
     bool ws_cleared[WS_COUNT];       // the slot's memory holds the zeros that its kernels count on (WS_ZERO all of it, others their counters)
+    bool ws_recorded[WS_COUNT];      // a graph has been recorded with the slot's memory
+    adadim_retired* retired;         // freed with the context
     // Gram launch plans already chosen, keyed by (token count, tile count, whether whole tiles may store): choosing
     // one simulates the launch's schedule (milliseconds of host time), and a model driver alternates between a few
     // input widths

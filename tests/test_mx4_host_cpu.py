@@ -123,3 +123,52 @@ def test_tickets_of_the_loss_whose_clearing_failed_are_cleared_by_the_next_call(
         assert loss(ctx) == OK, lib.adadim_last_error(ctx)
         assert sum("fill_zero_f32" in c for c in names()) == (again == 0), names()
     """)
+
+
+@pytest.mark.parametrize("small,large", [
+    ("matmul(ctx, 12, 96, 8192)", "matmul(ctx, 40, 1500, 8192)"),                                # counters and sums of shares
+    ("matmul(ctx, 700, 512, 333)", "matmul(ctx, 3000, 512, 333)"),                               # X copied
+    ("route(ctx, 700)", "route(ctx, 7000)"),                                                     # masks and counts of the chunks
+    ("gemv(ctx, 1024, 1024)", "gemv(ctx, 28672, 8192)")])
+def test_scratch_that_a_graph_was_recorded_with_outlives_the_calls_that_outgrow_it(run, small, large):
+    """A graph holds the addresses of the context's scratch.  A larger call makes the slot grow; the replay afterwards must find its memory."""
+    run(f"""
+    def route(ctx, tokens):
+        return lib.adadim_expert_route(ctx, A, 2, c_int64(tokens), c_int64(16), 16, 2, 1, A, A, A, A, A)
+    def memory(what):
+        return [c.split()[1] for c in calls() if c.split()[0] == what]
+    ctx = context()
+    assert {small} == OK, lib.adadim_last_error(ctx)
+    held = memory("have")
+    assert len(held) == 1, held
+    g = c_void_p()
+    assert lib.adadim_capture_begin(ctx) == OK
+    assert {small} == OK, lib.adadim_last_error(ctx)
+    assert lib.adadim_capture_end(ctx, byref(g)) == OK
+    fake.fake_reset()
+    assert {large} == OK, lib.adadim_last_error(ctx)
+    assert len(memory("have")) == 1 and memory("free") == [], calls()
+    assert lib.adadim_graph_launch(ctx, g) == OK
+    # the larger one was recorded by nobody: it goes when it is outgrown in turn, and all go with the context
+    assert {small} == OK and {large} == OK
+    assert len(memory("have")) == 1 and memory("free") == [], calls()
+    held += memory("have")
+    lib.adadim_graph_destroy(g)
+    lib.adadim_destroy(ctx)
+    assert sorted(memory("free")) == sorted(held), (calls(), held)
+    """)
+
+
+def test_scratch_that_no_graph_was_recorded_with_is_given_back(run):
+    run("""
+    ctx = context()
+    assert matmul(ctx, 12, 96, 8192) == OK and matmul(ctx, 40, 1500, 8192) == OK
+    assert [c.split()[0] for c in calls() if c.startswith(("have", "free"))] == ["have", "free", "have"], calls()
+    g = c_void_p()
+    assert lib.adadim_capture_begin(ctx) == OK                     # (a recording of something else)
+    assert gemv(ctx, 32, 4) != OK
+    assert lib.adadim_capture_end(ctx, byref(g)) == OK
+    fake.fake_reset()
+    assert matmul(ctx, 263, 3651, 6120) == OK
+    assert [c.split()[0] for c in calls() if c.startswith(("have", "free"))] == ["free", "have"], calls()
+    """)
