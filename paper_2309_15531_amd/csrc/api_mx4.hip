@@ -30,7 +30,7 @@ int adadim_mx4_quantize(adadim_ctx* ctx, const void* X, int x_type, int64_t rows
     if (!ctx) return ADADIM_ENULL;
     const char* me = "adadim_mx4_quantize";
     if (!is_float_type(x_type)) return adadim_fail(ctx, ADADIM_EINVAL, "%s: x_type must be F16, BF16 or F32, got %d", me, x_type);
-    if (rows < 0 || cols <= 0 || ldx < cols || rows > MOST_ROWS || cols > MOST_COLS || (rows + 3) / 4 * ((cols + 511) / 512) > INT32_MAX)
+    if (rows < 0 || cols <= 0 || ldx < cols || rows > MOST_ROWS || cols > MOST_COLS || !launchable((rows + 15) / 16 * ((cols + 511) / 512), 256))
         return adadim_fail(ctx, ADADIM_EINVAL, "%s: need rows >= 0, cols > 0, ldx >= cols in range (rows=%lld cols=%lld ldx=%lld)", me,
                            (long long)rows, (long long)cols, (long long)ldx);
     if (dW && dW_dtype != ADADIM_DW_F32 && dW_dtype != ADADIM_DW_F16 && dW_dtype != ADADIM_DW_F16_SCALED)
@@ -50,7 +50,7 @@ int adadim_mx4_dequantize(adadim_ctx* ctx, const uint8_t* codes, const uint8_t* 
     if (!ctx) return ADADIM_ENULL;
     const char* me = "adadim_mx4_dequantize";
     if (!is_float_type(y_type)) return adadim_fail(ctx, ADADIM_EINVAL, "%s: y_type must be F16, BF16 or F32, got %d", me, y_type);
-    if (rows < 0 || cols <= 0 || ldy < cols || rows > MOST_ROWS || cols > MOST_COLS || (rows + 3) / 4 * ((cols + 511) / 512) > INT32_MAX)
+    if (rows < 0 || cols <= 0 || ldy < cols || rows > MOST_ROWS || cols > MOST_COLS || !launchable((rows + 15) / 16 * ((cols + 511) / 512), 256))
         return adadim_fail(ctx, ADADIM_EINVAL, "%s: need rows >= 0, cols > 0, ldy >= cols in range (rows=%lld cols=%lld ldy=%lld)", me,
                            (long long)rows, (long long)cols, (long long)ldy);
     if (rows == 0) return ADADIM_OK;
@@ -110,10 +110,10 @@ int adadim_expert_route(adadim_ctx* ctx, const void* logits, int type, int64_t t
     if (!ctx) return ADADIM_ENULL;
     const char* me = "adadim_expert_route";
     if (!is_float_type(type)) return adadim_fail(ctx, ADADIM_EINVAL, "%s: type must be F16, BF16 or F32, got %d", me, type);
-    if (experts <= 0 || experts > 1024 || k <= 0 || k > 32 || k > experts || tokens < 0 || ldl < experts || tokens * k > INT32_MAX ||
-        tokens > MOST_ROWS || (renormalize != 0 && renormalize != 1))
+    if (experts <= 0 || experts > 1024 || k <= 0 || k > 32 || k > experts || tokens < 0 || ldl < experts || tokens > MOST_ROWS ||
+        tokens * k > INT32_MAX || !launchable((tokens + 63) / 64, 1024) || (renormalize != 0 && renormalize != 1))
         return adadim_fail(ctx, ADADIM_EINVAL,
-                           "%s: need 1..1024 experts, 1 <= k <= min(32, experts), ldl >= experts, tokens * k < 2^31, renormalize 0 or 1 "
+                           "%s: need 1..1024 experts, 1 <= k <= min(32, experts), ldl >= experts, tokens < 2^28, tokens * k < 2^31, renormalize 0 or 1 "
                            "(tokens=%lld ldl=%lld experts=%d k=%d renormalize=%d)",
                            me, (long long)tokens, (long long)ldl, experts, k, renormalize);
     if (!offsets || (tokens > 0 && (!logits || !chosen || !weights || !rows || !slots)))
@@ -131,7 +131,7 @@ int adadim_expert_combine(adadim_ctx* ctx, const void* Z, int z_type, int64_t n_
     if (!is_float_type(z_type) || !is_float_type(y_type))
         return adadim_fail(ctx, ADADIM_EINVAL, "%s: types must be F16, BF16 or F32, got %d and %d", me, z_type, y_type);
     if (n_rows < 0 || cols <= 0 || tokens < 0 || k <= 0 || k > 1024 || ldz < cols || ldy < cols || n_rows > MOST_ROWS || tokens > MOST_ROWS ||
-        cols > MOST_COLS || tokens * ((cols + 511) / 512) > INT32_MAX)
+        cols > MOST_COLS || !launchable(tokens * ((cols + 2047) / 2048), 256))
         return adadim_fail(ctx, ADADIM_EINVAL,
                            "%s: need n_rows, tokens >= 0, cols > 0, k in [1,1024], ldz, ldy >= cols in range (n_rows=%lld cols=%lld tokens=%lld "
                            "k=%d ldz=%lld ldy=%lld)",

@@ -159,6 +159,9 @@ struct PerDeviceOnce {
     }
 };
 
+// Whether a launch may have that many workgroups of `threads` along an axis: HIP takes less than 2^32 work items there.
+static inline bool launchable(int64_t workgroups, int threads) { return workgroups < (int64_t(1) << 32) / threads; }
+
 static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Launchers implemented in the .hip files.  All validate nothing: the API layer does.

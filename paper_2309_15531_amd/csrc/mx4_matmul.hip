@@ -343,7 +343,7 @@ inline int64_t most_row_tiles(const Product& a, int bm) {
 template <int BM, int BN, int WT, int WO>
 int launch_tiles(adadim_ctx* ctx, const Product& a) {
     const int64_t tiles = most_row_tiles(a, BM) * ((a.out + BN - 1) / BN);
-    if (tiles > INT32_MAX - 8) return adadim_fail(ctx, ADADIM_EINVAL, "mx4 product: more tiles than a launch has workgroups");
+    if (!launchable(tiles + 7, 64 * WT * WO)) return adadim_fail(ctx, ADADIM_EINVAL, "mx4 product: more tiles than a launch has workgroups");
     ProfScope prof(ctx, "mx4_tiles");
     hipLaunchKernelGGL((mx4_tiles<BM, BN, WT, WO>), dim3(static_cast<unsigned>((tiles + 7) / 8 * 8)), dim3(64 * WT * WO),
                        (Tiles<BM, BN, WT, WO>::LDS), ctx->stream, ProductArgs(a));
@@ -359,7 +359,7 @@ hipError_t raise_ring() {
 template <int XT, int BM, int BN, int WT, int WO, int NS>
 int launch_ring(adadim_ctx* ctx, const Product& a, int splits) {
     const int64_t tiles = most_row_tiles(a, BM) * ((a.out + BN - 1) / BN), grid = (tiles + 7) / 8 * 8;
-    if (tiles > INT32_MAX - 8) return adadim_fail(ctx, ADADIM_EINVAL, "mx4 product: more tiles than a launch has workgroups");
+    if (!launchable(tiles + 7, 64 * WT * WO)) return adadim_fail(ctx, ADADIM_EINVAL, "mx4 product: more tiles than a launch has workgroups");
     void* shared = nullptr;
     if (splits > 1) {
         const int rc = shares(ctx, size_t(splits) * size_t(grid) * BM * BN * 4, shared);
@@ -452,7 +452,7 @@ int launch_product(adadim_ctx* ctx, Product a) {
     const bool none = a.tokens == 0;
     if ((odd && p.form != Form::rows) || (far && (a.gather || !MX)) || none) {
         const int64_t to_pitch = MX ? pitch : pieces(a.in) * (2 * PIECE), blocks = (a.n_rows * to_pitch / 16 + 255) / 256;
-        if (blocks > INT32_MAX) return adadim_fail(ctx, ADADIM_EINVAL, "mx4 product: X too large to be copied");
+        if (!launchable(blocks, 256)) return adadim_fail(ctx, ADADIM_EINVAL, "mx4 product: X too large to be copied");
         const size_t codes = size_t(a.n_rows) * size_t(to_pitch);
         uint8_t* to = static_cast<uint8_t*>(adadim_workspace(ctx, WS_MX4_X, codes + (MX ? codes / 16 : 0)));
         if (!to) return ADADIM_EHIP;

@@ -172,3 +172,33 @@ def test_scratch_that_no_graph_was_recorded_with_is_given_back(run):
     assert matmul(ctx, 263, 3651, 6120) == OK
     assert [c.split()[0] for c in calls() if c.startswith(("have", "free"))] == ["free", "have"], calls()
     """)
+
+
+def test_no_launch_of_more_work_items_than_there_can_be(run):
+    """A launch takes less than 2^32 threads along an axis.  Calls that would need more are refused, those that just do not are made."""
+    run("""
+    def quantize(ctx, rows, cols):
+        return lib.adadim_mx4_quantize(ctx, A, 1, c_int64(rows), c_int64(cols), c_int64(cols), A, A, None, 0, None)
+    def dequantize(ctx, rows, cols):
+        return lib.adadim_mx4_dequantize(ctx, A, A, c_int64(rows), c_int64(cols), A, 1, c_int64(cols))
+    def route(ctx, tokens, experts):
+        return lib.adadim_expert_route(ctx, A, 2, c_int64(tokens), c_int64(experts), experts, 1, 1, A, A, A, A, A)
+    def combine(ctx, tokens, cols):
+        return lib.adadim_expert_combine(ctx, A, 1, c_int64(16), c_int64(cols), c_int64(cols), A, A, c_int64(tokens), 2, A, 1, c_int64(cols))
+    def product(ctx, x_type, rows, out, inn):
+        return lib.adadim_mx4_matmul(ctx, A, A, x_type, c_int64(rows), c_int64(inn), A, A, c_int64(out), c_int64(inn), A, 2, c_int64(out))
+    def most():
+        grids = [[int(v) for v in c.split()[2:5]] for c in calls() if c.startswith("launch")]
+        return max((x * threads for x, y, threads in grids), default=0)
+    ctx = context()
+    top = 1 << 32
+    edges = [(quantize, (1 << 28, 64), (1 << 28) - 16), (quantize, (1 << 20, 1 << 17), (1 << 20) - 16), (dequantize, (1 << 28, 512), (1 << 28) - 16),
+             (combine, (1 << 24, 2048), (1 << 24) - 1), (combine, (1 << 23, 2049), (1 << 23) - 1), (combine, (1 << 30, 8), None),
+             (route, (1 << 28, 4), None), (lambda c, n, i: product(c, 1, n, 64, i), (1 << 28, 1), None),
+             (lambda c, n, i: product(c, 3, n, i, 128), (1 << 30, 512), None), (lambda c, n, i: product(c, 1, n, i, 128), (1 << 30, 512), None)]
+    for call, (n, other), less in edges:
+        fake.fake_reset()
+        assert call(ctx, n, other) == EINVAL and not names(), (n, other, names(), most())
+        if less:
+            assert call(ctx, less, other) == OK and 0 < most() < top, (less, other, most(), lib.adadim_last_error(ctx))
+    """)
