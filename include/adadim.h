@@ -357,7 +357,7 @@ int adadim_gemv_ic_meta16(adadim_ctx* ctx, const uint32_t* packed, const uint16_
  * The last piece is filled up with codes 0 and scale bytes 127 (2^0), by whoever writes it: the products read whole pieces.
  * adadim_mx4_code_bytes / _scale_bytes give the sizes of the two arrays.
  * Rows up to 2^30, columns up to 2^24.  Sizes that would take a launch of 2^32 threads are refused with EINVAL: here and below, 2^24 tiles of
- * 16 x 512 values to or from mx4, 2^28 tokens to route, 2^24 runs of 2048 columns to combine, 2^35 and more outputs of a product.
+ * 16 x 512 values to or from mx4, 2^28 tokens to route, 2^24 runs of 2048 columns to combine, 2^23 or 2^24 tiles of a product.
  */
 #define ADADIM_TYPE_F16  0
 #define ADADIM_TYPE_BF16 1

@@ -3,8 +3,10 @@ import numpy as np
 import pytest
 import torch
 
+from mx4_group_forms import MX4_GROUP_FORMS
 from paper_2309_15531_amd import binding as B
-from test_gpu_mx4 import TYPES, mx4, rng, spread
+from test_gpu_mx4 import TYPES, check_route, mx4, rng, spread
+from test_gpu_mx4_forms import check, quantized, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -78,3 +80,82 @@ def test_a_recording_outlives_larger_calls(ctx):
         c.adadim_graph_destroy(graph)
     side.synchronize()
     c.close()
+
+
+# ------------------------------------------------------------------------------------------ loops that go round more than once
+@pytest.mark.parametrize("tokens,experts,k", [(16385, 8, 2), (40000, 6, 3), (2200, 1024, 2), (7000, 300, 4)])
+def test_route_of_more_chunks_than_workgroups_or_rounds(ctx, tokens, experts, k):
+    """Above 16384 tokens a workgroup places several chunks; with many experts the counts of the chunks are added up in several rounds.  Some
+    tokens have no expert, so that rows end in -1."""
+    l = rng(tokens, experts).standard_normal((tokens, experts))
+    l[5::97] = -np.inf
+    l[6::89, 1:] = -np.inf
+    check_route(ctx, l, k, True, torch.float32)
+
+
+@pytest.mark.parametrize("x", ["f16", "bf16", "mx4"])
+def test_tiles_of_more_experts_than_a_wave_has_lanes(ctx, x):
+    """Uneven groups, empty ones among them on both sides of every multiple of 64, rows in front of the first and behind the last."""
+    for (mx, experts, rows, out, inn), form in MX4_GROUP_FORMS.items():
+        if mx != (x == "mx4"):
+            continue
+        print((mx, experts, rows, out, inn), form, flush=True)
+        w = [quantized(ctx, randn(rows + e, out, inn) * 0.05) for e in range(experts)]
+        a = randn(out, 997, inn)
+        if mx:
+            X, xs, xv = quantized(ctx, a)
+        else:
+            X, xs = a.to(TYPES[x]), None
+            xv = X.float()
+        r = np.random.default_rng(rows + out)
+        share = r.random(experts) ** 3
+        share[[0, 62, 64, 65, 127, experts - 1]] = 0.0
+        share[[63, 66, 128]] = 2.0
+        lead, tail = 7, 11
+        sizes = np.floor(share / share.sum() * (rows - lead - tail)).astype(int)
+        offsets = (lead + np.concatenate([[0], np.cumsum(sizes)])).astype(np.int32)
+        named = r.integers(0, 997, rows).astype(np.int32)
+        full = torch.full((rows, out + 4), 9.0, device="cuda")
+        codes, scales = torch.stack([p[0] for p in w]), torch.stack([p[1] for p in w])
+        ctx.adadim_mx4_matmul_experts(X, codes, scales, torch.from_numpy(offsets).cuda(), full[:, :out], in_f=inn, x_scales=xs,
+                                      rows=torch.from_numpy(named).cuda())
+        at = torch.from_numpy(named).long().cuda()
+        for e in range(experts):
+            lo, hi = offsets[e], offsets[e + 1]
+            if hi > lo:
+                check(full[lo:hi, :out], xv[at[lo:hi]], w[e][2])
+        assert bool((full[:lead] == 9.0).all()) and bool((full[offsets[-1]:] == 9.0).all()) and bool((full[:, out:] == 9.0).all())
+
+
+# ------------------------------------------------------------------------------------------ products are exact
+FORM_SIZES = [1, 20, 40, 130, 700, 3000]                       # rows: few, and tiles of every height
+
+
+def every_weight():
+    """Codes and scales [255, 128]: row b has the scale byte b, its values all codes in turn."""
+    codes = torch.from_numpy(np.tile(np.arange(0x10, dtype=np.uint8).reshape(8, 2) @ np.array([1, 16], np.uint8), (253, 8)))
+    scales = torch.from_numpy(np.arange(253, dtype=np.uint8)[None, :, None].repeat(4, 2))
+    return codes.cuda(), scales.contiguous().cuda()
+
+
+@pytest.mark.parametrize("x", ["f16", "bf16", "mx4"])
+@pytest.mark.parametrize("rows", FORM_SIZES)
+@pytest.mark.parametrize("power", [10, -10])
+def test_a_product_of_one_term_is_exact(ctx, x, rows, power):
+    """One value of X that is not zero, a power of two: Y is the weight times it to the last bit, from the smallest weight that there is to the largest
+    that fp32 holds."""
+    codes, scales = every_weight()
+    w = torch.empty((253, 128), device="cuda")
+    ctx.adadim_mx4_dequantize(codes, scales, w)
+    keep = slice(0, 127) if power > 0 else slice(127, 253)     # products that fp32 holds as normal numbers
+    codes, scales, w = codes[keep].contiguous(), scales[:, keep].contiguous(), w[keep]
+    at = (torch.arange(rows, device="cuda") * 37) % 128
+    a = torch.zeros((rows, 128), device="cuda")
+    a[torch.arange(rows), at] = 2.0 ** power
+    X, xs = quantized(ctx, a)[:2] if x == "mx4" else (a.to(TYPES[x]), None)
+    Y = torch.empty((rows, len(w)), device="cuda")
+    ctx.adadim_mx4_matmul(X, codes, scales, Y, in_f=128, x_scales=xs)
+    want = w.double()[:, at].t() * 2.0 ** power
+    assert bool((want.abs()[want != 0] >= 2.0 ** -126).all())
+    off = Y.double() != want
+    assert not bool(off.any()), (off.nonzero()[:5].tolist(), Y[off][:5].tolist(), want[off][:5].tolist())

@@ -7,8 +7,10 @@ import textwrap
 
 import pytest
 
+from mx4_group_forms import MX4_GROUP_FORMS
 from paper_2309_15531_amd import binding as B
 from test_host_path_cpu import PREAMBLE
+from test_mx4_plan_cpu import plans  # noqa: F401  (the fixture)
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -202,3 +204,10 @@ def test_no_launch_of_more_work_items_than_there_can_be(run):
         if less:
             assert call(ctx, less, other) == OK and 0 < most() < top, (less, other, most(), lib.adadim_last_error(ctx))
     """)
+
+
+def test_the_forms_of_many_experts(plans):  # noqa: F811
+    sizes = [(rows, out, inn, experts, mx, 0) for mx, experts, rows, out, inn in MX4_GROUP_FORMS]
+    assert [p[0] for p in plans(sizes)] == list(MX4_GROUP_FORMS.values())
+    for mx in (False, True):
+        assert {f for k, f in MX4_GROUP_FORMS.items() if k[0] == mx} == {"ring32", "ring64", "ring64w", "mid", "big"}
