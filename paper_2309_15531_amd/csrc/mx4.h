@@ -89,14 +89,16 @@ __device__ __forceinline__ bf8v values8_bf16(uint32_t w, float scale) {
 // is 49152).  Whether one of a word's four scales lies outside, NaN among them: per byte 104 <= s <= 140.
 __device__ __forceinline__ bool beyond_f16(uint32_t byte) { return byte - 104u > 36u; }
 
-// x = hi + lo with both in bf16: 8 of fp16's 11 bits and the rest.  What is not finite goes whole into hi.
+// x = hi + lo with both in bf16: the first 8 of fp16's 11 bits and the rest.  Cut, not rounded: 65504 would become 65536, and its product
+// with a weight pass fp32's range where the exact one does not.  What is not finite goes whole into hi.
 __device__ __forceinline__ void split_f16(const half8v& x, bf8v& hi, bf8v& lo) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float f = static_cast<float>(x[i]);
-        hi[i] = static_cast<__bf16>(f);
-        const float rest = f - static_cast<float>(hi[i]);
-        lo[i] = static_cast<__bf16>(f - f == 0.0f ? rest : 0.0f);
+        const bool finite = f - f == 0.0f;
+        const float first = finite ? __uint_as_float(__float_as_uint(f) & 0xffff0000u) : f;
+        hi[i] = static_cast<__bf16>(first);
+        lo[i] = static_cast<__bf16>(finite ? f - first : 0.0f);
     }
 }
 

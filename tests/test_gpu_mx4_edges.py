@@ -159,3 +159,18 @@ def test_a_product_of_one_term_is_exact(ctx, x, rows, power):
     assert bool((want.abs()[want != 0] >= 2.0 ** -126).all())
     off = Y.double() != want
     assert not bool(off.any()), (off.nonzero()[:5].tolist(), Y[off][:5].tolist(), want[off][:5].tolist())
+
+
+@pytest.mark.parametrize("rows", FORM_SIZES)
+def test_the_largest_fp16_times_weights_beyond_fp16(ctx, rows):
+    """A number just below a power of two must not be taken for that power: 65504 x 2^112 is in fp32's range, 65536 x 2^112 is not."""
+    codes = torch.full((40, 64), 0x22, dtype=torch.uint8, device="cuda")           # ones
+    scales = torch.full((1, 40, 4), 112 + 127, dtype=torch.uint8, device="cuda")
+    X = torch.zeros((rows, 128), dtype=torch.float16, device="cuda")
+    X[:, 77] = 65504.0
+    X[rows // 2:, 77] = -65504.0
+    Y = torch.empty((rows, 40), device="cuda")
+    ctx.adadim_mx4_matmul(X, codes, scales, Y)
+    want = torch.full((rows, 40), 65504.0, dtype=torch.float64, device="cuda") * 2.0 ** 112
+    want[rows // 2:] *= -1.0
+    assert bool((Y.double() == want).all()), Y[:, 0]
