@@ -2,12 +2,41 @@
 
 Allocation and call order only; all arithmetic happens in libadadim.so, but for the activation between an expert's two products, which
 is the caller's.
+
+A call is part of the stream that is torch's current one, as torch's own operations are, whichever stream the context has.
 """
 from __future__ import annotations
 
 import torch
 
 from . import binding as B
+
+
+class _Ordered:
+    """The body's library calls and torch's own work in it, both on the context's stream.
+
+    Where torch's current stream is another one, the context's waits for it first and it waits for the context's behind the body: what came
+    before is done for the body, and what follows finds the body done.  So memory may go back to either stream's pool when the call
+    returns; what the caller gets is allocated before, from the current stream's."""
+
+    __slots__ = ("ctx", "here", "there", "switch")
+
+    def __init__(self, ctx):
+        self.ctx = ctx
+
+    def __enter__(self):
+        self.here = torch.cuda.current_stream()
+        self.there = None
+        if self.here.cuda_stream != self.ctx.stream:
+            self.there = torch.cuda.ExternalStream(self.ctx.stream) if self.ctx.stream else torch.cuda.default_stream()
+            self.there.wait_stream(self.here)
+            self.switch = torch.cuda.stream(self.there)
+            self.switch.__enter__()
+
+    def __exit__(self, *error):
+        if self.there is not None:
+            self.switch.__exit__(*error)
+            self.here.wait_stream(self.there)
 
 
 class Mx4Weight:
@@ -36,25 +65,29 @@ class Mx4Weight:
             raise ValueError(f"W: expected {(self.out_f, self.in_f)}, got {tuple(W.shape)}")
         codes, scales = self._part(expert)
         if hp is None:
-            self.ctx.adadim_mx4_quantize(W, codes, scales)
+            with _Ordered(self.ctx):
+                self.ctx.adadim_mx4_quantize(W, codes, scales)
             return None
-        dW = self.ctx.alloc_score(self.out_f, self.in_f, W.device)
         loss = torch.empty(1, dtype=torch.float32, device=W.device)
-        self.ctx.adadim_mx4_quantize(W, codes, scales, dW, B.DW_F16_SCALED, hp.colscale)
-        self.ctx.adadim_layer_error_prepared(dW, B.DW_F16_SCALED, hp.Hs, hp.hmeta, loss, shape=(self.out_f, self.in_f))
+        with _Ordered(self.ctx):
+            dW = self.ctx.alloc_score(self.out_f, self.in_f, W.device)
+            self.ctx.adadim_mx4_quantize(W, codes, scales, dW, B.DW_F16_SCALED, hp.colscale)
+            self.ctx.adadim_layer_error_prepared(dW, B.DW_F16_SCALED, hp.Hs, hp.hmeta, loss, shape=(self.out_f, self.in_f))
         return loss
 
     def values(self, expert: int | None = None, dtype=torch.float32):
         """The stored weight as [out, in] of `dtype`."""
         Y = torch.empty((self.out_f, self.in_f), dtype=dtype, device=self.codes.device)
-        self.ctx.adadim_mx4_dequantize(*self._part(expert), Y)
+        with _Ordered(self.ctx):
+            self.ctx.adadim_mx4_dequantize(*self._part(expert), Y)
         return Y
 
 
 def quantize_rows(ctx: B.Context, X):
     """(codes, scales) of the rows of X, as a product's left operand."""
     codes, scales = (torch.empty(n, dtype=torch.uint8, device=X.device) for n in B.mx4_shapes(*X.shape))
-    ctx.adadim_mx4_quantize(X, codes, scales)
+    with _Ordered(ctx):
+        ctx.adadim_mx4_quantize(X, codes, scales)
     return codes, scales
 
 
@@ -73,11 +106,12 @@ class Mx4Linear:
         w = self.weight
         if Y is None:
             Y = torch.empty((X.shape[0], w.out_f), dtype=X.dtype, device=X.device)
-        if self.mx4_inputs and X.shape[0] >= self.mx4_inputs:
-            codes, scales = quantize_rows(w.ctx, X)
-            w.ctx.adadim_mx4_matmul(codes, w.codes, w.scales, Y, in_f=w.in_f, x_scales=scales)
-        else:
-            w.ctx.adadim_mx4_matmul(X, w.codes, w.scales, Y, in_f=w.in_f)
+        with _Ordered(w.ctx):
+            if self.mx4_inputs and X.shape[0] >= self.mx4_inputs:
+                codes, scales = quantize_rows(w.ctx, X)
+                w.ctx.adadim_mx4_matmul(codes, w.codes, w.scales, Y, in_f=w.in_f, x_scales=scales)
+            else:
+                w.ctx.adadim_mx4_matmul(X, w.codes, w.scales, Y, in_f=w.in_f)
         return Y
 
 
@@ -109,14 +143,15 @@ class Mx4Experts:
     def __call__(self, X, logits, Y=None):
         """X [tokens, in] fp16 or bf16, logits [tokens, experts] (-infinity: an expert this token must not have)."""
         tokens, k, dev = X.shape[0], self.k, X.device
-        chosen, slots = (torch.empty((tokens, k), dtype=torch.int32, device=dev) for _ in range(2))
-        weights = torch.empty((tokens, k), dtype=torch.float32, device=dev)
-        offsets = torch.empty(self.up.experts + 1, dtype=torch.int32, device=dev)
-        rows = torch.empty(tokens * k, dtype=torch.int32, device=dev)
-        self.ctx.adadim_expert_route(logits, chosen, weights, offsets, rows, slots, renormalize=self.renormalize)
-        h = self._product(X, self.up, offsets, tokens * k, rows)
-        z = self._product(self.activation(h), self.down, offsets, tokens * k)
         if Y is None:
             Y = torch.empty((tokens, self.down.out_f), dtype=X.dtype, device=dev)
-        self.ctx.adadim_expert_combine(z, slots, weights, Y)
+        with _Ordered(self.ctx):
+            chosen, slots = (torch.empty((tokens, k), dtype=torch.int32, device=dev) for _ in range(2))
+            weights = torch.empty((tokens, k), dtype=torch.float32, device=dev)
+            offsets = torch.empty(self.up.experts + 1, dtype=torch.int32, device=dev)
+            rows = torch.empty(tokens * k, dtype=torch.int32, device=dev)
+            self.ctx.adadim_expert_route(logits, chosen, weights, offsets, rows, slots, renormalize=self.renormalize)
+            h = self._product(X, self.up, offsets, tokens * k, rows)
+            z = self._product(self.activation(h), self.down, offsets, tokens * k)
+            self.ctx.adadim_expert_combine(z, slots, weights, Y)
         return Y
