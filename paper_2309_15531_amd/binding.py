@@ -249,6 +249,8 @@ def _matrix(t, what: str):
 class Context:
     """One adadim_ctx bound to a HIP stream (default: torch's current stream)."""
 
+    recording = None                          # while a graph is recorded: what has to live as long as the graph
+
     def __init__(self, stream: int | None = None):
         self._lib = load_library()
         if stream is None:
@@ -260,6 +262,7 @@ class Context:
         if rc != OK:
             raise AdaDimError(rc, self._lib.adadim_last_error(None).decode())
         self._h = h
+        self._graphs = {}                     # graph -> what lives as long as it
 
     def close(self):
         if getattr(self, "_h", None):
@@ -414,11 +417,15 @@ class Context:
 
     def adadim_capture_begin(self):
         self._check(self._lib.adadim_capture_begin(self._h))
+        self.recording = []
 
     def adadim_capture_end(self):
         """Returns the graph handle (an int); free it with adadim_graph_destroy."""
         g = c_void_p()
+        kept, self.recording = self.recording, None
         self._check(self._lib.adadim_capture_end(self._h, byref(g)))
+        if kept:
+            self._graphs[g.value] = kept
         return g.value
 
     def adadim_graph_launch(self, graph: int):
@@ -427,6 +434,7 @@ class Context:
     def adadim_graph_destroy(self, graph):
         if graph:
             self._lib.adadim_graph_destroy(c_void_p(graph))
+            self._graphs.pop(graph, None)
 
     def adadim_gptq_prepare(self, H, perm, dead, U, percdamp: float = 0.01, act_order: bool = True):
         self._check(self._lib.adadim_gptq_prepare(self._h, _ptr(H), H.shape[0], c_float(percdamp), 1 if act_order else 0,

@@ -3,7 +3,9 @@
 Allocation and call order only; all arithmetic happens in libadadim.so, but for the activation between an expert's two products, which
 is the caller's.
 
-A call is part of the stream that is torch's current one, as torch's own operations are, whichever stream the context has.
+A call is part of the stream that is torch's current one, as torch's own operations are, whichever stream the context has.  While the context
+records a graph its stream has to be the current one; what the calls allocate then, the activation's tensors among it, stays until the graph is
+destroyed, and the results of the recorded calls with it.
 """
 from __future__ import annotations
 
@@ -17,7 +19,8 @@ class _Ordered:
 
     Where torch's current stream is another one, the context's waits for it first and it waits for the context's behind the body: what came
     before is done for the body, and what follows finds the body done.  So memory may go back to either stream's pool when the call
-    returns; what the caller gets is allocated before, from the current stream's."""
+    returns; what the caller gets is allocated before, from the current stream's.  While a graph is recorded the body's memory is the
+    recording's (a replay writes to the same addresses, whenever it comes)."""
 
     __slots__ = ("ctx", "here", "there", "switch")
 
@@ -25,18 +28,40 @@ class _Ordered:
         self.ctx = ctx
 
     def __enter__(self):
-        self.here = torch.cuda.current_stream()
-        self.there = None
-        if self.here.cuda_stream != self.ctx.stream:
-            self.there = torch.cuda.ExternalStream(self.ctx.stream) if self.ctx.stream else torch.cuda.default_stream()
-            self.there.wait_stream(self.here)
+        ctx = self.ctx
+        here = torch.cuda.current_stream()
+        self.there = self.switch = None
+        if here.cuda_stream != ctx.stream:
+            if ctx.recording is not None:
+                raise ValueError("a graph is being recorded: the context's stream has to be torch's current stream")
+            self.here, self.there = here, torch.cuda.ExternalStream(ctx.stream) if ctx.stream else torch.cuda.default_stream()
+            self.there.wait_stream(here)
             self.switch = torch.cuda.stream(self.there)
+        elif ctx.recording is not None:
+            self.switch = torch.cuda.use_mem_pool(_recordings_pool(ctx))
+        if self.switch is not None:
             self.switch.__enter__()
 
     def __exit__(self, *error):
-        if self.there is not None:
+        if self.switch is not None:
             self.switch.__exit__(*error)
+        if self.there is not None:
             self.here.wait_stream(self.there)
+
+
+def _recordings_pool(ctx):
+    """The memory that the graph being recorded has to itself."""
+    if not ctx.recording:
+        ctx.recording.append(torch.cuda.MemPool())
+    return ctx.recording[0]
+
+
+def _output(ctx, shape, dtype, device):
+    """What the caller gets from a call."""
+    if ctx.recording is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.use_mem_pool(_recordings_pool(ctx)):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 class Mx4Weight:
@@ -68,7 +93,7 @@ class Mx4Weight:
             with _Ordered(self.ctx):
                 self.ctx.adadim_mx4_quantize(W, codes, scales)
             return None
-        loss = torch.empty(1, dtype=torch.float32, device=W.device)
+        loss = _output(self.ctx, (1,), torch.float32, W.device)
         with _Ordered(self.ctx):
             dW = self.ctx.alloc_score(self.out_f, self.in_f, W.device)
             self.ctx.adadim_mx4_quantize(W, codes, scales, dW, B.DW_F16_SCALED, hp.colscale)
@@ -77,7 +102,7 @@ class Mx4Weight:
 
     def values(self, expert: int | None = None, dtype=torch.float32):
         """The stored weight as [out, in] of `dtype`."""
-        Y = torch.empty((self.out_f, self.in_f), dtype=dtype, device=self.codes.device)
+        Y = _output(self.ctx, (self.out_f, self.in_f), dtype, self.codes.device)
         with _Ordered(self.ctx):
             self.ctx.adadim_mx4_dequantize(*self._part(expert), Y)
         return Y
@@ -85,9 +110,16 @@ class Mx4Weight:
 
 def quantize_rows(ctx: B.Context, X):
     """(codes, scales) of the rows of X, as a product's left operand."""
-    codes, scales = (torch.empty(n, dtype=torch.uint8, device=X.device) for n in B.mx4_shapes(*X.shape))
+    codes, scales = (_output(ctx, n, torch.uint8, X.device) for n in B.mx4_shapes(*X.shape))
     with _Ordered(ctx):
         ctx.adadim_mx4_quantize(X, codes, scales)
+    return codes, scales
+
+
+def _quantized(ctx, X):
+    """The same where the call is ordered already."""
+    codes, scales = (torch.empty(n, dtype=torch.uint8, device=X.device) for n in B.mx4_shapes(*X.shape))
+    ctx.adadim_mx4_quantize(X, codes, scales)
     return codes, scales
 
 
@@ -105,10 +137,10 @@ class Mx4Linear:
     def __call__(self, X, Y=None):
         w = self.weight
         if Y is None:
-            Y = torch.empty((X.shape[0], w.out_f), dtype=X.dtype, device=X.device)
+            Y = _output(w.ctx, (X.shape[0], w.out_f), X.dtype, X.device)
         with _Ordered(w.ctx):
             if self.mx4_inputs and X.shape[0] >= self.mx4_inputs:
-                codes, scales = quantize_rows(w.ctx, X)
+                codes, scales = _quantized(w.ctx, X)
                 w.ctx.adadim_mx4_matmul(codes, w.codes, w.scales, Y, in_f=w.in_f, x_scales=scales)
             else:
                 w.ctx.adadim_mx4_matmul(X, w.codes, w.scales, Y, in_f=w.in_f)
@@ -121,7 +153,7 @@ class Mx4Experts:
     activation takes the rows [rows, up.out] to [rows, down.in] (fp16 or bf16); it may see rows that no expert has written where the
     router's mask leaves a token fewer than k experts: nothing reads them afterwards.  mx4_inputs as in Mx4Linear, by the rows
     of each product.  The host learns neither the choices nor how many rows an expert has: nothing here waits for the device, and
-    with the activation a layer can be recorded as a graph."""
+    with the activation a layer can be recorded as a graph (adadim_capture_begin; make the same call once before)."""
 
     def __init__(self, up: Mx4Weight, down: Mx4Weight, k: int, activation, renormalize: bool = True, mx4_inputs: int = 0):
         if up.experts != down.experts or not up.experts or up.in_f != down.out_f:
@@ -134,7 +166,7 @@ class Mx4Experts:
     def _product(self, X, weight, offsets, n_rows, rows=None):
         Y = torch.empty((n_rows, weight.out_f), dtype=X.dtype, device=X.device)
         if self.mx4_inputs and n_rows >= self.mx4_inputs:
-            codes, scales = quantize_rows(self.ctx, X)
+            codes, scales = _quantized(self.ctx, X)
             self.ctx.adadim_mx4_matmul_experts(codes, weight.codes, weight.scales, offsets, Y, in_f=weight.in_f, x_scales=scales, rows=rows)
         else:
             self.ctx.adadim_mx4_matmul_experts(X, weight.codes, weight.scales, offsets, Y, in_f=weight.in_f, rows=rows)
@@ -144,7 +176,7 @@ class Mx4Experts:
         """X [tokens, in] fp16 or bf16, logits [tokens, experts] (-infinity: an expert this token must not have)."""
         tokens, k, dev = X.shape[0], self.k, X.device
         if Y is None:
-            Y = torch.empty((tokens, self.down.out_f), dtype=X.dtype, device=dev)
+            Y = _output(self.ctx, (tokens, self.down.out_f), X.dtype, dev)
         with _Ordered(self.ctx):
             chosen, slots = (torch.empty((tokens, k), dtype=torch.int32, device=dev) for _ in range(2))
             weights = torch.empty((tokens, k), dtype=torch.float32, device=dev)

@@ -84,3 +84,63 @@ def test_layers_take_part_in_the_current_stream(tokens):
     own.synchronize()
     ctx.close()
     plain.close()
+
+
+@pytest.mark.parametrize("tokens", [1, 64, 300])
+@pytest.mark.parametrize("least", [0, 1])
+def test_recorded_layers_between_other_work(tokens, least):
+    """Two layers recorded as one graph; everything that the recording handed out is let go of but the result, the allocator is emptied and
+    memory filled with NaN.  Every replay gives what the eager calls give on the same inputs, and nobody else's memory is written."""
+    own = torch.cuda.Stream()
+    with torch.cuda.stream(own):
+        ctx = B.Context()
+        made = layers(ctx)
+        store(*made, [randn(1, 512, HIDDEN) * 0.05, randn(2, EXPERTS, INNER, HIDDEN) * 0.05, randn(3, EXPERTS, HIDDEN, INNER) * 0.05])
+        one, up, down = made
+        linear, experts = mx4.Mx4Linear(one, mx4_inputs=least), mx4.Mx4Experts(up, down, 2, silu, mx4_inputs=least)
+        x, logits = torch.empty((tokens, HIDDEN), dtype=torch.bfloat16, device="cuda"), torch.empty((tokens, EXPERTS), device="cuda")
+
+        def fill(seed):
+            x.copy_(randn(seed, tokens, HIDDEN))
+            logits.copy_(randn(seed + 50, tokens, EXPERTS))
+
+        def layer():
+            return linear(experts(x, logits) + x)             # (the sum is torch's own: recorded, and its memory the caller's)
+
+        fill(0)
+        layer()
+        sums = torch.empty_like(x)
+        ctx.adadim_capture_begin()
+        try:
+            first = experts(x, logits)
+            torch.add(first, x, out=sums)
+            y = linear(sums)
+            del first
+        finally:
+            graph = ctx.adadim_capture_end()
+        torch.cuda.empty_cache()
+        shapes = [(tokens, HIDDEN), (2 * tokens, INNER), (2 * tokens, HIDDEN), (tokens, 512), (2 * tokens,), (1 << 20,)]
+        for seed in range(1, 6):
+            fill(seed)
+            junk = [torch.full(s, float("nan"), dtype=t, device="cuda") for s in shapes for t in (torch.bfloat16, torch.float32)]
+            y.zero_()
+            for _ in range(seed % 2 + 1):
+                ctx.adadim_graph_launch(graph)
+            got = y.clone()
+            assert all(bool(j.isnan().all()) for j in junk), seed
+            want = layer()
+            assert torch.equal(got, want), seed
+            own.synchronize()
+            del junk
+        ctx.adadim_graph_destroy(graph)
+        assert torch.equal(y, want), "a result outlives the graph for whoever holds it"
+    own.synchronize()
+    with pytest.raises(ValueError, match="stream"):
+        with torch.cuda.stream(own):
+            ctx.adadim_capture_begin()
+        try:
+            linear(x)
+        finally:
+            with torch.cuda.stream(own):
+                ctx.adadim_graph_destroy(ctx.adadim_capture_end())
+    ctx.close()

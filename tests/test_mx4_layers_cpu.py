@@ -114,3 +114,131 @@ def test_a_call_that_raises_leaves_the_streams_in_order(monkeypatch, what):
     with pytest.raises(ValueError, match="no"):
         call()
     assert m.log[-1] == ("wait", 3, 7) and len(m.current) == 1
+
+
+# ------------------------------------------------------------------------------------------ while a graph is recorded
+class Library:
+    """Stands in for the shared library: every call succeeds, a recording yields the next handle."""
+
+    def __init__(self):
+        self.graphs = 0
+
+    def __getattr__(self, name):
+        return lambda *a: 0
+
+    def adadim_capture_end(self, h, out):
+        self.graphs += 1
+        out._obj.value = 100 + self.graphs
+        return 0
+
+
+class Pool:
+    live = []
+
+    def __init__(self):
+        Pool.live.append(self)
+
+
+def recorder(monkeypatch, own, current):
+    """A context with its own bookkeeping of recordings, and the pool that torch allocates from at each call."""
+    from paper_2309_15531_amd import binding as B
+    m = Machine(monkeypatch, own, current)
+    pools = [None]
+
+    @contextlib.contextmanager
+    def use(pool):
+        assert pools[-1] is None, "pools do not nest"
+        pools.append(pool)
+        try:
+            yield
+        finally:
+            pools.pop()
+
+    class Recorder(B.Context):
+        def __init__(self):
+            self._lib, self._h, self.stream = Library(), None, own
+            self._graphs = {}
+
+        alloc_score = lambda self, rows, cols, device: torch.empty(rows * cols, dtype=torch.float16)
+
+    for name in dir(B.Context):
+        if name.startswith(("adadim_mx4", "adadim_expert", "adadim_layer")):
+            setattr(Recorder, name, lambda self, *a, _n=name, **k: m.log.append((_n, m.current[-1].cuda_stream)))
+    empty = mx4.torch.empty
+
+    def allocate(*size, **kw):
+        m.log.append(("from", pools[-1]))
+        return empty(*size, **kw)
+    Pool.live = []
+    monkeypatch.setattr(torch.cuda, "MemPool", Pool)
+    monkeypatch.setattr(torch.cuda, "use_mem_pool", use)
+    monkeypatch.setattr(mx4.torch, "empty", allocate)
+    c = Recorder()
+    c.log, c.activation = m.log, lambda h: torch.empty(h.shape[0], 64)
+    return c
+
+
+@pytest.mark.parametrize("what", NAMES)
+def test_what_a_recorded_call_allocates_lives_as_long_as_the_graph(monkeypatch, what):
+    """A replay writes to the addresses of the recording: they belong to a pool that nothing else takes memory from."""
+    c = recorder(monkeypatch, 7, 7)
+    todo = calls(c)
+    c.adadim_capture_begin()
+    todo[what]()
+    todo[what]()
+    graph = c.adadim_capture_end()
+    taken = [e[1] for e in c.log if e[0] == "from"]
+    if taken:
+        assert len(Pool.live) == 1 and all(p is Pool.live[0] for p in taken), "one pool for the whole recording, and no other memory"
+        assert c._graphs[graph] == [Pool.live[0]]
+    else:
+        assert what == "store"
+    del c.log[:]
+    todo[what]()
+    assert all(e[1] is None for e in c.log if e[0] == "from"), "behind the recording memory is ordinary again"
+    c.adadim_graph_destroy(graph)
+    assert not c._graphs
+
+
+def test_recordings_keep_what_is_theirs(monkeypatch):
+    c = recorder(monkeypatch, 7, 7)
+    todo = calls(c)
+    graphs = []
+    for _ in range(2):
+        c.adadim_capture_begin()
+        todo["experts mx4"]()
+        graphs.append(c.adadim_capture_end())
+    c.adadim_capture_begin()
+    graphs.append(c.adadim_capture_end())
+    assert [c._graphs.get(g) for g in graphs] == [[Pool.live[0]], [Pool.live[1]], None]
+    c.adadim_graph_destroy(graphs[0])
+    c.adadim_graph_destroy(None)
+    assert list(c._graphs) == [graphs[1]]
+
+
+def test_a_recording_that_fails_keeps_nothing(monkeypatch):
+    from paper_2309_15531_amd import binding as B
+    c = recorder(monkeypatch, 7, 7)
+    todo = calls(c)
+    c.adadim_capture_begin()
+    todo["linear mx4"]()
+    c._lib.adadim_capture_end = lambda h, out: B.EHIP
+    c.last_error = lambda: "no"
+    with pytest.raises(B.AdaDimError):
+        c.adadim_capture_end()
+    assert c.recording is None and not c._graphs
+    c._lib.adadim_capture_begin = lambda h: B.EINVAL
+    with pytest.raises(B.AdaDimError):
+        c.adadim_capture_begin()
+    assert c.recording is None
+
+
+@pytest.mark.parametrize("what", NAMES)
+def test_from_another_stream_nothing_is_recorded(monkeypatch, what):
+    """Torch's own work there would not be part of the recording, and waiting for it would break it."""
+    c = recorder(monkeypatch, 7, 3)
+    todo = calls(c)
+    c.adadim_capture_begin()
+    with pytest.raises(ValueError, match="stream"):
+        todo[what]()
+    assert not any(e[0] == "wait" or e[0].startswith("adadim_") for e in c.log)
