@@ -39,6 +39,7 @@ class Machine:
             return empty(*size, **kw)
 
         monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: self.current[-1])
+        monkeypatch.setattr(mx4, "_raw_stream", lambda device: self.current[-1].cuda_stream, raising=False)
         monkeypatch.setattr(torch.cuda, "stream", stream)
         monkeypatch.setattr(torch.cuda, "ExternalStream", lambda n, *a: Stream(self.log, n))
         monkeypatch.setattr(torch.cuda, "default_stream", lambda *a: Stream(self.log, 0))
@@ -242,3 +243,14 @@ def test_from_another_stream_nothing_is_recorded(monkeypatch, what):
     with pytest.raises(ValueError, match="stream"):
         todo[what]()
     assert not any(e[0] == "wait" or e[0].startswith("adadim_") for e in c.log)
+
+
+def test_host_tensors_are_refused_by_name():
+    from paper_2309_15531_amd import binding as B
+    ctx = B.Context(stream=0)
+    one = mx4.Mx4Weight(ctx, 64, 32, device="cpu")
+    for call in (lambda: mx4.Mx4Linear(one)(torch.zeros(5, 32, dtype=torch.bfloat16)), lambda: one.store(torch.zeros(64, 32)),
+                 lambda: mx4.quantize_rows(ctx, torch.zeros(5, 32)), lambda: one.values()):
+        with pytest.raises(TypeError, match="device tensor"):
+            call()
+    ctx.close()
