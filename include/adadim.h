@@ -436,8 +436,8 @@ int adadim_expert_combine(adadim_ctx* ctx, const void* Z, int z_type, int64_t n_
  * one the gaps between them are a tenth of the step on a 4096 x 4096 layer, replayed as a graph they close.
  *   adadim_capture_begin  starts recording on the context's stream, which must not be the default
  *           stream (EINVAL).  Calls made on the context until adadim_capture_end are recorded, not run.
- *           While recording, a call that would have to grow the context's scratch fails with EINVAL (make the
- *           same calls once beforehand), adadim_select takes no host output, adadim_profile records nothing,
+ *           While recording, a call that would have to grow the context's scratch fails (EHIP; the text names the
+ *           scratch: make the same calls once beforehand), adadim_select takes no host output, adadim_profile records nothing,
  *           and the caller must not synchronise the stream or the device.
  *   adadim_capture_end    stops recording and returns the instantiated graph (a hipGraphExec_t as void*).  The
  *           graph holds the pointers and sizes of the recorded calls: the buffers must stay where they are,

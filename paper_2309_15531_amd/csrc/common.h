@@ -37,8 +37,8 @@ enum {
     WS_GPTQ_V,          // int32 position of each original channel in the visiting order
     WS_PROBE,           // output of the matrix-core rate probe
     WS_MX4_X,           // rows of X copied to where 16-byte transfers can take them
-    WS_MX4_PART,        // counters of the few-row products' output tiles, then their partial outputs
-    WS_ROUTE,           // the router's masks of tokens per expert and the places behind them
+    WS_MX4_PART,        // counters of the output tiles whose contraction is shared, then their partial sums
+    WS_ROUTE,           // the router's masks of tokens per chunk and expert, then their counts
     WS_COUNT
 };
 

@@ -86,7 +86,7 @@ __device__ __forceinline__ bf8v values8_bf16(uint32_t w, float scale) {
 }
 
 // fp16 holds the values of a block exactly for scales 2^-23 (half of it is fp16's smallest subnormal) to 2^13 (6 times it
-// is 49152).  Whether one of a word's four scales lies outside, NaN among them: per byte 104 <= s <= 140.
+// is 49152).  Whether a scale byte lies outside 104 .. 140, as NaN's does.
 __device__ __forceinline__ bool beyond_f16(uint32_t byte) { return byte - 104u > 36u; }
 
 // x = hi + lo with both in bf16: the first 8 of fp16's 11 bits and the rest.  Cut, not rounded: 65504 would become 65536, and its product

@@ -24,9 +24,10 @@ constexpr int XF16 = ADADIM_TYPE_F16, XBF16 = ADADIM_TYPE_BF16, XMX4 = ADADIM_TY
 // does not exist: it costs no access and reads as zeros.
 //
 // Eight waves, so that a wave has few pieces one after the other (4 at 4096 deep); NT by the estimates of mx4_plan.h: more outputs of a
-// workgroup read X less often, fewer give more workgroups.  With weights that come from memory: 1 token, 28672 -> 8192, mx4 X 24.6 us
-// (5.1 TB/s), 8192 -> 28672 fp16 30 us (4.1 TB/s), 4096 -> 11008 8.2 us (2.9 TB/s: a launch's start is 3 us of it); 16 tokens x 2 of 8
-// experts, 4096 -> 11008 fp16 45 us (4.2 TB/s).  Deeper unrolling, a second set of registers for the next piece, and X turned in LDS gained
+// workgroup read X less often, fewer give more workgroups.  With weights that come from memory: 1 token, 28672 -> 8192, mx4 X 24.6 to
+// 28.7 us (4.4 to 5.1 TB/s), 8192 -> 28672 fp16 30.5 us (4.1 TB/s), 4096 -> 11008 8.2 to 9.0 us (2.7 to 2.9 TB/s: a launch's start is 3 us of it); 16
+// tokens x 2 of 8 experts, 4096 -> 11008 fp16 45 us (4.2 TB/s).  Where there are more rows every workgroup draws all of X through the L2: 16 tokens,
+// 4096 -> 11008, 11.8 us.  Deeper unrolling, a second set of registers for the next piece, and X turned in LDS gained
 // nothing.
 constexpr int RW_WAVES = 8;
 constexpr uint32_t NO_ROW = 0x80000000u;          // an offset that no X has (the host copies X where it is larger)

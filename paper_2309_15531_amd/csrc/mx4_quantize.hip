@@ -10,7 +10,9 @@
 // holds 8 consecutive values, so a wave's load is one contiguous KB (two for fp32), a block lives in a quad (its amax meets by
 // DPP), a piece in a row of 16 lanes, and codes leave as 256 contiguous bytes.  The scale words of the tile are
 // collected in LDS and leave as runs along the rows, the way they are stored.
-// 28672 x 8192 fp16: 126 us there (4.7 TB/s of 5.06 that a large copy reaches), 92 us back; 16 x 4096 2.5 and 2.3 us.
+// 28672 x 8192 fp16: 102 us there, one call behind the other (5.8 TB/s; a large copy reaches 5.06, with half of its bytes written), 126 us there and
+// 92 us back in turn; 16 x 4096 2.5 and 2.3 us.  With dW: 183 us for F16, 294 for F32 (5.8, 5.2 TB/s); 486 for F16_SCALED (2.2 TB/s), whose
+// layout takes 64 bytes of a row at a time, rows apart from wave to wave.
 #include "mx4.h"
 
 namespace {

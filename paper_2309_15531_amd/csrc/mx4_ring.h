@@ -17,11 +17,12 @@ using namespace mx4;
 // The lane (row r, half h) of instruction number j of a stage takes, of mx4 X, chunk j + 2 h (so that its scale is byte j of the word
 // shifted by 16 h) and, of 16-bit X, values 64 h + 8 j .. + 7.
 //
-// 16-bit X: bound by the matrix cores at the clock that the power limit leaves (2048 x 11008 -> 4096 fp16: pipes busy 63 % of the time at
-// 1.8 GHz).  128 x 256: 8192 x 8192 x 8192 bf16 848 us (1.30 PFLOP/s), fp16 886 us, 2048 x 11008 -> 4096 fp16 150 us (1.23 PFLOP/s); 256 x 256 in
-// two stages took 1.0 to 1.9 times as long, 128 x 128 through the same ring 1.2 to 1.26 times at these sizes.
+// 16-bit X: bound by the matrix cores at the clock that the power limit leaves (2048 x 11008 -> 4096 fp16: pipes busy 62 % of the time at
+// 1.8 GHz).  128 x 256, 8192 x 8192 x 8192: bf16 848 to 889 us, fp16 886 to 921 us (1.24 to 1.30 and 1.19 to 1.24 PFLOP/s); 2048 x 11008 -> 4096
+// fp16 148 to 157 us among other passes (1.17 to 1.25 PFLOP/s), 170 to 176 each by itself under a profiler; 256 x 256 in two stages
+// took 1.0 to 1.9 times as long, 128 x 128 through the same ring 1.2 to 1.26 times at these sizes.
 // mx4 X: for tiles too small for the two-stage kernel; 256 x 256 through the ring, in rows of 64 bytes a stage, took 298 us for 8192 x 8192 x 8192 where
-// two stages of 128 bytes a row take 248.
+// two stages of 128 bytes a row take 248 (both with one set of operands).
 // NS: of the small tiles, as many slots as leave two to four workgroups to a compute unit's 160 KB; of the large ones, what fits.
 template <int XT, int BM, int BN, int WT, int WO, int NS>
 struct Ring {

@@ -158,8 +158,9 @@ __device__ __forceinline__ void store_tile(const Product& a, const float16v (&ac
 // works through the second.  Two stages of LDS: one is computed while the other arrives.
 //
 // Bound by the matrix cores at the clock that the power limit leaves, and by what a tile does outside its loop (its first stage and its output: 6 us
-// of 55 at 8192 deep).  256 x 256: 8192 x 8192 x 8192 248 us (4.43 PFLOP/s; instructions on registers alone reach 6.4 with such operands),
-// 8192 x 8192 -> 28672 868 to 903 us, 4096 tokens x 2 of 16 experts, 5120 -> 4096, 139 to 152 us.  128 x 128: 2048 x 4096 -> 4096 24.6 us.  Between them, 128 x 256
+// of 55 at 8192 deep).  256 x 256: 8192 x 8192 x 8192 248 us with one set of operands, 263 to 285 with several in turn (4.43 and 3.9 to 4.2 PFLOP/s;
+// instructions on registers alone reach 6.4 with such operands), 8192 x 8192 -> 28672 868 to 911 us, 4096 tokens x 2 of 16 experts, 5120 -> 4096, 139 to
+// 156 us.  128 x 128: 2048 x 4096 -> 4096 24.6 us.  Between them, 128 x 256
 // and 256 x 128 by four waves took 1.2 to 1.4 times 256 x 256: LDS gives them too few operands.  Scales read from memory by each wave took
 // 3 to 10 % longer than those brought to LDS with the codes.  Prefetching a stage further into the L2 took 5 % longer.  Workgroups that go on to
 // further tiles, the next one's first stage under the output of the last, gained nothing (258 us both; the experts 152 against 144): the time saved goes
@@ -193,10 +194,10 @@ __global__ __launch_bounds__(64 * WT * WO) void mx4_tiles(ProductArgs args) {
     const int wt = wave / WO, wo = wave % WO, fr = lane & 31, fh = lane >> 5;
     const int n_st = static_cast<int>((np + 1) / 2);
 
-    // a row of X to read in place of one that does not exist: its products are not stored, or stored as zeros
+    // where rows are gathered: a row of X, the first in place of one that does not exist (its products are not stored, or stored as zeros)
     auto x_row = [&](int i) {
         const int64_t s = source_row(a, r_first + i, gr.hi);
-        return s < 0 ? (a.gather ? int64_t(0) : r_first) : s;
+        return s < 0 ? int64_t(0) : s;
     };
     // Transfers.  Number i of a wave takes ROWS_PER rows; every lane has the same chunk in all of them.  They are given as 32-bit offsets
     // from a row that all share: the tile's first (W; X in Y's order) or that of token 0, which the host holds within 4 GB.

@@ -124,7 +124,7 @@ class Mx4Linear:
     """Y = X W^T for X fp16 or bf16 [tokens, in].
 
     mx4_inputs: from that many tokens on X is quantized as well (0: never), and the product runs at the 4-bit rate: 4096 tokens through
-    [4096, 4096] take 48 us with the quantization, 115 us as bf16."""
+    [4096, 4096] take 47 us with the quantization, 117 us as bf16."""
 
     def __init__(self, weight: Mx4Weight, mx4_inputs: int = 0):
         if weight.experts:
