@@ -5,7 +5,7 @@
 // contraction, X's type and the groups, so each form's time is estimated and the shortest taken.  The estimates are fits to the
 // kernels' times over shapes drawn at random (1 to 8192 rows, 64 to 28672 outputs, 64 to 28672 deep; 4 to 128 experts): mean error 9 to 15 % a form, and
 // the form chosen is 2 % (one weight) and 4 % (experts) slower in the geometric mean than the best of them all.  (How far that best one is from
-// what the sizes need is another matter: 1.1 to 3.8 times over those shapes, most between a few dozen and a few thousand rows.)
+// what the sizes need is another matter: 1.1 to 3.8 times at sizes looked at, most between a few dozen and a few thousand rows.)
 #pragma once
 
 #include <algorithm>
