@@ -442,7 +442,9 @@ int adadim_expert_combine(adadim_ctx* ctx, const void* Z, int z_type, int64_t n_
  *   adadim_capture_end    stops recording and returns the instantiated graph (a hipGraphExec_t as void*).  The
  *           graph holds the pointers and sizes of the recorded calls: the buffers must stay where they are,
  *           new contents are picked up on every launch.  The context's scratch that it was recorded with stays until
- *           adadim_destroy, also where calls of other sizes have outgrown it in the meantime.
+ *           adadim_destroy, also where calls of other sizes have outgrown it in the meantime.  (The context knows of
+ *           recordings that these two calls frame.  Where its stream is captured by other means, make the largest
+ *           calls before: scratch that grows afterwards is freed under such a graph.)
  *   adadim_graph_launch   runs the graph on the context's stream (asynchronous like every other call).
  *   adadim_graph_destroy  frees it.  NULL is allowed.
  */
