@@ -432,6 +432,87 @@ int adadim_expert_combine(adadim_ctx* ctx, const void* Z, int z_type, int64_t n_
                           const float* weights, int64_t tokens, int k, void* Y, int y_type, int64_t ldy);
 
 /*
+ * A paged cache of keys and values in mx4 for serving: a pool of pages of `page` positions (a power of two, 32 to 65536), each with the
+ * keys and values of `heads` key-value heads of `dim` elements (1..256, filled up to 64, 128 or 256: D).  A position is named by its
+ * slot, page number * page + place in the page.  Fewer than 2^31 positions in a pool, and in a sequence's row of the table.
+ *   cache  u8 [pages, heads, page/32, 34 D], 16-byte aligned: 4.25 bits a value.  In a record of 32 positions lie
+ *            the keys' codes    [32][D/2]            element 2i of a position in the low half of byte i
+ *            the values' codes  [4][16][8][D/32]     (g, m, i): elements m D/16 .. of position 4g + i (i < 4) or 12 + 4g + i
+ *            the keys' scales   [32][D/32]           a byte for each block of 32 elements
+ *            the values' scales [4][D/32][8]         (g, block, i)
+ *          so that a position's bytes are its own: appending one reads nothing and touches no other.
+ *   Scales lie in 2^-23 .. 2^13.  A position with an infinity or a NaN in a head's key or value has key scales 255 and zeros otherwise there.
+ * adadim_mx4_cache_bytes gives the size of the pool (0 for arguments that are none).
+ */
+int64_t adadim_mx4_cache_bytes(int64_t pages, int page, int heads, int dim);
+
+/*
+ * Pages and slots for the tokens that a batch adds, from a stack of free pages: free[0 .. count) are free, the last one goes first.
+ * Sequence s holds held[s] tokens in the first ceil(held/page) pages of its row of the table and gets the pages that added[s] more need,
+ * the sequences in their order.
+ *   held, added  int32 [sequences]     table  int32 [sequences, width]: entries of new pages are written, no others
+ *   free     int32 [pool]; count  int32 [1]
+ *   lengths  int32 [sequences]: held + added (may be held itself)
+ *   offsets  int32 [sequences + 1]: where each sequence's new rows begin, for adadim_mx4_attention
+ *   slots, positions  int32 [tokens]: of each new row; -1 behind the last sequence's.  tokens 0 to 2^20
+ *   left     int32 [1]: pages left on the stack (may be count itself)
+ *   lacking  int32 [1]: 0, or what the call was refused for on the device: the number of pages that the stack is short of; -1 where a
+ *            sequence would outgrow its row of the table, the rows are too few, or a number is negative.  Then nothing is taken:
+ *            lengths are held, offsets 0, slots and positions -1, left is count, and the table stays.
+ * All arrays on the device; the host learns nothing of them.  sequences 1..4096.  Arrays must not overlap but for those named.
+ */
+int adadim_cache_reserve(adadim_ctx* ctx, const int32_t* held, const int32_t* added, int sequences, int page, int32_t* table, int64_t width,
+                         const int32_t* free, int64_t pool, const int32_t* count, int32_t* lengths, int32_t* offsets, int32_t* slots,
+                         int32_t* positions, int64_t tokens, int32_t* left, int32_t* lacking);
+
+/*
+ * The way back: sequence s keeps its first kept[s] tokens (0: it has ended; more than held: all, less than 0: none), and the pages behind
+ * them go onto the stack, the sequences in their order, each one's pages in theirs.
+ *   lengths  int32 [sequences]: what is kept (may be held itself)     left  int32 [1]: pages on the stack (may be count itself)
+ * The table stays: entries behind a sequence's pages are not read.  Pages beyond the pool's size (of which there are none if each page is on
+ * the stack or in a table once) are dropped.
+ */
+int adadim_cache_trim(adadim_ctx* ctx, const int32_t* held, const int32_t* kept, int sequences, int page, const int32_t* table, int64_t width,
+                      int32_t* free, int64_t pool, const int32_t* count, int32_t* lengths, int32_t* left);
+
+/*
+ * Rows of keys and values to their slots.  Scale and codes as in adadim_mx4_quantize, the exponent held to -23 .. 13: of a value at most
+ * 49152 is kept, and blocks of less than 2^-21 are kept to 2^-24.
+ *   K, V   [tokens, heads * dim] of type F16, BF16 or F32, row pitches ldk, ldv; any alignment of an element
+ *   slots  int32 [tokens]: each at most once; a row with one outside the pool is not stored
+ * tokens 0 to 2^20.
+ */
+int adadim_mx4_cache_store(adadim_ctx* ctx, const void* K, const void* V, int type, int64_t tokens, int64_t ldk, int64_t ldv,
+                           const int32_t* slots, uint8_t* cache, int64_t pages, int page, int heads, int dim);
+
+/* The values behind slots, into K and V [tokens, heads * dim] (exact in all three types); zeros where a slot is outside the pool.  A slot may
+ * come more than once. */
+int adadim_mx4_cache_load(adadim_ctx* ctx, const int32_t* slots, int64_t tokens, const uint8_t* cache, int64_t pages, int page, int heads,
+                          int dim, void* K, void* V, int type, int64_t ldk, int64_t ldv);
+
+/*
+ * Attention over the cache: Y[t, h] = sum_j softmax_j(scale Q[t, h] . k_j) v_j, head h of q_heads over key-value head h / (q_heads / heads).
+ * Rows offsets[s] .. offsets[s+1] of Q are the last tokens of sequence s, whose keys and values are in the cache already:
+ * of n rows, row i is position lengths[s] - n + i.  It sees the positions below lengths[s], with causal = 1 those up to its own,
+ * with a window those of the last `window` up to its own and whatever causal lets it see behind.
+ *   Q        [tokens, q_heads * dim] F16 or BF16, pitch ldq;  Y  [tokens, q_heads * dim] of y_type F16, BF16 or F32, pitch ldy
+ *   table    int32 [sequences, width]; a page outside [0, pages) holds nothing that a row sees
+ *   offsets  int32 [sequences + 1]: not decreasing, inside [0, tokens] (values outside are taken as the nearer end).  Rows of Y in no sequence
+ *            are not written.
+ *   lengths  int32 [sequences]: inside [0, width * page] (values outside are taken as the nearer end)
+ *   scale    positive;  window  0: none
+ *   max_new, max_length  the most new tokens and positions that a sequence has, as far as the host knows (0: unknown): what the launch is
+ *            laid out for.  Results do not depend on them but for the order of sums.
+ * A row that sees nothing is zeros.  A row that sees a position stored with an infinity or a NaN is NaN; positions that it does not see do
+ * not touch it, whatever they hold.  Scores and sums are fp32 and keys and values enter exactly; the weights 2^(score - largest) are rounded
+ * to fp16 (2^-33 of the row's largest is kept) for the product with the values.  Sums in a fixed order: same bits every run.
+ */
+int adadim_mx4_attention(adadim_ctx* ctx, const void* Q, int q_type, int64_t tokens, int64_t ldq, int q_heads, const uint8_t* cache,
+                         int64_t pages, int page, int heads, int dim, const int32_t* table, int64_t width, int sequences,
+                         const int32_t* offsets, const int32_t* lengths, void* Y, int y_type, int64_t ldy, float scale, int causal,
+                         int64_t window, int64_t max_new, int64_t max_length);
+
+/*
  * Recording a sequence of calls as one HIP graph.  A layer's search is a dozen short kernels; launched one by
  * one the gaps between them are a tenth of the step on a 4096 x 4096 layer, replayed as a graph they close.
  *   adadim_capture_begin  starts recording on the context's stream, which must not be the default

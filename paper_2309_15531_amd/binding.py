@@ -31,6 +31,8 @@ EXPORTS = (
     "adadim_layer_error_batch_select_noalloc", "adadim_noalloc_scratch_bytes", "adadim_probe_mfma", "adadim_probe_mfma_f64",
     "adadim_mx4_code_bytes", "adadim_mx4_scale_bytes", "adadim_mx4_quantize", "adadim_mx4_dequantize", "adadim_mx4_matmul",
     "adadim_mx4_matmul_experts", "adadim_expert_route", "adadim_expert_combine",
+    "adadim_mx4_cache_bytes", "adadim_cache_reserve", "adadim_cache_trim", "adadim_mx4_cache_store", "adadim_mx4_cache_load",
+    "adadim_mx4_attention",
 )
 
 _lib = None
@@ -166,7 +168,14 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
             ("adadim_mx4_matmul", c_int, [p, p, p, c_int, i64, i64, p, p, i64, i64, p, c_int, i64]),
             ("adadim_mx4_matmul_experts", c_int, [p, p, p, c_int, i64, i64, p, i64, p, c_int, p, p, i64, i64, p, c_int, i64]),
             ("adadim_expert_route", c_int, [p, p, c_int, i64, i64, c_int, c_int, c_int, p, p, p, p, p]),
-            ("adadim_expert_combine", c_int, [p, p, c_int, i64, i64, i64, p, p, i64, c_int, p, c_int, i64])):
+            ("adadim_expert_combine", c_int, [p, p, c_int, i64, i64, i64, p, p, i64, c_int, p, c_int, i64]),
+            ("adadim_mx4_cache_bytes", c_int64, [i64, c_int, c_int, c_int]),
+            ("adadim_cache_reserve", c_int, [p, p, p, c_int, c_int, p, i64, p, i64, p, p, p, p, p, i64, p, p]),
+            ("adadim_cache_trim", c_int, [p, p, p, c_int, c_int, p, i64, p, i64, p, p, p]),
+            ("adadim_mx4_cache_store", c_int, [p, p, p, c_int, i64, i64, i64, p, p, i64, c_int, c_int, c_int]),
+            ("adadim_mx4_cache_load", c_int, [p, p, i64, p, i64, c_int, c_int, c_int, p, p, c_int, i64, i64]),
+            ("adadim_mx4_attention", c_int, [p, p, c_int, i64, i64, c_int, p, i64, c_int, c_int, c_int, p, i64, c_int, p, p, p, c_int, i64,
+                                             c_float, c_int, i64, i64, i64])):
         f = getattr(lib, name)
         f.restype, f.argtypes = res, args
     if path is None:
@@ -205,6 +214,11 @@ def mx4_shapes(rows: int, cols: int):
     """Shapes of the codes and scales (uint8) of `rows` rows of `cols` values in mx4."""
     pieces = (cols + 127) // 128
     return (rows, 64 * pieces), (pieces, rows, 4)
+
+
+def mx4_cache_shape(pages: int, page: int, heads: int, dim: int):
+    """Shape of a cache (uint8) of `pages` pages of `page` positions of `heads` heads of `dim` elements."""
+    return pages, heads, page // 32, 34 * (64 if dim <= 64 else 128 if dim <= 128 else 256)
 
 
 class _Dtypes(dict):
@@ -547,6 +561,79 @@ class Context:
             raise ValueError(f"Y: expected {cols} columns, got {y_cols}")
         slots, weights = _array(slots, "slots", "torch.int32", (tokens, k)), _array(weights, "weights", "torch.float32", (tokens, k))
         rc = self._lib.adadim_expert_combine(self._h, z, z_kind, n_rows, cols, ldz, slots, weights, tokens, k, y, y_kind, ldy)
+        if rc:
+            self._check(rc)
+
+    # -- a paged cache of keys and values --------------------------------
+    def adadim_cache_reserve(self, held, added, page: int, table, free, count, lengths, offsets, slots, positions, left, lacking):
+        """Pages from the stack free[0 .. count) for added[s] more tokens of each sequence, and their rows' slots and positions; all int32.
+        table [sequences, width], offsets [sequences + 1]; slots and positions as many as there may be rows."""
+        i32, n, tokens = "torch.int32", held.numel(), slots.numel()
+        width = table.shape[-1]
+        rc = self._lib.adadim_cache_reserve(
+            self._h, _array(held, "held", i32, (n,)), _array(added, "added", i32, (n,)), n, page, _array(table, "table", i32, (n, width)), width,
+            _array(free, "free", i32, (free.numel(),)), free.numel(), _array(count, "count", i32, (1,)), _array(lengths, "lengths", i32, (n,)),
+            _array(offsets, "offsets", i32, (n + 1,)), _array(slots, "slots", i32, (tokens,)), _array(positions, "positions", i32, (tokens,)),
+            tokens, _array(left, "left", i32, (1,)), _array(lacking, "lacking", i32, (1,)))
+        if rc:
+            self._check(rc)
+
+    def adadim_cache_trim(self, held, kept, page: int, table, free, count, lengths, left):
+        """The pages behind the first kept[s] tokens of each sequence back to the stack."""
+        i32, n = "torch.int32", held.numel()
+        width = table.shape[-1]
+        rc = self._lib.adadim_cache_trim(
+            self._h, _array(held, "held", i32, (n,)), _array(kept, "kept", i32, (n,)), n, page, _array(table, "table", i32, (n, width)), width,
+            _array(free, "free", i32, (free.numel(),)), free.numel(), _array(count, "count", i32, (1,)), _array(lengths, "lengths", i32, (n,)),
+            _array(left, "left", i32, (1,)))
+        if rc:
+            self._check(rc)
+
+    def _mx4_cache(self, cache, dim):
+        """(address, pages, page, heads) of a cache of heads of `dim` elements."""
+        shape = cache.shape
+        if len(shape) != 4 or not 1 <= dim <= 256 or shape[3] != mx4_cache_shape(1, 32, 1, dim)[3]:
+            raise ValueError(f"cache: expected [pages, heads, page / 32, record] of heads of {dim}, got shape {tuple(shape)}")
+        return _array(cache, "cache", "torch.uint8", shape), shape[0], 32 * shape[2], shape[1]
+
+    def _mx4_rows(self, K, V, slots, cache):
+        k, kind, tokens, cols, ldk = _matrix(K, "K")
+        v, v_kind, v_tokens, v_cols, ldv = _matrix(V, "V")
+        heads = cache.shape[1] if cache.dim() == 4 else 0
+        if v_kind != kind or v_tokens != tokens or v_cols != cols or heads < 1 or cols % heads:
+            raise ValueError(f"K and V: one type and shape, columns a multiple of the cache's {heads} heads, got {tuple(K.shape)} and {tuple(V.shape)}")
+        c, pages, page, heads = self._mx4_cache(cache, cols // heads)
+        return k, v, kind, tokens, ldk, ldv, _array(slots, "slots", "torch.int32", (tokens,)), c, pages, page, heads, cols // heads
+
+    def adadim_mx4_cache_store(self, K, V, slots, cache):
+        """Rows of K and V [tokens, heads * dim] (rows may be pitched) to their slots in cache [pages, heads, page / 32, record]."""
+        k, v, kind, tokens, ldk, ldv, slots, c, pages, page, heads, dim = self._mx4_rows(K, V, slots, cache)
+        rc = self._lib.adadim_mx4_cache_store(self._h, k, v, kind, tokens, ldk, ldv, slots, c, pages, page, heads, dim)
+        if rc:
+            self._check(rc)
+
+    def adadim_mx4_cache_load(self, slots, cache, K, V):
+        """The values behind slots into K and V."""
+        k, v, kind, tokens, ldk, ldv, slots, c, pages, page, heads, dim = self._mx4_rows(K, V, slots, cache)
+        rc = self._lib.adadim_mx4_cache_load(self._h, slots, tokens, c, pages, page, heads, dim, k, v, kind, ldk, ldv)
+        if rc:
+            self._check(rc)
+
+    def adadim_mx4_attention(self, Q, cache, table, offsets, lengths, Y, dim: int, scale: float | None = None, causal: bool = True,
+                             window: int = 0, max_new: int = 0, max_length: int = 0):
+        """Q, Y [tokens, query heads * dim] (rows may be pitched); table [sequences, width].  scale: dim ** -0.5 if None.  max_new, max_length:
+        the most new tokens and positions of a sequence, where the host knows them."""
+        q, kind, tokens, cols, ldq = _matrix(Q, "Q")
+        y, y_kind, y_tokens, y_cols, ldy = _matrix(Y, "Y")
+        c, pages, page, heads = self._mx4_cache(cache, dim)
+        if y_tokens != tokens or y_cols != cols or cols % dim:
+            raise ValueError(f"Q and Y: one shape, columns a multiple of {dim}, got {tuple(Q.shape)} and {tuple(Y.shape)}")
+        n = lengths.numel()
+        width = table.shape[-1]
+        rc = self._lib.adadim_mx4_attention(
+            self._h, q, kind, tokens, ldq, cols // dim, c, pages, page, heads, dim, _array(table, "table", "torch.int32", (n, width)), width, n,
+            _array(offsets, "offsets", "torch.int32", (n + 1,)), _array(lengths, "lengths", "torch.int32", (n,)), y, y_kind, ldy,
+            dim ** -0.5 if scale is None else scale, 1 if causal else 0, window, max_new, max_length)
         if rc:
             self._check(rc)
 

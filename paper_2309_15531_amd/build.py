@@ -15,7 +15,8 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libadadim.so")
 SOURCES = ["api.hip", "quantize.hip", "hessian.hip", "layer_error.hip", "gemv_ic.hip", "gptq.hip", "probe.hip",
-           "api_mx4.hip", "mx4_quantize.hip", "mx4_matmul.hip", "experts.hip"]
+           "api_mx4.hip", "mx4_quantize.hip", "mx4_matmul.hip", "experts.hip",
+           "api_cache.hip", "cache_pages.hip", "mx4_cache.hip", "mx4_attention.hip", "mx4_attention_f16.hip", "mx4_attention_bf16.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-ffp-contract=off",                      # one rounding per operation in the quantizer

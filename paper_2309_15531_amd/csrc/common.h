@@ -39,6 +39,8 @@ enum {
     WS_MX4_X,           // rows of X copied to where 16-byte transfers can take them
     WS_MX4_PART,        // counters of the output tiles whose contraction is shared, then their partial sums
     WS_ROUTE,           // the router's masks of tokens per chunk and expert, then their counts
+    WS_CACHE_PLAN,      // what the rows of a batch need of the page plan: per sequence tokens held, first new page; the state of the stack
+    WS_ATTEND,          // counters of the attention tiles whose positions are shared, then their partial sums
     WS_COUNT
 };
 
