@@ -8,10 +8,9 @@
 // sum are numbers of its lanes.  The maximum m is only raised (and O^T and the sum scaled) where a score passes it by more than 7:
 // p stays below 2^15.  The sum is of p before rounding.  Scores, sums and O^T are fp32.
 //
-// KEYS: the four waves of a workgroup have the same rows and take records in turn (few rows: the read of the cache bounds it); their sums meet
-// in LDS.  Otherwise each wave has 16 NT rows of its own and all go over the same records, which the L1 then holds.
-// Either way a tile's records may be shared between workgroups (gridDim.y); partial sums travel as relaxed atomics at device scope, and
-// the workgroup that finishes last joins them in their order: same bits every run.
+// Few rows (this file): the four waves of a workgroup have the same rows and take records in turn; their sums meet in LDS.  Many rows:
+// mx4_attention_tiles.h.  Either way a tile's records may be shared between workgroups (gridDim.y); partial sums travel as relaxed atomics at
+// device scope, and the workgroup that finishes last joins them in their order: same bits every run.
 #pragma once
 
 #include "mx4_cache.h"
@@ -43,29 +42,60 @@ template <> struct Dots<__bf16> {
     static __device__ __forceinline__ float4v mfma(vec a, vec b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 
-// The bytes of a record that a lane needs.
+// The bytes of a record's keys that a lane of row m and quarter g needs: of positions m and 16 + m the elements (D/4) g ...
 template <int D>
-struct Bytes {
-    static constexpr int W = D / 32, VW = D / 16;             // words of a key's quarter, of 8 positions' values
-    uint32_t k[2][W], v[VW], ks[2], vs[2];
+struct KeyBytes {
+    static constexpr int W = D / 32;
+    uint32_t words[2][W], scale_bytes[2];
     __device__ __forceinline__ void load(const uint8_t* r, int lane) {
-        typedef Record<D> R;
         const int m = lane & 15, g = lane >> 4;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const int key = 16 * t + m;
             const uint32_t* p = reinterpret_cast<const uint32_t*>(r + key * (D / 2) + g * (D / 8));
 #pragma unroll
-            for (int c = 0; c < W; ++c) k[t][c] = p[c];
-            if constexpr (D == 256) ks[t] = *reinterpret_cast<const uint16_t*>(r + R::KEY_SCALES + key * 8 + 2 * g);
-            else ks[t] = r[R::KEY_SCALES + key * W + g * W / 4];
+            for (int c = 0; c < W; ++c) words[t][c] = p[c];
+            if constexpr (D == 256) scale_bytes[t] = *reinterpret_cast<const uint16_t*>(r + Record<D>::KEY_SCALES + key * 8 + 2 * g);
+            else scale_bytes[t] = r[Record<D>::KEY_SCALES + key * W + g * W / 4];
         }
-        const uint32_t* p = reinterpret_cast<const uint32_t*>(r + R::VALUES + (g * 16 + m) * (8 * R::UNIT));
+    }
+    __device__ __forceinline__ float scale(int t, int w) const {
+        return scale_operand(D == 256 ? w < 4 ? scale_bytes[t] & 255u : scale_bytes[t] >> 8 : scale_bytes[t]);
+    }
+};
+
+// Of its values: the elements m D/16 .. of the 8 positions of quarter g.
+template <int D>
+struct ValueBytes {
+    static constexpr int W = D / 32;
+    uint32_t words[D / 16], scale_words[2];
+    __device__ __forceinline__ void load(const uint8_t* r, int lane) {
+        const int m = lane & 15, g = lane >> 4;
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(r + Record<D>::VALUES + (g * 16 + m) * (8 * Record<D>::UNIT));
 #pragma unroll
-        for (int c = 0; c < VW; ++c) v[c] = p[c];
-        const uint32_t* s = reinterpret_cast<const uint32_t*>(r + R::VALUE_SCALES + (g * W + m * W / 16) * 8);
-        vs[0] = s[0];
-        vs[1] = s[1];
+        for (int c = 0; c < D / 16; ++c) words[c] = p[c];
+        const uint32_t* s = reinterpret_cast<const uint32_t*>(r + Record<D>::VALUE_SCALES + (g * W + m * W / 16) * 8);
+        scale_words[0] = s[0];
+        scale_words[1] = s[1];
+    }
+    // the 8 positions' scales; those that do not exist (have: how many do) become zeros whatever their codes: 2^-127 in fp16
+    __device__ __forceinline__ void scales(float (&v)[8], int g, int have) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = scale_operand((scale_words[i >> 2] >> (8 * (i & 3))) & 255u);
+        if (have < RECORD) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = 4 * g + (i < 4 ? i : 12 + i) < have ? v[i] : 0.0f;
+        }
+    }
+    // elements 2 u and 2 u + 1 of position i
+    __device__ __forceinline__ half2v pair(int i, int u, float scale) const {
+        const int at = i * W + u;
+        switch (at & 3) {
+            case 0: return __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(words[at >> 2], scale, 0);
+            case 1: return __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(words[at >> 2], scale, 1);
+            case 2: return __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(words[at >> 2], scale, 2);
+            default: return __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(words[at >> 2], scale, 3);
+        }
     }
 };
 
@@ -96,8 +126,7 @@ struct Rows {
     }
 
     // lo, hi: the positions that the rows see, counted from the record's first; have: how many of it exist
-    template <bool MASK>
-    __device__ __forceinline__ void add(const Bytes<D>& b, int lane, const int (&lo)[NT], const int (&hi)[NT], int have) {
+    __device__ __forceinline__ void add(const KeyBytes<D>& kb, const ValueBytes<D>& vb, int lane, bool mask, const int (&lo)[NT], const int (&hi)[NT], int have) {
         const int g = lane >> 4;
         float4v s[NT][2];
 #pragma unroll
@@ -106,17 +135,15 @@ struct Rows {
             for (int n = 0; n < NT; ++n) s[n][t] = float4v{0, 0, 0, 0};
 #pragma unroll
             for (int w = 0; w < W; ++w) {
-                const uint32_t byte = D == 256 ? w < 4 ? b.ks[t] & 255u : b.ks[t] >> 8 : b.ks[t];
-                const vec k = Dots<T>::keys(b.k[t][w], scale_operand(byte));
+                const vec k = Dots<T>::keys(kb.words[t][w], kb.scale(t, w));
 #pragma unroll
                 for (int n = 0; n < NT; ++n) s[n][t] = Dots<T>::mfma(k, q[n][w], s[n][t]);
             }
         }
-        float top[NT];
-        bool raise = false;
+        __builtin_amdgcn_sched_barrier(0);        // (keys' and values' operands are not held at the same time)
+        if (mask) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            if constexpr (MASK) {
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -124,7 +151,11 @@ struct Rows {
                         const int at = 16 * t + 4 * g + i;
                         s[n][t][i] = at >= lo[n] && at < hi[n] ? s[n][t][i] : -INFINITY;
                     }
-            }
+        }
+        float top[NT];
+        bool raise = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
             top[n] = fmaxf(fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3])),
                            fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3]))) * c;
             raise = raise || top[n] > m[n] + RAISE;
@@ -153,25 +184,15 @@ struct Rows {
                     p[n][4 * t + i] = static_cast<_Float16>(e);
                 }
         }
+        __builtin_amdgcn_sched_barrier(0);
         float vs[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            vs[i] = scale_operand((b.vs[i >> 2] >> (8 * (i & 3))) & 255u);
-            if constexpr (MASK) vs[i] = 4 * g + (i < 4 ? i : 12 + i) < have ? vs[i] : 0.0f;        // (2^-127: zeros in fp16)
-        }
+        vb.scales(vs, g, have);
 #pragma unroll
         for (int u = 0; u < D / 32; ++u) {
             half8v even, odd;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int at = i * (D / 32) + u;
-                half2v v;
-                switch (at & 3) {
-                    case 0: v = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(b.v[at >> 2], vs[i], 0); break;
-                    case 1: v = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(b.v[at >> 2], vs[i], 1); break;
-                    case 2: v = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(b.v[at >> 2], vs[i], 2); break;
-                    default: v = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(b.v[at >> 2], vs[i], 3); break;
-                }
+                const half2v v = vb.pair(i, u, vs[i]);
                 even[i] = v.x;
                 odd[i] = v.y;
             }
@@ -245,78 +266,127 @@ __device__ __forceinline__ TileRows tile_rows(const Attention& a, int tile) {
     return t;
 }
 
-template <class T, int D, int NT, bool KEYS>
-__global__ __launch_bounds__(64 * AT_WAVES) void mx4_attend(AttentionArgs args) {
-    const Attention& a = args.a;
-    constexpr int WROWS = 16 * NT, R = KEYS ? WROWS : AT_WAVES * WROWS;
-    constexpr int TILES = D / 16;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
-    const int head = blockIdx.x % a.heads, tile = args.tiles - 1 - static_cast<int>(blockIdx.x / a.heads);        // (the longest rows first)
-    const TileRows tr = tile_rows<R>(a, tile);
-    if (tr.rows == 0) return;
-    const int64_t most = a.width << a.log_page;
-    const int length = static_cast<int>(min(max(int64_t(a.lengths[tr.sequence]), int64_t(0)), most));
-    // the position of new token t is before + t
-    const int before = length - tr.added;
-    auto token_of = [&](int row) { return tr.token + (tr.rest + row) / a.group; };
-    auto sees_to = [&](int token) { return a.causal ? min(max(before + token + 1, 0), length) : length; };
-    auto sees_from = [&](int token) { return a.window ? static_cast<int>(max(int64_t(before) + token + 1 - a.window, int64_t(0))) : 0; };
-
-    // ---- the records of the tile, of the workgroup's share, of the wave
-    const int t_last = token_of(tr.rows - 1);
-    const int r_begin = sees_from(tr.token) >> 5, r_end = (sees_to(t_last) + 31) >> 5;
-    const int n_records = max(r_end - r_begin, 0);
-    const int share = max((n_records + static_cast<int>(gridDim.y) - 1) / static_cast<int>(gridDim.y), args.least);
-    const int shares = max((n_records + share - 1) / share, 1);
-    if (static_cast<int>(blockIdx.y) >= shares) return;
-    const int w_row = KEYS ? 0 : WROWS * wave;                // the wave's first row
-    const int w_rows = min(WROWS, tr.rows - w_row);           // (not positive: none)
-    int b = r_begin + share * blockIdx.y, e = min(b + share, r_end);
-    const int w_first = token_of(w_row), w_last = token_of(max(w_row + w_rows - 1, w_row));
-    if constexpr (KEYS) b += wave;
-    else {
-        if (w_rows <= 0) e = b;
-        b = max(b, sees_from(w_first) >> 5);
-        e = min(e, (sees_to(w_last) + 31) >> 5);
+// What a workgroup has to do: its rows, the records of its share, how many shares there are (0: nothing to do).
+struct Work {
+    TileRows tr;
+    int head, length, before;                     // before + t: the position of new token t
+    int begin, end, shares;
+    __device__ __forceinline__ int token_of(const Attention& a, int row) const { return tr.token + (tr.rest + row) / a.group; }
+    __device__ __forceinline__ int head_of(const Attention& a, int row) const { return head * a.group + (tr.rest + row) % a.group; }
+    __device__ __forceinline__ int sees_to(const Attention& a, int token) const { return a.causal ? min(max(before + token + 1, 0), length) : length; }
+    __device__ __forceinline__ int sees_from(const Attention& a, int token) const {
+        return a.window ? static_cast<int>(max(int64_t(before) + token + 1 - a.window, int64_t(0))) : 0;
     }
-    constexpr int STEP = KEYS ? AT_WAVES : 1;
-    // records from all_from to before all_to hide nothing from any row
-    const int all_from = (sees_from(w_last) + 31) >> 5, all_to = sees_to(w_first) >> 5;
+    __device__ __forceinline__ int64_t row_of_y(const Attention& a, int row) const {
+        return (tr.first - tr.token + token_of(a, row)) * a.ldy + int64_t(head_of(a, row)) * a.dim;
+    }
+};
+template <int R>
+__device__ __forceinline__ Work work_of(const AttentionArgs& args) {
+    const Attention& a = args.a;
+    Work w;
+    w.shares = 0;
+    w.head = blockIdx.x % a.heads;
+    w.tr = tile_rows<R>(a, args.tiles - 1 - static_cast<int>(blockIdx.x / a.heads));         // (the longest rows first)
+    if (w.tr.rows == 0) return w;
+    w.length = static_cast<int>(min(max(int64_t(a.lengths[w.tr.sequence]), int64_t(0)), a.width << a.log_page));
+    w.before = w.length - w.tr.added;
+    const int begin = w.sees_from(a, w.tr.token) >> 5, end = (w.sees_to(a, w.token_of(a, w.tr.rows - 1)) + 31) >> 5;
+    const int records = max(end - begin, 0), y = static_cast<int>(blockIdx.y), ny = static_cast<int>(gridDim.y);
+    const int share = max((records + ny - 1) / ny, args.least);
+    const int shares = max((records + share - 1) / share, 1);
+    w.shares = y < shares ? shares : 0;
+    w.begin = begin + share * y;
+    w.end = min(w.begin + share, end);
+    return w;
+}
 
-    // ---- the wave's rows
+// Partial sums: per tile, head and share [R rows][D + 2], the sums, then m and l.  Who finishes last joins the shares.
+template <int D> constexpr int PART = D + 2;
+template <int R, int D, int WAVES>
+__device__ __forceinline__ void join(const AttentionArgs& args, const Work& w) {
+    constexpr int N = D / 16;
+    __shared__ unsigned s_ticket;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) s_ticket = __hip_atomic_fetch_add(args.tickets + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (s_ticket != unsigned(w.shares) - 1) return;
+    if (threadIdx.x == 0) __hip_atomic_store(args.tickets + blockIdx.x, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const float* const all = args.parts + int64_t(blockIdx.x) * gridDim.y * (R * PART<D>);
+    const int d0 = (threadIdx.x & 15) * N;
+    for (int row = threadIdx.x >> 4; row < w.tr.rows; row += 4 * WAVES) {
+        const float* const p = all + row * PART<D>;
+        float m = LOWEST, l = 0.0f, v[N];
+        for (int z = 0; z < w.shares; ++z) m = fmaxf(m, get(p + int64_t(z) * (R * PART<D>) + D));
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = 0.0f;
+        for (int z = 0; z < w.shares; ++z) {
+            const float* const q = p + int64_t(z) * (R * PART<D>);
+            const float by = __builtin_amdgcn_exp2f(get(q + D) - m);
+            l += get(q + D + 1) * by;
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] += get(q + d0 + j) * by;
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = l == 0.0f ? 0.0f : v[j] / l;
+        store_row(args.a, w.row_of_y(args.a, row), d0, v);
+    }
+}
+
+// Waves of a SIMD that the registers have to leave room for.
+template <int D, int NT> constexpr int FEW_WAVES = NT == 1 ? (D == 64 ? 4 : D == 128 ? 3 : 1) : D == 64 ? 3 : 2;
+
+template <class T, int D, int NT>
+__global__ __launch_bounds__(64 * AT_WAVES, (FEW_WAVES<D, NT>)) void mx4_attend_few(AttentionArgs args) {
+    const Attention& a = args.a;
+    constexpr int R = 16 * NT, TILES = D / 16;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
+    const Work w = work_of<R>(args);
+    if (w.shares == 0) return;
+    int b = w.begin + wave;
+    const int e = w.end;
+    const int t_last = w.token_of(a, w.tr.rows - 1);
+    // records from all_from to before all_to hide nothing from any row
+    const int all_from = (w.sees_from(a, t_last) + 31) >> 5, all_to = w.sees_to(a, w.tr.token) >> 5;
+
     Rows<T, D, NT> rows;
     rows.c = a.scale * 1.44269504088896340736f;
     rows.clear();
-    int row_token[NT], lo[NT], hi[NT];
-    int64_t row_at[NT];                           // (token, head) of the lane's row, as the place of its element 0 in units of a pitch and elements
+    int lo[NT], hi[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int row = min(w_row + 16 * n + (lane & 15), tr.rows - 1);       // (rows that are not there repeat the last one)
-        const int t = token_of(row), h = (tr.rest + row) % a.group;
-        row_token[n] = t;
-        lo[n] = sees_from(t);
-        hi[n] = sees_to(t);
-        row_at[n] = int64_t(head) * a.group + h;
-        const T* q = static_cast<const T*>(a.Q) + (tr.first - tr.token + t) * a.ldq + row_at[n] * a.dim;
+        const int row = min(16 * n + (lane & 15), w.tr.rows - 1);             // (rows that are not there repeat the last one)
+        const int t = w.token_of(a, row);
+        lo[n] = w.sees_from(a, t);
+        hi[n] = w.sees_to(a, t);
+        const T* q = static_cast<const T*>(a.Q) + (w.tr.first - w.tr.token + t) * a.ldq + int64_t(w.head_of(a, row)) * a.dim;
 #pragma unroll
-        for (int w = 0; w < D / 32; ++w) {
-            const int d = (D / 4) * g + 8 * w;
-            rows.q[n][w] = d < a.dim ? __builtin_bit_cast(typename Dots<T>::vec, Chunk<T, 8>::load(q + d, a.dim - d)) : typename Dots<T>::vec{};
+        for (int k = 0; k < D / 32; ++k) {
+            const int d = (D / 4) * g + 8 * k;
+            rows.q[n][k] = d < a.dim ? __builtin_bit_cast(typename Dots<T>::vec, Chunk<T, 8>::load(q + d, a.dim - d)) : typename Dots<T>::vec{};
         }
     }
-    const int32_t* const table = a.table + int64_t(tr.sequence) * a.width;
+    const int32_t* const table = a.table + int64_t(w.tr.sequence) * a.width;
     const int per_page = a.log_page - 5;
     auto page_of = [&](int r) { return r < e ? table[r >> per_page] : -1; };
     auto record = [&](int page, int r) {
         const int64_t p = uint32_t(page) < uint64_t(a.pages) ? page : 0;      // (a page that is not there is not used; page 0 is)
-        return a.cache + (((p * a.heads + head) << per_page) + (r & ((1 << per_page) - 1))) * Record<D>::BYTES;
+        return a.cache + (((p * a.heads + w.head) << per_page) + (r & ((1 << per_page) - 1))) * Record<D>::BYTES;
     };
-    Bytes<D> now, next;
-    int page = page_of(b), page1 = page_of(b + STEP);
-    if (b < e) now.load(record(page, b), lane);
-    for (; b < e; b += STEP) {
-        const int page2 = page_of(b + 2 * STEP);
-        if (b + STEP < e) next.load(record(page1, b + STEP), lane);
+    KeyBytes<D> k_now, k_next;
+    ValueBytes<D> v_now, v_next;
+    int page = page_of(b), page1 = page_of(b + AT_WAVES);
+    if (b < e) {
+        k_now.load(record(page, b), lane);
+        v_now.load(record(page, b), lane);
+    }
+    for (; b < e; b += AT_WAVES) {
+        const int page2 = page_of(b + 2 * AT_WAVES);
+        if (b + AT_WAVES < e) {
+            k_next.load(record(page1, b + AT_WAVES), lane);
+            v_next.load(record(page1, b + AT_WAVES), lane);
+        }
         if (uint32_t(page) < uint64_t(a.pages)) {
             int from[NT], to[NT];
 #pragma unroll
@@ -324,132 +394,74 @@ __global__ __launch_bounds__(64 * AT_WAVES) void mx4_attend(AttentionArgs args) 
                 from[n] = lo[n] - 32 * b;
                 to[n] = hi[n] - 32 * b;
             }
-            if (b >= all_from && b < all_to) rows.template add<false>(now, lane, from, to, 32);
-            else rows.template add<true>(now, lane, from, to, length - 32 * b);
+            rows.add(k_now, v_now, lane, b < all_from || b >= all_to, from, to, w.length - 32 * b);
         }
-        now = next;
+        k_now = k_next;
+        v_now = v_next;
         page = page1;
         page1 = page2;
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) rows.l[n] = quarters(rows.l[n], [](float x, float y) { return x + y; });
 
-    // ---- out.  parts: per shared tile and head [share][R rows][D + 2]: sums, then m and l
-    constexpr int PITCH = D + 2;
-    const int64_t item = int64_t(blockIdx.x);
-    float* const mine = args.parts + (item * gridDim.y + blockIdx.y) * (R * PITCH);
-    __shared__ unsigned s_ticket;
-    if constexpr (KEYS) {
-        constexpr int PARTS = D > 128 ? 2 : 1, JT = TILES / PARTS;             // (a part of D's elements at a time: 64 KB)
-        __shared__ float s_o[AT_WAVES][16][16 * JT + 4];
-        __shared__ float s_m[AT_WAVES][WROWS], s_l[AT_WAVES][WROWS];
-        if (lane < 16)
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                s_m[wave][16 * n + lane] = rows.m[n];
-                s_l[wave][16 * n + lane] = rows.l[n];
-            }
-        __syncthreads();
-        const int r = threadIdx.x >> 4, x = threadIdx.x & 15;
+    // ---- the four waves' sums
+    float* const mine = args.parts + (int64_t(blockIdx.x) * gridDim.y + blockIdx.y) * (R * PART<D>);
+    constexpr int PARTS = D > 128 ? 2 : 1, JT = TILES / PARTS;             // (a part of D's elements at a time: 64 KB)
+    __shared__ float s_o[AT_WAVES][16][16 * JT + 4];
+    __shared__ float s_m[AT_WAVES][R], s_l[AT_WAVES][R];
+    if (lane < 16)
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int rn = 16 * n + (lane & 15), row = 16 * n + r;
-            float top = s_m[0][rn], m = s_m[0][row], l = 0.0f;
-#pragma unroll
-            for (int w = 1; w < AT_WAVES; ++w) {
-                top = fmaxf(top, s_m[w][rn]);
-                m = fmaxf(m, s_m[w][row]);
-            }
-            const float by = __builtin_amdgcn_exp2f(rows.m[n] - top);
-#pragma unroll
-            for (int w = 0; w < AT_WAVES; ++w) l += s_l[w][row] * __builtin_amdgcn_exp2f(s_m[w][row] - m);
-            const float by1 = l == 0.0f ? 0.0f : 1.0f / l;
-#pragma unroll
-            for (int part = 0; part < PARTS; ++part) {
-                if (n > 0 || part > 0) __syncthreads();
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < JT; ++j) s_o[wave][lane & 15][JT * (4 * g + i) + j] = rows.o[n][part * JT + j][i] * by;
-                __syncthreads();
-                if (row >= tr.rows) continue;
-                const int d0 = TILES * x + part * JT;
-                float v[JT];
-#pragma unroll
-                for (int j = 0; j < JT; ++j) {
-                    v[j] = 0.0f;
-#pragma unroll
-                    for (int w = 0; w < AT_WAVES; ++w) v[j] += s_o[w][r][JT * x + j];
-                }
-                if (shares > 1) {
-#pragma unroll
-                    for (int j = 0; j < JT; ++j) put(mine + row * PITCH + d0 + j, v[j]);
-                    if (d0 == 0) {
-                        put(mine + row * PITCH + D, m);
-                        put(mine + row * PITCH + D + 1, l);
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < JT; ++j) v[j] = l == 0.0f ? 0.0f : v[j] * by1;
-                    store_row(a, (tr.first - tr.token + token_of(row)) * a.ldy + (int64_t(head) * a.group + (tr.rest + row) % a.group) * a.dim, d0, v);
-                }
-            }
+            s_m[wave][16 * n + lane] = rows.m[n];
+            s_l[wave][16 * n + lane] = rows.l[n];
         }
-    } else {
+    __syncthreads();
+    const int r = threadIdx.x >> 4, x = threadIdx.x & 15;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int row = w_row + 16 * n + (lane & 15);
-            if (row >= tr.rows) continue;
-            const float l = rows.l[n], by = l == 0.0f ? 0.0f : 1.0f / l;
+    for (int n = 0; n < NT; ++n) {
+        const int rn = 16 * n + (lane & 15), row = 16 * n + r;
+        float top = s_m[0][rn], m = s_m[0][row], l = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float v[TILES];
+        for (int i = 1; i < AT_WAVES; ++i) {
+            top = fmaxf(top, s_m[i][rn]);
+            m = fmaxf(m, s_m[i][row]);
+        }
+        const float by = __builtin_amdgcn_exp2f(rows.m[n] - top);
 #pragma unroll
-                for (int j = 0; j < TILES; ++j) v[j] = rows.o[n][j][i];
-                const int d = TILES * (4 * g + i);
-                if (shares > 1) {
+        for (int i = 0; i < AT_WAVES; ++i) l += s_l[i][row] * __builtin_amdgcn_exp2f(s_m[i][row] - m);
+        const float by1 = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-                    for (int j = 0; j < TILES; ++j) put(mine + row * PITCH + d + j, v[j]);
-                } else {
+        for (int part = 0; part < PARTS; ++part) {
+            if (n > 0 || part > 0) __syncthreads();
 #pragma unroll
-                    for (int j = 0; j < TILES; ++j) v[j] = l == 0.0f ? 0.0f : v[j] * by;
-                    store_row(a, (tr.first - tr.token + row_token[n]) * a.ldy + row_at[n] * a.dim, d, v);
-                }
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < JT; ++j) s_o[wave][lane & 15][JT * (4 * g + i) + j] = rows.o[n][part * JT + j][i] * by;
+            __syncthreads();
+            if (row >= w.tr.rows) continue;
+            const int d0 = TILES * x + part * JT;
+            float v[JT];
+#pragma unroll
+            for (int j = 0; j < JT; ++j) {
+                v[j] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < AT_WAVES; ++i) v[j] += s_o[i][r][JT * x + j];
             }
-            if (shares > 1 && g == 0) {
-                put(mine + row * PITCH + D, rows.m[n]);
-                put(mine + row * PITCH + D + 1, l);
+            if (w.shares > 1) {
+#pragma unroll
+                for (int j = 0; j < JT; ++j) put(mine + row * PART<D> + d0 + j, v[j]);
+                if (d0 == 0) {
+                    put(mine + row * PART<D> + D, m);
+                    put(mine + row * PART<D> + D + 1, l);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < JT; ++j) v[j] = l == 0.0f ? 0.0f : v[j] * by1;
+                store_row(a, w.row_of_y(a, row), d0, v);
             }
         }
     }
-    if (shares == 1) return;
-
-    // ---- who finishes last joins the shares
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (threadIdx.x == 0) s_ticket = __hip_atomic_fetch_add(args.tickets + item, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    if (s_ticket != unsigned(shares) - 1) return;
-    if (threadIdx.x == 0) __hip_atomic_store(args.tickets + item, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const float* const all = args.parts + item * gridDim.y * (R * PITCH);
-    const int d0 = (threadIdx.x & 15) * TILES;
-    for (int row = threadIdx.x >> 4; row < tr.rows; row += 16) {
-        const float* const p = all + row * PITCH;
-        float m = LOWEST, l = 0.0f, v[TILES];
-        for (int z = 0; z < shares; ++z) m = fmaxf(m, get(p + int64_t(z) * (R * PITCH) + D));
-#pragma unroll
-        for (int j = 0; j < TILES; ++j) v[j] = 0.0f;
-        for (int z = 0; z < shares; ++z) {
-            const float* const q = p + int64_t(z) * (R * PITCH);
-            const float by = __builtin_amdgcn_exp2f(get(q + D) - m);
-            l += get(q + D + 1) * by;
-#pragma unroll
-            for (int j = 0; j < TILES; ++j) v[j] += get(q + d0 + j) * by;
-        }
-#pragma unroll
-        for (int j = 0; j < TILES; ++j) v[j] = l == 0.0f ? 0.0f : v[j] / l;
-        store_row(a, (tr.first - tr.token + token_of(row)) * a.ldy + (int64_t(head) * a.group + (tr.rest + row) % a.group) * a.dim, d0, v);
-    }
+    if (w.shares > 1) join<R, D, AT_WAVES>(args, w);
 }
 
 }  // namespace mx4

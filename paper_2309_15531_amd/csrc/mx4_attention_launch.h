@@ -1,7 +1,7 @@
 // The attention kernels of one type of queries, and the choice among them.
 #pragma once
 
-#include "mx4_attention.h"
+#include "mx4_attention_tiles.h"
 
 int attention_shares(adadim_ctx* ctx, size_t bytes, void*& shared);
 
@@ -22,35 +22,59 @@ inline Shares shares_of(const Attention& a, int64_t tiles, int rows, bool keys) 
     return {static_cast<int>(std::min<int64_t>(n, 256)), least};
 }
 
-template <class T, int D, int NT, bool KEYS>
-int launch_form(adadim_ctx* ctx, const Attention& a) {
-    constexpr int R = KEYS ? 16 * NT : AT_WAVES * 16 * NT;
+// The launch's tiles, shares and scratch; R: rows of a tile.
+template <int R, int D>
+int laid_out(adadim_ctx* ctx, const Attention& a, bool keys, AttentionArgs& args, dim3& grid) {
     const int64_t tiles = a.tokens * a.group / R + a.sequences;
-    const Shares s = shares_of(a, tiles, R, KEYS);
-    AttentionArgs args{a, static_cast<int>(tiles), s.least, nullptr, nullptr};
-    if (s.most > 1) {
-        void* shared = nullptr;
-        const int rc = attention_shares(ctx, size_t(tiles) * a.heads * s.most * R * (D + 2) * 4, shared);
-        if (rc != ADADIM_OK) return rc;
-        args.tickets = static_cast<unsigned*>(shared);
-        args.parts = static_cast<float*>(shared) + AT_TICKETS;
-    }
-    ProfScope prof(ctx, "mx4_attend");
-    hipLaunchKernelGGL((mx4_attend<T, D, NT, KEYS>), dim3(static_cast<unsigned>(tiles * a.heads), s.most), dim3(64 * AT_WAVES), 0, ctx->stream, args);
-    ADADIM_LAUNCH_CHECK(ctx, "mx4_attend");
+    const Shares s = shares_of(a, tiles, R, keys);
+    args = AttentionArgs{a, static_cast<int>(tiles), s.least, nullptr, nullptr};
+    grid = dim3(static_cast<unsigned>(tiles * a.heads), s.most);
+    if (s.most == 1) return ADADIM_OK;
+    void* shared = nullptr;
+    const int rc = attention_shares(ctx, size_t(tiles) * a.heads * s.most * R * PART<D> * 4, shared);
+    if (rc != ADADIM_OK) return rc;
+    args.tickets = static_cast<unsigned*>(shared);
+    args.parts = static_cast<float*>(shared) + AT_TICKETS;
+    return ADADIM_OK;
+}
+
+template <class T, int D, int NT>
+int launch_few(adadim_ctx* ctx, const Attention& a) {
+    AttentionArgs args;
+    dim3 grid;
+    const int rc = laid_out<16 * NT, D>(ctx, a, true, args, grid);
+    if (rc != ADADIM_OK) return rc;
+    ProfScope prof(ctx, "mx4_attend_few");
+    hipLaunchKernelGGL((mx4_attend_few<T, D, NT>), grid, dim3(64 * AT_WAVES), 0, ctx->stream, args);
+    ADADIM_LAUNCH_CHECK(ctx, "mx4_attend_few");
+    return ADADIM_OK;
+}
+
+template <class T, int D>
+int launch_tiles(adadim_ctx* ctx, const Attention& a) {
+    static PerDeviceOnce once;
+    ADADIM_HIP_TRY(ctx, once.run([] {
+        return hipFuncSetAttribute(reinterpret_cast<const void*>(&mx4_attend_tiles<T, D>), hipFuncAttributeMaxDynamicSharedMemorySize, Stage<D>::LDS);
+    }));
+    AttentionArgs args;
+    dim3 grid;
+    const int rc = laid_out<TL_WAVES * 32, D>(ctx, a, false, args, grid);
+    if (rc != ADADIM_OK) return rc;
+    ProfScope prof(ctx, "mx4_attend_tiles");
+    hipLaunchKernelGGL((mx4_attend_tiles<T, D>), grid, dim3(64 * TL_WAVES), Stage<D>::LDS, ctx->stream, args);
+    ADADIM_LAUNCH_CHECK(ctx, "mx4_attend_tiles");
     return ADADIM_OK;
 }
 
 template <class T, int D>
 int launch_head(adadim_ctx* ctx, const Attention& a) {
     const int64_t rows = a.max_new * a.group;
-    if (rows <= 16) return launch_form<T, D, 1, true>(ctx, a);
-    if (rows <= 32) return launch_form<T, D, 2, true>(ctx, a);
-    if constexpr (D <= 128) {
-        if (rows <= 64) return launch_form<T, D, 4, true>(ctx, a);
-        return launch_form<T, D, 4, false>(ctx, a);
-    } else
-        return launch_form<T, D, 2, false>(ctx, a);
+    if (rows <= 16) return launch_few<T, D, 1>(ctx, a);
+    if (rows <= 64) {
+        if constexpr (D <= 128) return launch_few<T, D, 2>(ctx, a);
+        else return launch_few<T, D, 1>(ctx, a);
+    }
+    return launch_tiles<T, D>(ctx, a);
 }
 
 template <class T>

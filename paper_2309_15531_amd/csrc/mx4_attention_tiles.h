@@ -1,0 +1,243 @@
+// Attention of many rows over a paged cache in mx4 (the mathematics: mx4_attention.h).
+//
+// A workgroup has eight waves, two a SIMD, of 32 rows each: while one weighs scores on the vector unit the other multiplies.  Its records go
+// through LDS four at a time, each converted by two of the waves, one its keys and one its values: what costs most to prepare, the
+// values of codes with their scales, is done once for all 256 rows.  They lie there as the 32-row instruction takes
+// its left operand, lane by lane in 16 bytes (no bank is met twice in a read): keys [step][half][position], with step s of half h the
+// elements h D/2 + 8 s ..; values [tile jj][step][half][row r], with row r of tile jj the element (D/16) (r % 16) + (D/32) (r / 16) + jj, and
+// the step's positions 4 h .. and 8 + 4 h .. of 16 as S^T leaves them in a lane of half h.
+#pragma once
+
+#include "mx4_attention.h"
+
+namespace mx4 {
+
+template <class T> struct Dots32;
+template <> struct Dots32<_Float16> {
+    static __device__ __forceinline__ float16v mfma(half8v a, half8v b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct Dots32<__bf16> {
+    static __device__ __forceinline__ float16v mfma(bf8v a, bf8v b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+
+constexpr int TL_WAVES = 8;
+
+template <int D>
+struct Stage {
+    static constexpr int KEYS = 64 * D, BYTES = 128 * D;      // of a record: its keys' part, all
+    static constexpr int RECORDS = 4, BUFFERS = D > 128 ? 1 : 2;
+    static constexpr int LDS = BUFFERS * RECORDS * BYTES;
+};
+
+// A record's keys to their places in LDS.
+template <class T, int D>
+__device__ __forceinline__ void convert_keys(const KeyBytes<D>& b, uint8_t* to, int lane) {
+    constexpr int W = D / 32;
+    const int m = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+            *reinterpret_cast<typename Dots<T>::vec*>(to + ((((g & 1) * W + w) * 2 + (g >> 1)) * 32 + 16 * t + m) * 16) = Dots<T>::keys(b.words[t][w], b.scale(t, w));
+}
+
+// Its values; have: positions that exist.
+template <int D>
+__device__ __forceinline__ void convert_values(const ValueBytes<D>& b, uint8_t* to, int lane, int have) {
+    const int m = lane & 15, g = lane >> 4;
+    float vs[8];
+    b.scales(vs, g, have);
+    uint8_t* const v0 = to + Stage<D>::KEYS + ((g & 1) * 32 + m) * 16 + (g >> 1) * 8;
+#pragma unroll
+    for (int u = 0; u < D / 32; ++u) {
+        half8v both[2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const half2v v = b.pair(i, u, vs[i]);
+            both[0][i] = v.x;
+            both[1][i] = v.y;
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int j = 2 * u + x, jj = j % (D / 32), high = j / (D / 32);                              // the unit's element j
+            typedef _Float16 half4v __attribute__((ext_vector_type(4)));
+            uint8_t* const p = v0 + (jj * 128 + high * 16) * 16;
+            *reinterpret_cast<half4v*>(p) = half4v{both[x][0], both[x][1], both[x][2], both[x][3]};
+            *reinterpret_cast<half4v*>(p + 64 * 16) = half4v{both[x][4], both[x][5], both[x][6], both[x][7]};
+        }
+    }
+}
+
+template <class T, int D>
+struct Tiles32 {
+    static constexpr int STEPS = D / 16, OT = D / 32;
+    typedef typename Dots<T>::vec vec;
+    vec q[STEPS];
+    float16v o[OT];
+    float m, l, c;
+
+    __device__ __forceinline__ float16v scores(const uint8_t* r, int lane) const {
+        float16v s = {};
+#pragma unroll
+        for (int k = 0; k < STEPS; ++k) s = Dots32<T>::mfma(*reinterpret_cast<const vec*>(r + (k * 64 + lane) * 16), q[k], s);
+        return s;
+    }
+    __device__ __forceinline__ void raise(const float16v& s) {
+        float top = fmaxf(s[0], s[1]);
+#pragma unroll
+        for (int i = 2; i < 16; ++i) top = fmaxf(top, s[i]);
+        top *= c;
+        if (__any(top > m + RAISE)) {
+            const float up = fmaxf(m, fmaxf(top, __shfl_xor(top, 32))), by = __builtin_amdgcn_exp2f(m - up);
+            m = up;
+            l *= by;
+#pragma unroll
+            for (int j = 0; j < OT; ++j) o[j] *= by;
+        }
+    }
+    __device__ __forceinline__ void weigh(const float16v& s, half8v (&p)[2]) {
+        const float base = HEAD - m;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, base));
+            l += e;
+            p[i >> 3][i & 7] = static_cast<_Float16>(e);
+        }
+    }
+    __device__ __forceinline__ void values(const uint8_t* r, int lane, const half8v (&p)[2]) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int j = 0; j < OT; ++j)
+                o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8v*>(r + Stage<D>::KEYS + ((j * 2 + k) * 64 + lane) * 16), p[k], o[j], 0, 0, 0);
+    }
+};
+
+template <class T, int D>
+__global__ __launch_bounds__(64 * TL_WAVES, 2) void mx4_attend_tiles(AttentionArgs args) {
+    const Attention& a = args.a;
+    constexpr int WROWS = 32, R = TL_WAVES * WROWS, N = D / 16;
+    constexpr int BUFFERS = Stage<D>::BUFFERS, RECORDS = Stage<D>::RECORDS, BYTES = Stage<D>::BYTES;
+    extern __shared__ __attribute__((aligned(16))) uint8_t s_stage[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+    const Work w = work_of<R>(args);
+    if (w.shares == 0) return;
+
+    // ---- the wave's rows and the records that they see
+    const int w_row = WROWS * wave, w_last = min(w_row + WROWS, w.tr.rows) - 1;                           // (w_last < w_row: none)
+    const int row = min(w_row + (lane & 31), w.tr.rows - 1), token = w.token_of(a, row);                  // (rows that are not there repeat the last one)
+    const int t_first = w.token_of(a, min(w_row, w.tr.rows - 1)), t_last = w.token_of(a, max(w_last, 0));
+    const int from = w_last < w_row ? w.end : w.sees_from(a, t_first) >> 5;
+    const int to = w_last < w_row ? w.begin : min((w.sees_to(a, t_last) + 31) >> 5, w.end);
+    const int all_from = (w.sees_from(a, t_last) + 31) >> 5, all_to = w.sees_to(a, t_first) >> 5;         // (these hide nothing from any row)
+    const int lo = w.sees_from(a, token), hi = w.sees_to(a, token);
+    Tiles32<T, D> t;
+    t.c = a.scale * 1.44269504088896340736f;
+    t.m = LOWEST;
+    t.l = 0.0f;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) t.o[j] = float16v{};
+    {
+        const T* q = static_cast<const T*>(a.Q) + (w.tr.first - w.tr.token + token) * a.ldq + int64_t(w.head_of(a, row)) * a.dim;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+            const int d = (D / 2) * h + 8 * k;
+            t.q[k] = d < a.dim ? __builtin_bit_cast(typename Dots<T>::vec, Chunk<T, 8>::load(q + d, a.dim - d)) : typename Dots<T>::vec{};
+        }
+    }
+
+    const int32_t* const table = a.table + int64_t(w.tr.sequence) * a.width;
+    const int per_page = a.log_page - 5;
+    auto page_of = [&](int r) { return r < w.end ? table[r >> per_page] : -1; };
+    auto there = [&](int page) { return uint32_t(page) < uint64_t(a.pages); };
+    // the wave's part of a stage: the keys of a record or its values
+    const int part = wave & 3;
+    const bool keys = wave < 4;
+    KeyBytes<D> kb;
+    ValueBytes<D> vb;
+    auto fetch = [&](int first) {
+        const int r = first + part;
+        if (r >= w.end) return;
+        const int page = page_of(r);
+        const int64_t p = there(page) ? page : 0;             // (a page that is not there is not used; page 0 is)
+        const uint8_t* const rec = a.cache + (((p * a.heads + w.head) << per_page) + (r & ((1 << per_page) - 1))) * Record<D>::BYTES;
+        if (keys) kb.load(rec, lane);
+        else vb.load(rec, lane);
+    };
+    auto bring = [&](int first, int buffer) {
+        const int r = first + part;
+        if (r >= w.end) return;
+        uint8_t* const at = s_stage + (buffer * RECORDS + part) * BYTES;
+        if (keys) convert_keys<T, D>(kb, at, lane);
+        else convert_values<D>(vb, at, lane, w.length - RECORD * r);
+    };
+    auto stage = [&](int first, int buffer) {
+        const uint8_t* const at = s_stage + buffer * RECORDS * BYTES;
+        const int r1 = min(first + RECORDS, to);
+        for (int r = max(first, from); r < r1; ++r) {
+            if (!there(page_of(r))) continue;
+            const uint8_t* const rec = at + (r - first) * BYTES;
+            float16v s = t.scores(rec, lane);
+            if (r < all_from || r >= all_to) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int key = RECORD * r + 8 * (i >> 2) + 4 * h + (i & 3);
+                    s[i] = key >= lo && key < hi ? s[i] : -INFINITY;
+                }
+            }
+            t.raise(s);
+            half8v p[2];
+            t.weigh(s, p);
+            t.values(rec, lane, p);
+        }
+    };
+    fetch(w.begin);
+    bring(w.begin, 0);
+    fetch(w.begin + RECORDS);
+    __syncthreads();
+    int buffer = 0;
+    for (int first = w.begin; first < w.end; first += RECORDS) {
+        if constexpr (BUFFERS == 2) {
+            bring(first + RECORDS, buffer ^ 1);
+            fetch(first + 2 * RECORDS);
+            stage(first, buffer);
+            __syncthreads();
+            buffer ^= 1;
+        } else {
+            stage(first, 0);
+            __syncthreads();
+            bring(first + RECORDS, 0);
+            fetch(first + 2 * RECORDS);
+            __syncthreads();
+        }
+    }
+
+    // ---- out
+    float* const mine = args.parts + (int64_t(blockIdx.x) * gridDim.y + blockIdx.y) * (R * PART<D>);
+    const float l = t.l + __shfl_xor(t.l, 32), by = l == 0.0f ? 0.0f : 1.0f / l;
+    if (w_row + (lane & 31) <= w_last) {
+        const int64_t y = w.row_of_y(a, row);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int d = N * (8 * (i >> 2) + 4 * h + (i & 3));
+            float v[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = t.o[j % (D / 32)][i + 8 * (j / (D / 32))];
+            if (w.shares > 1) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) put(mine + row * PART<D> + d + j, v[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[j] = l == 0.0f ? 0.0f : v[j] * by;
+                store_row(a, y, d, v);
+            }
+        }
+        if (w.shares > 1 && h == 0) {
+            put(mine + row * PART<D> + D, t.m);
+            put(mine + row * PART<D> + D + 1, l);
+        }
+    }
+    if (w.shares > 1) join<R, D, TL_WAVES>(args, w);
+}
+
+}  // namespace mx4
