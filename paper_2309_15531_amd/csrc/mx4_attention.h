@@ -1,14 +1,14 @@
 // Attention over a paged cache in mx4:  y = sum_j softmax_j(scale q . k_j) v_j  over the positions j that a query sees.
 //
-// A tile is 16 NT rows (a row: one query head of one new token) of a sequence that share a key-value head.  A wave goes over records of 32
-// positions:  S^T = K Q^T, 2 tiles of 16 positions by NT tiles of 16 rows, keys converted in registers to the queries' type (exact:
+// A tile is a number of rows (a row: one query head of one new token) of a sequence that share a key-value head.  A wave goes over records of 32
+// positions:  S^T = K Q^T, keys converted in registers to the queries' type (exact:
 // 2 bits and fp16's or bf16's exponents), then p = 2^(scale log2(e) s - m + 8) in fp32, rounded to fp16 (11 bits; with the
 // 2^8 the smallest number that fp16 still holds is 2^-33 of the row's largest), and O^T += V^T P^T with the values in fp16 (exact).  Positions
 // lie along a lane's registers and rows along the lanes in S^T and in O^T: neither is turned round, and a row's maximum and
 // sum are numbers of its lanes.  The maximum m is only raised (and O^T and the sum scaled) where a score passes it by more than 7:
 // p stays below 2^15.  The sum is of p before rounding.  Scores, sums and O^T are fp32.
 //
-// Few rows (this file): the four waves of a workgroup have the same rows and take records in turn; their sums meet in LDS.  Many rows:
+// Few rows (this file): the waves of a workgroup have the same rows and take records in turn; their sums meet in LDS.  Many rows:
 // mx4_attention_tiles.h.  Either way a tile's records may be shared between workgroups (gridDim.y); partial sums travel as relaxed atomics at
 // device scope, and the workgroup that finishes last joins them in their order: same bits every run.
 #pragma once
@@ -17,7 +17,7 @@
 
 namespace mx4 {
 
-constexpr int AT_WAVES = 4;
+constexpr int AT_WAVES = 8;                       // of a workgroup of few rows
 constexpr int AT_TICKETS = 8192;                  // tiles that may be shared
 constexpr float LOWEST = -3e38f;                  // a maximum before the first score
 constexpr float RAISE = 7.0f, HEAD = 8.0f;
@@ -42,49 +42,43 @@ template <> struct Dots<__bf16> {
     static __device__ __forceinline__ float4v mfma(vec a, vec b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 
-// The bytes of a record's keys that a lane of row m and quarter g needs: of positions m and 16 + m the elements (D/4) g ...
+// The bytes of a record's keys that a lane of row m and quarter g needs: of position 16 t + m the elements (D/4) g ..
 template <int D>
 struct KeyBytes {
     static constexpr int W = D / 32;
-    uint32_t words[2][W], scale_bytes[2];
-    __device__ __forceinline__ void load(const uint8_t* r, int lane) {
-        const int m = lane & 15, g = lane >> 4;
+    uint32_t words[W], scale_bytes;
+    __device__ __forceinline__ void load(const uint8_t* r, int t, int lane) {
+        const int key = 16 * t + (lane & 15), g = lane >> 4;
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(r + key * (D / 2) + g * (D / 8));
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int key = 16 * t + m;
-            const uint32_t* p = reinterpret_cast<const uint32_t*>(r + key * (D / 2) + g * (D / 8));
-#pragma unroll
-            for (int c = 0; c < W; ++c) words[t][c] = p[c];
-            if constexpr (D == 256) scale_bytes[t] = *reinterpret_cast<const uint16_t*>(r + Record<D>::KEY_SCALES + key * 8 + 2 * g);
-            else scale_bytes[t] = r[Record<D>::KEY_SCALES + key * W + g * W / 4];
-        }
+        for (int c = 0; c < W; ++c) words[c] = p[c];
+        if constexpr (D == 256) scale_bytes = *reinterpret_cast<const uint16_t*>(r + Record<D>::KEY_SCALES + key * 8 + 2 * g);
+        else scale_bytes = r[Record<D>::KEY_SCALES + key * W + g * W / 4];
     }
-    __device__ __forceinline__ float scale(int t, int w) const {
-        return scale_operand(D == 256 ? w < 4 ? scale_bytes[t] & 255u : scale_bytes[t] >> 8 : scale_bytes[t]);
+    __device__ __forceinline__ float scale(int w) const {
+        return scale_operand(D == 256 ? w < 4 ? scale_bytes & 255u : scale_bytes >> 8 : scale_bytes);
     }
 };
 
-// Of its values: the elements m D/16 .. of the 8 positions of quarter g.
+// Of its values: the elements m D/16 .. of the positions 16 t + 4 g .. (four).
 template <int D>
 struct ValueBytes {
     static constexpr int W = D / 32;
-    uint32_t words[D / 16], scale_words[2];
-    __device__ __forceinline__ void load(const uint8_t* r, int lane) {
+    uint32_t words[W], scale_word;
+    __device__ __forceinline__ void load(const uint8_t* r, int t, int lane) {
         const int m = lane & 15, g = lane >> 4;
-        const uint32_t* p = reinterpret_cast<const uint32_t*>(r + Record<D>::VALUES + (g * 16 + m) * (8 * Record<D>::UNIT));
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(r + Record<D>::VALUES + ((g * 16 + m) * 8 + 4 * t) * Record<D>::UNIT);
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) words[c] = p[c];
-        const uint32_t* s = reinterpret_cast<const uint32_t*>(r + Record<D>::VALUE_SCALES + (g * W + m * W / 16) * 8);
-        scale_words[0] = s[0];
-        scale_words[1] = s[1];
+        for (int c = 0; c < W; ++c) words[c] = p[c];
+        scale_word = *reinterpret_cast<const uint32_t*>(r + Record<D>::VALUE_SCALES + (g * W + m * W / 16) * 8 + 4 * t);
     }
-    // the 8 positions' scales; those that do not exist (have: how many do) become zeros whatever their codes: 2^-127 in fp16
-    __device__ __forceinline__ void scales(float (&v)[8], int g, int have) const {
+    // the positions' scales; those that do not exist (have: how many of the record do) become zeros whatever their codes: 2^-127 in fp16
+    __device__ __forceinline__ void scales(float (&v)[4], int t, int g, int have) const {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = scale_operand((scale_words[i >> 2] >> (8 * (i & 3))) & 255u);
+        for (int i = 0; i < 4; ++i) v[i] = scale_operand((scale_word >> (8 * i)) & 255u);
         if (have < RECORD) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = 4 * g + (i < 4 ? i : 12 + i) < have ? v[i] : 0.0f;
+            for (int i = 0; i < 4; ++i) v[i] = 16 * t + 4 * g + i < have ? v[i] : 0.0f;
         }
     }
     // elements 2 u and 2 u + 1 of position i
@@ -106,101 +100,70 @@ __device__ __forceinline__ float quarters(float v, F f) {
     return f(v, __shfl_xor(v, 32));
 }
 
-template <class T, int D, int NT>
+template <class T, int D>
 struct Rows {
     static constexpr int W = D / 32, TILES = D / 16;
     typedef typename Dots<T>::vec vec;
-    vec q[NT][W];
-    float4v o[NT][TILES];
-    float m[NT], l[NT];                           // m: largest score so far, times c, of all quarters; l: sum of this lane's p
+    float4v o[TILES];
+    float m, l;                                   // m: largest score so far, times c, of all quarters; l: sum of this lane's p
     float c;                                      // scale log2(e)
 
-    __device__ __forceinline__ void clear() {
+    // q: the rows of Q in LDS, 64 lanes' 16 bytes for each of the W instructions
+    static __device__ __forceinline__ void scores(const KeyBytes<D> (&b)[2], const vec* q, int lane, float4v (&s)[2]) {
+        s[0] = s[1] = float4v{0, 0, 0, 0};
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            m[n] = LOWEST;
-            l[n] = 0.0f;
+        for (int w = 0; w < W; ++w) {
+            const vec x = q[w * 64 + lane];
 #pragma unroll
-            for (int j = 0; j < TILES; ++j) o[n][j] = float4v{0, 0, 0, 0};
+            for (int t = 0; t < 2; ++t) s[t] = Dots<T>::mfma(Dots<T>::keys(b[t].words[w], b[t].scale(w)), x, s[t]);
         }
     }
-
-    // lo, hi: the positions that the rows see, counted from the record's first; have: how many of it exist
-    __device__ __forceinline__ void add(const KeyBytes<D>& kb, const ValueBytes<D>& vb, int lane, bool mask, const int (&lo)[NT], const int (&hi)[NT], int have) {
-        const int g = lane >> 4;
-        float4v s[NT][2];
+    // what lies outside lo .. hi; first: the record's first position
+    static __device__ __forceinline__ void hide(float4v (&s)[2], int g, int lo, int hi, int first) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) s[n][t] = float4v{0, 0, 0, 0};
-#pragma unroll
-            for (int w = 0; w < W; ++w) {
-                const vec k = Dots<T>::keys(kb.words[t][w], kb.scale(t, w));
-#pragma unroll
-                for (int n = 0; n < NT; ++n) s[n][t] = Dots<T>::mfma(k, q[n][w], s[n][t]);
+            for (int i = 0; i < 4; ++i) {
+                const int at = first + 16 * t + 4 * g + i;
+                s[t][i] = at >= lo && at < hi ? s[t][i] : -INFINITY;
             }
+    }
+    __device__ __forceinline__ void weigh(const float4v (&s)[2], half8v& p) {
+        const float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))) * c;
+        if (__any(top > m + RAISE)) {
+            const float up = fmaxf(m, quarters(top, [](float x, float y) { return fmaxf(x, y); }));
+            const float by = __builtin_amdgcn_exp2f(m - up);
+            m = up;
+            l *= by;
+#pragma unroll
+            for (int j = 0; j < TILES; ++j) o[j] *= by;
         }
-        __builtin_amdgcn_sched_barrier(0);        // (keys' and values' operands are not held at the same time)
-        if (mask) {
+        const float base = HEAD - m;
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int at = 16 * t + 4 * g + i;
-                        s[n][t][i] = at >= lo[n] && at < hi[n] ? s[n][t][i] : -INFINITY;
-                    }
-        }
-        float top[NT];
-        bool raise = false;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            top[n] = fmaxf(fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3])),
-                           fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3]))) * c;
-            raise = raise || top[n] > m[n] + RAISE;
-        }
-        if (__any(raise)) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const float up = fmaxf(m[n], quarters(top[n], [](float x, float y) { return fmaxf(x, y); }));
-                const float by = __builtin_amdgcn_exp2f(m[n] - up);
-                m[n] = up;
-                l[n] *= by;
-#pragma unroll
-                for (int j = 0; j < TILES; ++j) o[n][j] *= by;
+            for (int i = 0; i < 4; ++i) {
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], c, base));
+                l += e;
+                p[4 * t + i] = static_cast<_Float16>(e);
             }
-        }
-        half8v p[NT];
+    }
+    // have: how many positions of the record exist
+    __device__ __forceinline__ void values(const ValueBytes<D> (&b)[2], int g, int have, const half8v& p) {
+        float vs[2][4];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const float base = HEAD - m[n];
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][t][i], c, base));
-                    l[n] += e;
-                    p[n][4 * t + i] = static_cast<_Float16>(e);
-                }
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        float vs[8];
-        vb.scales(vs, g, have);
+        for (int t = 0; t < 2; ++t) b[t].scales(vs[t], t, g, have);
 #pragma unroll
         for (int u = 0; u < D / 32; ++u) {
             half8v even, odd;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const half2v v = vb.pair(i, u, vs[i]);
+                const half2v v = b[i >> 2].pair(i & 3, u, vs[i >> 2][i & 3]);
                 even[i] = v.x;
                 odd[i] = v.y;
             }
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                o[n][2 * u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(even, p[n], o[n][2 * u], 0, 0, 0);
-                o[n][2 * u + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(odd, p[n], o[n][2 * u + 1], 0, 0, 0);
-            }
+            o[2 * u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(even, p, o[2 * u], 0, 0, 0);
+            o[2 * u + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(odd, p, o[2 * u + 1], 0, 0, 0);
         }
     }
 };
@@ -228,8 +191,17 @@ __device__ __forceinline__ void store_row(const Attention& a, int64_t at, int d,
     }
 }
 
-__device__ __forceinline__ void put(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ float get(const float* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// Partial sums on their way past the L2s, where all XCDs meet: two numbers at a time.
+typedef float float2p __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void put(float* p, float x, float y) {
+    __hip_atomic_store(reinterpret_cast<uint64_t*>(p), __builtin_bit_cast(uint64_t, float2p{x, y}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2p get(const float* p) {
+    return __builtin_bit_cast(float2p, __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+
+// What all lanes have the same goes into a scalar register: branches and loads by it are scalar then.  (Quotients come from the vector unit.)
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // The rows of tile `tile` of R rows: sequence s has the tiles from offsets[s] * group / R + s on (enough for it: each begins one of its own).
 struct TileRows {
@@ -239,30 +211,40 @@ struct TileRows {
     int rest;                                     // its head within the group
     int added;                                    // the sequence's new tokens
     int sequence;
+    int length;                                   // its positions
 };
 template <int R>
 __device__ __forceinline__ TileRows tile_rows(const Attention& a, int tile) {
     const int lane = threadIdx.x & 63;
-    auto offset = [&](int s) { return min(max(int64_t(a.offsets[s]), int64_t(0)), a.tokens); };
-    auto begin = [&](int s) { return offset(s) * a.group / R + s; };
-    int lo = 0, n = a.sequences;                  // the last of the n from lo on that begins at or before the tile
-    while (n > 1) {
-        const int step = (n + 63) / 64, s = lo + lane * step;
-        const uint64_t at = __ballot(s < lo + n && begin(min(s, a.sequences)) <= tile);
+    auto offset = [&](int s) { return static_cast<int>(min(max(int64_t(a.offsets[s]), int64_t(0)), a.tokens)); };
+    auto begin = [&](int o, int s) { return static_cast<int>(int64_t(o) * a.group / R) + s; };
+    int lo = 0, n = a.sequences, o0, o1, length;  // the last of the n from lo on that begins at or before the tile
+    while (n > 63) {
+        const int step = (n + 63) / 64, s = min(lo + lane * step, a.sequences);
+        const uint64_t at = __ballot(s < lo + n && begin(offset(s), s) <= tile);
         const int last = at ? 63 - __builtin_clzll(at) : 0;
         n = min(step, n - last * step);
         lo += last * step;
     }
-    const int64_t o0 = offset(lo), o1 = offset(lo + 1);
-    const int64_t r0 = (tile - begin(lo)) * R, have = (o1 - o0) * a.group;
-    TileRows t;
-    t.sequence = __builtin_amdgcn_readfirstlane(lo);
-    t.added = __builtin_amdgcn_readfirstlane(static_cast<int>(max(o1 - o0, int64_t(0))));
+    {                                             // what is left, and all of it that is needed, in one load of each array
+        const int s = lo + min(lane, n), o = offset(s), l = a.lengths[min(s, a.sequences - 1)];
+        const uint64_t at = __ballot(lane < n && begin(o, s) <= tile);
+        const int last = at ? 63 - __builtin_clzll(at) : 0;
+        o0 = __builtin_amdgcn_readlane(o, last);
+        o1 = __builtin_amdgcn_readlane(o, last + 1);
+        length = __builtin_amdgcn_readlane(l, last);
+        lo += last;
+    }
+    const int64_t r0 = int64_t(tile - begin(o0, lo)) * R, have = int64_t(o1 - o0) * a.group;
     const bool ok = r0 >= 0 && r0 < have;
-    t.rows = __builtin_amdgcn_readfirstlane(ok ? static_cast<int>(min(int64_t(R), have - r0)) : 0);
-    t.token = __builtin_amdgcn_readfirstlane(ok ? static_cast<int>(r0 / a.group) : 0);
-    t.rest = __builtin_amdgcn_readfirstlane(ok ? static_cast<int>(r0 % a.group) : 0);
-    t.first = o0 + t.token;
+    TileRows t;
+    t.sequence = uniform(lo);
+    t.length = uniform(static_cast<int>(min(max(int64_t(length), int64_t(0)), a.width << a.log_page)));
+    t.added = uniform(max(o1 - o0, 0));
+    t.rows = uniform(ok ? static_cast<int>(min(int64_t(R), have - r0)) : 0);
+    t.token = uniform(ok ? static_cast<int>(r0 / a.group) : 0);
+    t.rest = uniform(ok ? static_cast<int>(r0 % a.group) : 0);
+    t.first = uniform(o0) + t.token;
     return t;
 }
 
@@ -289,23 +271,25 @@ __device__ __forceinline__ Work work_of(const AttentionArgs& args) {
     w.head = blockIdx.x % a.heads;
     w.tr = tile_rows<R>(a, args.tiles - 1 - static_cast<int>(blockIdx.x / a.heads));         // (the longest rows first)
     if (w.tr.rows == 0) return w;
-    w.length = static_cast<int>(min(max(int64_t(a.lengths[w.tr.sequence]), int64_t(0)), a.width << a.log_page));
+    w.length = w.tr.length;
     w.before = w.length - w.tr.added;
-    const int begin = w.sees_from(a, w.tr.token) >> 5, end = (w.sees_to(a, w.token_of(a, w.tr.rows - 1)) + 31) >> 5;
+    const int begin = uniform(w.sees_from(a, w.tr.token) >> 5), end = uniform((w.sees_to(a, w.token_of(a, w.tr.rows - 1)) + 31) >> 5);
     const int records = max(end - begin, 0), y = static_cast<int>(blockIdx.y), ny = static_cast<int>(gridDim.y);
-    const int share = max((records + ny - 1) / ny, args.least);
-    const int shares = max((records + share - 1) / share, 1);
+    const int share = uniform(max((records + ny - 1) / ny, args.least));
+    const int shares = uniform(max((records + share - 1) / share, 1));
     w.shares = y < shares ? shares : 0;
     w.begin = begin + share * y;
     w.end = min(w.begin + share, end);
     return w;
 }
 
-// Partial sums: per tile, head and share [R rows][D + 2], the sums, then m and l.  Who finishes last joins the shares.
+// Partial sums: per tile, head and share [R rows][D + 2], the sums, then m and l.  Who finishes last joins the shares: 16 lanes a row, whose
+// lane x has the elements 64 j + 4 x .. and first the m and l of the shares x, x + 16, ..
 template <int D> constexpr int PART = D + 2;
+constexpr int MOST_SHARES = 64;
 template <int R, int D, int WAVES>
 __device__ __forceinline__ void join(const AttentionArgs& args, const Work& w) {
-    constexpr int N = D / 16;
+    constexpr int N = D / 64, AT_ONCE = 4;
     __shared__ unsigned s_ticket;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
@@ -314,151 +298,184 @@ __device__ __forceinline__ void join(const AttentionArgs& args, const Work& w) {
     if (s_ticket != unsigned(w.shares) - 1) return;
     if (threadIdx.x == 0) __hip_atomic_store(args.tickets + blockIdx.x, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     const float* const all = args.parts + int64_t(blockIdx.x) * gridDim.y * (R * PART<D>);
-    const int d0 = (threadIdx.x & 15) * N;
-    for (int row = threadIdx.x >> 4; row < w.tr.rows; row += 4 * WAVES) {
+    const int x = threadIdx.x & 15, lane0 = threadIdx.x & 48;
+    for (int row0 = 0; row0 < w.tr.rows; row0 += 4 * WAVES) {
+        const int row = min(row0 + static_cast<int>(threadIdx.x >> 4), w.tr.rows - 1);
         const float* const p = all + row * PART<D>;
-        float m = LOWEST, l = 0.0f, v[N];
-        for (int z = 0; z < w.shares; ++z) m = fmaxf(m, get(p + int64_t(z) * (R * PART<D>) + D));
+        float by[MOST_SHARES / 16], m = LOWEST, l = 0.0f;
+        float2p ml[MOST_SHARES / 16];
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = 0.0f;
-        for (int z = 0; z < w.shares; ++z) {
-            const float* const q = p + int64_t(z) * (R * PART<D>);
-            const float by = __builtin_amdgcn_exp2f(get(q + D) - m);
-            l += get(q + D + 1) * by;
+        for (int i = 0; i < MOST_SHARES / 16; ++i) ml[i] = 16 * i + x < w.shares ? get(p + int64_t(16 * i + x) * (R * PART<D>) + D) : float2p{LOWEST, 0.0f};
 #pragma unroll
-            for (int j = 0; j < N; ++j) v[j] += get(q + d0 + j) * by;
+        for (int i = 0; i < MOST_SHARES / 16; ++i) m = fmaxf(m, ml[i].x);
+#pragma unroll
+        for (int d = 1; d < 16; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+#pragma unroll
+        for (int i = 0; i < MOST_SHARES / 16; ++i) {
+            by[i] = __builtin_amdgcn_exp2f(ml[i].x - m);
+            l += ml[i].y * by[i];
         }
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = l == 0.0f ? 0.0f : v[j] / l;
-        store_row(args.a, w.row_of_y(args.a, row), d0, v);
+        for (int d = 1; d < 16; d *= 2) l += __shfl_xor(l, d);
+        float v[N][4];
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[j][k] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < MOST_SHARES / 16; ++i)
+            for (int z0 = 16 * i; z0 < min(16 * i + 16, w.shares); z0 += AT_ONCE) {
+                float2p part[AT_ONCE][N][2];
+#pragma unroll
+                for (int z = 0; z < AT_ONCE; ++z)
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            part[z][j][k] = float2p{0.0f, 0.0f};
+                            if (z0 + z < w.shares) part[z][j][k] = get(p + int64_t(z0 + z) * (R * PART<D>) + 64 * j + 4 * x + 2 * k);
+                        }
+#pragma unroll
+                for (int z = 0; z < AT_ONCE; ++z) {
+                    const float f = __shfl(by[i], lane0 + ((z0 + z) & 15));
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) v[j][k] += part[z][j][k >> 1][k & 1] * f;
+                }
+            }
+        if (row0 + static_cast<int>(threadIdx.x >> 4) >= w.tr.rows) continue;
+        const int64_t y = w.row_of_y(args.a, row);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[j][k] = l == 0.0f ? 0.0f : v[j][k] / l;
+            store_row(args.a, y, 64 * j + 4 * x, v[j]);
+        }
     }
 }
 
 // Waves of a SIMD that the registers have to leave room for.
-template <int D, int NT> constexpr int FEW_WAVES = NT == 1 ? (D == 64 ? 4 : D == 128 ? 3 : 1) : D == 64 ? 3 : 2;
+template <int D> constexpr int FEW_WAVES = D <= 128 ? 4 : 2;
 
-template <class T, int D, int NT>
-__global__ __launch_bounds__(64 * AT_WAVES, (FEW_WAVES<D, NT>)) void mx4_attend_few(AttentionArgs args) {
+template <class T, int D>
+__global__ __launch_bounds__(64 * AT_WAVES, FEW_WAVES<D>) void mx4_attend_few(AttentionArgs args) {
     const Attention& a = args.a;
-    constexpr int R = 16 * NT, TILES = D / 16;
+    constexpr int R = 16, TILES = D / 16, W = D / 32;
+    typedef typename Dots<T>::vec vec;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
     const Work w = work_of<R>(args);
     if (w.shares == 0) return;
     int b = w.begin + wave;
     const int e = w.end;
-    const int t_last = w.token_of(a, w.tr.rows - 1);
-    // records from all_from to before all_to hide nothing from any row
-    const int all_from = (w.sees_from(a, t_last) + 31) >> 5, all_to = w.sees_to(a, w.tr.token) >> 5;
-
-    Rows<T, D, NT> rows;
-    rows.c = a.scale * 1.44269504088896340736f;
-    rows.clear();
-    int lo[NT], hi[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int row = min(16 * n + (lane & 15), w.tr.rows - 1);             // (rows that are not there repeat the last one)
-        const int t = w.token_of(a, row);
-        lo[n] = w.sees_from(a, t);
-        hi[n] = w.sees_to(a, t);
-        const T* q = static_cast<const T*>(a.Q) + (w.tr.first - w.tr.token + t) * a.ldq + int64_t(w.head_of(a, row)) * a.dim;
-#pragma unroll
-        for (int k = 0; k < D / 32; ++k) {
-            const int d = (D / 4) * g + 8 * k;
-            rows.q[n][k] = d < a.dim ? __builtin_bit_cast(typename Dots<T>::vec, Chunk<T, 8>::load(q + d, a.dim - d)) : typename Dots<T>::vec{};
-        }
-    }
     const int32_t* const table = a.table + int64_t(w.tr.sequence) * a.width;
     const int per_page = a.log_page - 5;
     auto page_of = [&](int r) { return r < e ? table[r >> per_page] : -1; };
+    auto there = [&](int page) { return uint32_t(page) < uint64_t(a.pages); };
     auto record = [&](int page, int r) {
-        const int64_t p = uint32_t(page) < uint64_t(a.pages) ? page : 0;      // (a page that is not there is not used; page 0 is)
+        const int64_t p = there(page) ? page : 0;             // (a page that is not there is not used; page 0 is)
         return a.cache + (((p * a.heads + w.head) << per_page) + (r & ((1 << per_page) - 1))) * Record<D>::BYTES;
     };
-    KeyBytes<D> k_now, k_next;
-    ValueBytes<D> v_now, v_next;
     int page = page_of(b), page1 = page_of(b + AT_WAVES);
+    KeyBytes<D> kb[2];
+    ValueBytes<D> vb[2];
+    auto load_keys = [&](const uint8_t* r) { kb[0].load(r, 0, lane); kb[1].load(r, 1, lane); };
+    auto load_values = [&](const uint8_t* r) { vb[0].load(r, 0, lane); vb[1].load(r, 1, lane); };
     if (b < e) {
-        k_now.load(record(page, b), lane);
-        v_now.load(record(page, b), lane);
+        load_keys(record(page, b));
+        load_values(record(page, b));
     }
-    for (; b < e; b += AT_WAVES) {
-        const int page2 = page_of(b + 2 * AT_WAVES);
-        if (b + AT_WAVES < e) {
-            k_next.load(record(page1, b + AT_WAVES), lane);
-            v_next.load(record(page1, b + AT_WAVES), lane);
-        }
-        if (uint32_t(page) < uint64_t(a.pages)) {
-            int from[NT], to[NT];
+
+    // ---- the rows: every wave has the same
+    __shared__ vec s_q[W * 64];
+    Rows<T, D> rows;
+    rows.c = a.scale * 1.44269504088896340736f;
+    rows.m = LOWEST;
+    rows.l = 0.0f;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                from[n] = lo[n] - 32 * b;
-                to[n] = hi[n] - 32 * b;
-            }
-            rows.add(k_now, v_now, lane, b < all_from || b >= all_to, from, to, w.length - 32 * b);
+    for (int j = 0; j < TILES; ++j) rows.o[j] = float4v{0, 0, 0, 0};
+    const int my_row = min(lane & 15, w.tr.rows - 1), token = w.token_of(a, my_row);        // (rows that are not there repeat the last one)
+    const int lo = w.sees_from(a, token), hi = w.sees_to(a, token);
+    if (wave < W) {
+        const T* q = static_cast<const T*>(a.Q) + (w.tr.first - w.tr.token + token) * a.ldq + int64_t(w.head_of(a, my_row)) * a.dim;
+        const int d = (D / 4) * g + 8 * wave;
+        s_q[wave * 64 + lane] = d < a.dim ? __builtin_bit_cast(vec, Chunk<T, 8>::load(q + d, a.dim - d)) : vec{};
+    }
+    // records from all_from to before all_to hide nothing from any row
+    const int all_from = uniform((w.sees_from(a, w.token_of(a, w.tr.rows - 1)) + 31) >> 5), all_to = uniform(w.sees_to(a, w.tr.token) >> 5);
+    __syncthreads();
+
+    for (; b < e; b += AT_WAVES) {
+        // the next record's keys come while this one's scores are weighed, its values while the next one's scores are computed: bytes of
+        // one record at a time, in favour of more waves
+        const int next = b + AT_WAVES, page2 = page_of(next + AT_WAVES);
+        const bool use = there(page);
+        float4v s[2];
+        half8v p;
+        if (use) rows.scores(kb, s_q, lane, s);
+        __builtin_amdgcn_sched_barrier(0);
+        if (next < e) load_keys(record(page1, next));
+        if (use) {
+            if (b < all_from || b >= all_to) rows.hide(s, g, lo, hi, RECORD * b);
+            rows.weigh(s, p);
+            __builtin_amdgcn_sched_barrier(0);
+            rows.values(vb, g, w.length - RECORD * b, p);
         }
-        k_now = k_next;
-        v_now = v_next;
+        __builtin_amdgcn_sched_barrier(0);
+        if (next < e) load_values(record(page1, next));
         page = page1;
         page1 = page2;
     }
-#pragma unroll
-    for (int n = 0; n < NT; ++n) rows.l[n] = quarters(rows.l[n], [](float x, float y) { return x + y; });
+    rows.l = quarters(rows.l, [](float x, float y) { return x + y; });
 
-    // ---- the four waves' sums
+    // ---- the waves' sums, in PASSES of 64 elements (35 KB): of the TILES elements of a unit the four from 4 pass on (all with D = 64)
     float* const mine = args.parts + (int64_t(blockIdx.x) * gridDim.y + blockIdx.y) * (R * PART<D>);
-    constexpr int PARTS = D > 128 ? 2 : 1, JT = TILES / PARTS;             // (a part of D's elements at a time: 64 KB)
-    __shared__ float s_o[AT_WAVES][16][16 * JT + 4];
+    constexpr int PASSES = D / 64;
+    __shared__ __attribute__((aligned(16))) float s_o[AT_WAVES][16][64 + 4];
     __shared__ float s_m[AT_WAVES][R], s_l[AT_WAVES][R];
-    if (lane < 16)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            s_m[wave][16 * n + lane] = rows.m[n];
-            s_l[wave][16 * n + lane] = rows.l[n];
-        }
+    if (lane < 16) {
+        s_m[wave][lane] = rows.m;
+        s_l[wave][lane] = rows.l;
+    }
     __syncthreads();
-    const int r = threadIdx.x >> 4, x = threadIdx.x & 15;
+    const int row = threadIdx.x >> 5, x = threadIdx.x & 31;   // 32 lanes a row, two elements each
+    float top = s_m[0][lane & 15], m = s_m[0][row], l = 0.0f;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int rn = 16 * n + (lane & 15), row = 16 * n + r;
-        float top = s_m[0][rn], m = s_m[0][row], l = 0.0f;
+    for (int i = 1; i < AT_WAVES; ++i) {
+        top = fmaxf(top, s_m[i][lane & 15]);
+        m = fmaxf(m, s_m[i][row]);
+    }
+    const float by = __builtin_amdgcn_exp2f(rows.m - top);
 #pragma unroll
-        for (int i = 1; i < AT_WAVES; ++i) {
-            top = fmaxf(top, s_m[i][rn]);
-            m = fmaxf(m, s_m[i][row]);
+    for (int i = 0; i < AT_WAVES; ++i) l += s_l[i][row] * __builtin_amdgcn_exp2f(s_m[i][row] - m);
+    const float by1 = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (int pass = 0; pass < PASSES; ++pass) {
+        if (pass > 0) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float4v v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = rows.o[4 * pass + j][i] * by;
+            *reinterpret_cast<float4v*>(&s_o[wave][lane & 15][4 * (4 * g + i)]) = v;
         }
-        const float by = __builtin_amdgcn_exp2f(rows.m[n] - top);
+        __syncthreads();
+        if (row >= w.tr.rows) continue;
+        float v[2] = {0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < AT_WAVES; ++i) l += s_l[i][row] * __builtin_amdgcn_exp2f(s_m[i][row] - m);
-        const float by1 = l == 0.0f ? 0.0f : 1.0f / l;
+        for (int i = 0; i < AT_WAVES; ++i) {
+            const float2v o = *reinterpret_cast<const float2v*>(&s_o[i][row][2 * x]);
+            v[0] += o.x;
+            v[1] += o.y;
+        }
+        const int d = (x >> 1) * TILES + 4 * pass + 2 * (x & 1);
+        if (w.shares > 1) {
+            put(mine + row * PART<D> + d, v[0], v[1]);
+            if (x == 0 && pass == 0) put(mine + row * PART<D> + D, m, l);
+        } else {
 #pragma unroll
-        for (int part = 0; part < PARTS; ++part) {
-            if (n > 0 || part > 0) __syncthreads();
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < JT; ++j) s_o[wave][lane & 15][JT * (4 * g + i) + j] = rows.o[n][part * JT + j][i] * by;
-            __syncthreads();
-            if (row >= w.tr.rows) continue;
-            const int d0 = TILES * x + part * JT;
-            float v[JT];
-#pragma unroll
-            for (int j = 0; j < JT; ++j) {
-                v[j] = 0.0f;
-#pragma unroll
-                for (int i = 0; i < AT_WAVES; ++i) v[j] += s_o[i][r][JT * x + j];
-            }
-            if (w.shares > 1) {
-#pragma unroll
-                for (int j = 0; j < JT; ++j) put(mine + row * PART<D> + d0 + j, v[j]);
-                if (d0 == 0) {
-                    put(mine + row * PART<D> + D, m);
-                    put(mine + row * PART<D> + D + 1, l);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < JT; ++j) v[j] = l == 0.0f ? 0.0f : v[j] * by1;
-                store_row(a, w.row_of_y(a, row), d0, v);
-            }
+            for (int k = 0; k < 2; ++k) v[k] = l == 0.0f ? 0.0f : v[k] * by1;
+            store_row(a, w.row_of_y(a, row), d, v);
         }
     }
     if (w.shares > 1) join<R, D, AT_WAVES>(args, w);

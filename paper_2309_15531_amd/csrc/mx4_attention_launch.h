@@ -8,18 +8,18 @@ int attention_shares(adadim_ctx* ctx, size_t bytes, void*& shared);
 namespace mx4 {
 
 // How many shares a tile's records are cut into (an upper bound; a tile with few takes fewer) and how many records one has at least.
+// wanted: workgroups that keep the chip busy, with some to spare for sequences of unlike lengths.  A share costs about 10 us beside its records
+// (start, the waves' sums, the way to the join), a record of eight waves 0.15: they are cut to 32 records only while that is one round of workgroups.
 struct Shares { int most, least; };
-inline Shares shares_of(const Attention& a, int64_t tiles, int rows, bool keys) {
-    const int64_t items = tiles * a.heads;
+inline Shares shares_of(const Attention& a, int64_t tiles, int rows, bool few) {
     const int64_t seen = a.window ? std::min(a.max_length, a.window + a.max_new) : a.max_length;
     const int64_t records = (seen + 31) / 32 + 1;
     // tiles that hold rows, as far as the host can tell
-    const int64_t real = std::min(tiles, a.sequences * ((a.max_new * a.group + rows - 1) / rows)) * a.heads;
-    const int least = keys ? 4 * AT_WAVES : 32;
-    const int64_t wanted = (keys ? 1024 : 512) / std::max<int64_t>(real, 1);
-    int64_t n = std::min(wanted, records / least);
-    if (items > AT_TICKETS || n < 1) n = 1;
-    return {static_cast<int>(std::min<int64_t>(n, 256)), least};
+    const int64_t real = std::max<int64_t>(1, std::min(tiles, a.sequences * ((a.max_new * a.group + rows - 1) / rows)) * a.heads);
+    const int64_t wanted = (few ? 1024 : 512) / real;
+    const int least = few && real * ((records + 31) / 32) > 512 ? 64 : 32;
+    const int64_t n = tiles * a.heads > AT_TICKETS ? 1 : std::min(wanted, records / least);
+    return {static_cast<int>(std::min<int64_t>(std::max<int64_t>(n, 1), MOST_SHARES)), least};
 }
 
 // The launch's tiles, shares and scratch; R: rows of a tile.
@@ -38,14 +38,14 @@ int laid_out(adadim_ctx* ctx, const Attention& a, bool keys, AttentionArgs& args
     return ADADIM_OK;
 }
 
-template <class T, int D, int NT>
+template <class T, int D>
 int launch_few(adadim_ctx* ctx, const Attention& a) {
     AttentionArgs args;
     dim3 grid;
-    const int rc = laid_out<16 * NT, D>(ctx, a, true, args, grid);
+    const int rc = laid_out<16, D>(ctx, a, true, args, grid);
     if (rc != ADADIM_OK) return rc;
     ProfScope prof(ctx, "mx4_attend_few");
-    hipLaunchKernelGGL((mx4_attend_few<T, D, NT>), grid, dim3(64 * AT_WAVES), 0, ctx->stream, args);
+    hipLaunchKernelGGL((mx4_attend_few<T, D>), grid, dim3(64 * AT_WAVES), 0, ctx->stream, args);
     ADADIM_LAUNCH_CHECK(ctx, "mx4_attend_few");
     return ADADIM_OK;
 }
@@ -68,13 +68,7 @@ int launch_tiles(adadim_ctx* ctx, const Attention& a) {
 
 template <class T, int D>
 int launch_head(adadim_ctx* ctx, const Attention& a) {
-    const int64_t rows = a.max_new * a.group;
-    if (rows <= 16) return launch_few<T, D, 1>(ctx, a);
-    if (rows <= 64) {
-        if constexpr (D <= 128) return launch_few<T, D, 2>(ctx, a);
-        else return launch_few<T, D, 1>(ctx, a);
-    }
-    return launch_tiles<T, D>(ctx, a);
+    return a.max_new * a.group <= 64 ? launch_few<T, D>(ctx, a) : launch_tiles<T, D>(ctx, a);
 }
 
 template <class T>

@@ -1,7 +1,7 @@
 // Attention of many rows over a paged cache in mx4 (the mathematics: mx4_attention.h).
 //
 // A workgroup has eight waves, two a SIMD, of 32 rows each: while one weighs scores on the vector unit the other multiplies.  Its records go
-// through LDS four at a time, each converted by two of the waves, one its keys and one its values: what costs most to prepare, the
+// through LDS four at a time, each converted by two of the waves, half of its positions each: what costs most to prepare, the
 // values of codes with their scales, is done once for all 256 rows.  They lie there as the 32-row instruction takes
 // its left operand, lane by lane in 16 bytes (no bank is met twice in a read): keys [step][half][position], with step s of half h the
 // elements h D/2 + 8 s ..; values [tile jj][step][half][row r], with row r of tile jj the element (D/16) (r % 16) + (D/32) (r / 16) + jj, and
@@ -29,30 +29,27 @@ struct Stage {
     static constexpr int LDS = BUFFERS * RECORDS * BYTES;
 };
 
-// A record's keys to their places in LDS.
+// Half a record, its positions 16 t .. 16 t + 15, to its places in LDS.
 template <class T, int D>
-__device__ __forceinline__ void convert_keys(const KeyBytes<D>& b, uint8_t* to, int lane) {
+__device__ __forceinline__ void convert_keys(const KeyBytes<D>& b, uint8_t* to, int t, int lane) {
     constexpr int W = D / 32;
     const int m = lane & 15, g = lane >> 4;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int w = 0; w < W; ++w)
-            *reinterpret_cast<typename Dots<T>::vec*>(to + ((((g & 1) * W + w) * 2 + (g >> 1)) * 32 + 16 * t + m) * 16) = Dots<T>::keys(b.words[t][w], b.scale(t, w));
+    for (int w = 0; w < W; ++w)
+        *reinterpret_cast<typename Dots<T>::vec*>(to + ((((g & 1) * W + w) * 2 + (g >> 1)) * 32 + 16 * t + m) * 16) = Dots<T>::keys(b.words[w], b.scale(w));
 }
-
-// Its values; have: positions that exist.
 template <int D>
-__device__ __forceinline__ void convert_values(const ValueBytes<D>& b, uint8_t* to, int lane, int have) {
+__device__ __forceinline__ void convert_values(const ValueBytes<D>& b, uint8_t* to, int t, int lane, int have) {
     const int m = lane & 15, g = lane >> 4;
-    float vs[8];
-    b.scales(vs, g, have);
-    uint8_t* const v0 = to + Stage<D>::KEYS + ((g & 1) * 32 + m) * 16 + (g >> 1) * 8;
+    typedef _Float16 half4v __attribute__((ext_vector_type(4)));
+    float vs[4];
+    b.scales(vs, t, g, have);
+    uint8_t* const v0 = to + Stage<D>::KEYS + (t * 64 + (g & 1) * 32 + m) * 16 + (g >> 1) * 8;
 #pragma unroll
     for (int u = 0; u < D / 32; ++u) {
-        half8v both[2];
+        half4v both[2];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4; ++i) {
             const half2v v = b.pair(i, u, vs[i]);
             both[0][i] = v.x;
             both[1][i] = v.y;
@@ -60,10 +57,7 @@ __device__ __forceinline__ void convert_values(const ValueBytes<D>& b, uint8_t* 
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             const int j = 2 * u + x, jj = j % (D / 32), high = j / (D / 32);                              // the unit's element j
-            typedef _Float16 half4v __attribute__((ext_vector_type(4)));
-            uint8_t* const p = v0 + (jj * 128 + high * 16) * 16;
-            *reinterpret_cast<half4v*>(p) = half4v{both[x][0], both[x][1], both[x][2], both[x][3]};
-            *reinterpret_cast<half4v*>(p + 64 * 16) = half4v{both[x][4], both[x][5], both[x][6], both[x][7]};
+            *reinterpret_cast<half4v*>(v0 + (jj * 128 + high * 16) * 16) = both[x];
         }
     }
 }
@@ -126,7 +120,7 @@ __global__ __launch_bounds__(64 * TL_WAVES, 2) void mx4_attend_tiles(AttentionAr
     // ---- the wave's rows and the records that they see
     const int w_row = WROWS * wave, w_last = min(w_row + WROWS, w.tr.rows) - 1;                           // (w_last < w_row: none)
     const int row = min(w_row + (lane & 31), w.tr.rows - 1), token = w.token_of(a, row);                  // (rows that are not there repeat the last one)
-    const int t_first = w.token_of(a, min(w_row, w.tr.rows - 1)), t_last = w.token_of(a, max(w_last, 0));
+    const int t_first = uniform(w.token_of(a, min(w_row, w.tr.rows - 1))), t_last = uniform(w.token_of(a, max(w_last, 0)));
     const int from = w_last < w_row ? w.end : w.sees_from(a, t_first) >> 5;
     const int to = w_last < w_row ? w.begin : min((w.sees_to(a, t_last) + 31) >> 5, w.end);
     const int all_from = (w.sees_from(a, t_last) + 31) >> 5, all_to = w.sees_to(a, t_first) >> 5;         // (these hide nothing from any row)
@@ -150,32 +144,42 @@ __global__ __launch_bounds__(64 * TL_WAVES, 2) void mx4_attend_tiles(AttentionAr
     const int per_page = a.log_page - 5;
     auto page_of = [&](int r) { return r < w.end ? table[r >> per_page] : -1; };
     auto there = [&](int page) { return uint32_t(page) < uint64_t(a.pages); };
-    // the wave's part of a stage: the keys of a record or its values
-    const int part = wave & 3;
-    const bool keys = wave < 4;
+    // whether all the pages are there, looked up once for all: a scalar load for each record would be waited for
+    bool whole = true;
+    for (int p = (w.begin >> per_page) + lane, end = w.begin < w.end ? (w.end - 1) >> per_page : -1; __any(p <= end); p += 64) whole = whole && !__any(p <= end && !there(table[p]));
+    // the wave's part of a stage: half a record
+    const int part = wave & 3, half = wave >> 2;
     KeyBytes<D> kb;
     ValueBytes<D> vb;
+    // (the page's number a stage ahead, by a vector load: waiting for a scalar one would wait for LDS, too, and the other way)
+    auto page_ahead = [&](int r) {
+        int i = r < w.end ? r >> per_page : 0;
+        asm volatile("" : "+v"(i));
+        return table[i];
+    };
+    int page = page_ahead(w.begin + part);
     auto fetch = [&](int first) {
         const int r = first + part;
         if (r >= w.end) return;
-        const int page = page_of(r);
-        const int64_t p = there(page) ? page : 0;             // (a page that is not there is not used; page 0 is)
+        const int id = uniform(page);
+        const int64_t p = there(id) ? id : 0;                 // (a page that is not there is not used; page 0 is)
         const uint8_t* const rec = a.cache + (((p * a.heads + w.head) << per_page) + (r & ((1 << per_page) - 1))) * Record<D>::BYTES;
-        if (keys) kb.load(rec, lane);
-        else vb.load(rec, lane);
+        page = page_ahead(r + RECORDS);
+        kb.load(rec, half, lane);
+        vb.load(rec, half, lane);
     };
     auto bring = [&](int first, int buffer) {
         const int r = first + part;
         if (r >= w.end) return;
         uint8_t* const at = s_stage + (buffer * RECORDS + part) * BYTES;
-        if (keys) convert_keys<T, D>(kb, at, lane);
-        else convert_values<D>(vb, at, lane, w.length - RECORD * r);
+        convert_keys<T, D>(kb, at, half, lane);
+        convert_values<D>(vb, at, half, lane, w.length - RECORD * r);
     };
     auto stage = [&](int first, int buffer) {
         const uint8_t* const at = s_stage + buffer * RECORDS * BYTES;
         const int r1 = min(first + RECORDS, to);
         for (int r = max(first, from); r < r1; ++r) {
-            if (!there(page_of(r))) continue;
+            if (!whole && !there(page_of(r))) continue;
             const uint8_t* const rec = at + (r - first) * BYTES;
             float16v s = t.scores(rec, lane);
             if (r < all_from || r >= all_to) {
@@ -225,17 +229,14 @@ __global__ __launch_bounds__(64 * TL_WAVES, 2) void mx4_attend_tiles(AttentionAr
             for (int j = 0; j < N; ++j) v[j] = t.o[j % (D / 32)][i + 8 * (j / (D / 32))];
             if (w.shares > 1) {
 #pragma unroll
-                for (int j = 0; j < N; ++j) put(mine + row * PART<D> + d + j, v[j]);
+                for (int j = 0; j < N; j += 2) put(mine + row * PART<D> + d + j, v[j], v[j + 1]);
             } else {
 #pragma unroll
                 for (int j = 0; j < N; ++j) v[j] = l == 0.0f ? 0.0f : v[j] * by;
                 store_row(a, y, d, v);
             }
         }
-        if (w.shares > 1 && h == 0) {
-            put(mine + row * PART<D> + D, t.m);
-            put(mine + row * PART<D> + D + 1, l);
-        }
+        if (w.shares > 1 && h == 0) put(mine + row * PART<D> + D, t.m, l);
     }
     if (w.shares > 1) join<R, D, TL_WAVES>(args, w);
 }
