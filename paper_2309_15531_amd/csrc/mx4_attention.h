@@ -9,8 +9,8 @@
 // p stays below 2^15.  The sum is of p before rounding.  Scores, sums and O^T are fp32.
 //
 // Few rows (this file): the waves of a workgroup have the same rows and take records in turn; their sums meet in LDS.  Many rows:
-// mx4_attention_tiles.h.  Either way a tile's records may be shared between workgroups (gridDim.y); partial sums travel as relaxed atomics at
-// device scope, and the workgroup that finishes last joins them in their order: same bits every run.
+// mx4_attention_tiles.h.  Either way a tile's records may be shared between workgroups (gridDim.y), whose partial sums are joined in their order:
+// same bits every run.  Here they travel as relaxed atomics at device scope, and the workgroup that finishes last joins them.
 #pragma once
 
 #include "mx4_cache.h"
@@ -26,6 +26,7 @@ struct AttentionArgs {
     Attention a;
     int tiles;                                    // row tiles, of which each sequence has one that may not exist
     int least;                                    // records that a share has at least
+    int most;                                     // shares of a tile at most
     unsigned* tickets;
     float* parts;
 };
@@ -264,7 +265,7 @@ struct Work {
     }
 };
 template <int R>
-__device__ __forceinline__ Work work_of(const AttentionArgs& args) {
+__device__ __forceinline__ Work work_of(const AttentionArgs& args, int y) {
     const Attention& a = args.a;
     Work w;
     w.shares = 0;
@@ -274,8 +275,8 @@ __device__ __forceinline__ Work work_of(const AttentionArgs& args) {
     w.length = w.tr.length;
     w.before = w.length - w.tr.added;
     const int begin = uniform(w.sees_from(a, w.tr.token) >> 5), end = uniform((w.sees_to(a, w.token_of(a, w.tr.rows - 1)) + 31) >> 5);
-    const int records = max(end - begin, 0), y = static_cast<int>(blockIdx.y), ny = static_cast<int>(gridDim.y);
-    const int share = uniform(max((records + ny - 1) / ny, args.least));
+    const int records = max(end - begin, 0);
+    const int share = uniform(max((records + args.most - 1) / args.most, args.least));
     const int shares = uniform(max((records + share - 1) / share, 1));
     w.shares = y < shares ? shares : 0;
     w.begin = begin + share * y;
@@ -283,24 +284,17 @@ __device__ __forceinline__ Work work_of(const AttentionArgs& args) {
     return w;
 }
 
-// Partial sums: per tile, head and share [R rows][D + 2], the sums, then m and l.  Who finishes last joins the shares: 16 lanes a row, whose
-// lane x has the elements 64 j + 4 x .. and first the m and l of the shares x, x + 16, ..
+// Partial sums: per tile, head and share [R rows][D + 2], the sums, then m and l.  Joining them: 16 lanes a row, whose lane x has the elements
+// 64 j + 4 x .. and first the m and l of the shares x, x + 16, ..; `at_once` rows from row0 on, one for each 16 threads.
 template <int D> constexpr int PART = D + 2;
 constexpr int MOST_SHARES = 64;
-template <int R, int D, int WAVES>
-__device__ __forceinline__ void join(const AttentionArgs& args, const Work& w) {
+template <int R, int D>
+__device__ __forceinline__ void join_rows(const AttentionArgs& args, const Work& w, int row_begin, int row_end, int at_once) {
     constexpr int N = D / 64, AT_ONCE = 4;
-    __shared__ unsigned s_ticket;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (threadIdx.x == 0) s_ticket = __hip_atomic_fetch_add(args.tickets + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    if (s_ticket != unsigned(w.shares) - 1) return;
-    if (threadIdx.x == 0) __hip_atomic_store(args.tickets + blockIdx.x, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const float* const all = args.parts + int64_t(blockIdx.x) * gridDim.y * (R * PART<D>);
+    const float* const all = args.parts + int64_t(blockIdx.x) * args.most * (R * PART<D>);
     const int x = threadIdx.x & 15, lane0 = threadIdx.x & 48;
-    for (int row0 = 0; row0 < w.tr.rows; row0 += 4 * WAVES) {
-        const int row = min(row0 + static_cast<int>(threadIdx.x >> 4), w.tr.rows - 1);
+    for (int row0 = row_begin; row0 < row_end; row0 += at_once) {
+        const int row = min(row0 + static_cast<int>(threadIdx.x >> 4), row_end - 1);
         const float* const p = all + row * PART<D>;
         float by[MOST_SHARES / 16], m = LOWEST, l = 0.0f;
         float2p ml[MOST_SHARES / 16];
@@ -344,7 +338,7 @@ __device__ __forceinline__ void join(const AttentionArgs& args, const Work& w) {
                         for (int k = 0; k < 4; ++k) v[j][k] += part[z][j][k >> 1][k & 1] * f;
                 }
             }
-        if (row0 + static_cast<int>(threadIdx.x >> 4) >= w.tr.rows) continue;
+        if (row0 + static_cast<int>(threadIdx.x >> 4) >= row_end) continue;
         const int64_t y = w.row_of_y(args.a, row);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
@@ -353,6 +347,19 @@ __device__ __forceinline__ void join(const AttentionArgs& args, const Work& w) {
             store_row(args.a, y, 64 * j + 4 * x, v[j]);
         }
     }
+}
+
+// The workgroup that finishes last joins.
+template <int R, int D, int WAVES>
+__device__ __forceinline__ void join(const AttentionArgs& args, const Work& w) {
+    __shared__ unsigned s_ticket;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) s_ticket = __hip_atomic_fetch_add(args.tickets + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (s_ticket != unsigned(w.shares) - 1) return;
+    if (threadIdx.x == 0) __hip_atomic_store(args.tickets + blockIdx.x, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    join_rows<R, D>(args, w, 0, w.tr.rows, 4 * WAVES);
 }
 
 // Waves of a SIMD that the registers have to leave room for.
@@ -364,7 +371,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, FEW_WAVES<D>) void mx4_attend_few(At
     constexpr int R = 16, TILES = D / 16, W = D / 32;
     typedef typename Dots<T>::vec vec;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
-    const Work w = work_of<R>(args);
+    const Work w = work_of<R>(args, blockIdx.y);
     if (w.shares == 0) return;
     int b = w.begin + wave;
     const int e = w.end;
@@ -429,7 +436,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, FEW_WAVES<D>) void mx4_attend_few(At
     rows.l = quarters(rows.l, [](float x, float y) { return x + y; });
 
     // ---- the waves' sums, in PASSES of 64 elements (35 KB): of the TILES elements of a unit the four from 4 pass on (all with D = 64)
-    float* const mine = args.parts + (int64_t(blockIdx.x) * gridDim.y + blockIdx.y) * (R * PART<D>);
+    float* const mine = args.parts + (int64_t(blockIdx.x) * args.most + blockIdx.y) * (R * PART<D>);
     constexpr int PASSES = D / 64;
     __shared__ __attribute__((aligned(16))) float s_o[AT_WAVES][16][64 + 4];
     __shared__ float s_m[AT_WAVES][R], s_l[AT_WAVES][R];

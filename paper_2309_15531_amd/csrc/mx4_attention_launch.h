@@ -8,16 +8,17 @@ int attention_shares(adadim_ctx* ctx, size_t bytes, void*& shared);
 namespace mx4 {
 
 // How many shares a tile's records are cut into (an upper bound; a tile with few takes fewer) and how many records one has at least.
-// wanted: workgroups that keep the chip busy, with some to spare for sequences of unlike lengths.  A share costs about 10 us beside its records
-// (start, the waves' sums, the way to the join), a record of eight waves 0.15: they are cut to 32 records only while that is one round of workgroups.
+// Few rows: two rounds of workgroups, for sequences of unlike lengths.  A share costs about 10 us beside its records (start, the waves' sums, the way
+// to the join), a record of eight waves 0.15: cut below 64 records only while the shares are one round.  Many rows: one round (2 x 4000 positions, 1000
+// new ones, 32 heads: 125 us, 138 with two); a record takes 0.5 us there.
 struct Shares { int most, least; };
 inline Shares shares_of(const Attention& a, int64_t tiles, int rows, bool few) {
     const int64_t seen = a.window ? std::min(a.max_length, a.window + a.max_new) : a.max_length;
     const int64_t records = (seen + 31) / 32 + 1;
     // tiles that hold rows, as far as the host can tell
     const int64_t real = std::max<int64_t>(1, std::min(tiles, a.sequences * ((a.max_new * a.group + rows - 1) / rows)) * a.heads);
-    const int64_t wanted = (few ? 1024 : 512) / real;
-    const int least = few && real * ((records + 31) / 32) > 512 ? 64 : 32;
+    const int64_t wanted = (few ? 1024 : 256) / real;
+    const int least = !few ? 16 : real * ((records + 31) / 32) > 512 ? 64 : 32;
     const int64_t n = tiles * a.heads > AT_TICKETS ? 1 : std::min(wanted, records / least);
     return {static_cast<int>(std::min<int64_t>(std::max<int64_t>(n, 1), MOST_SHARES)), least};
 }
@@ -27,7 +28,7 @@ template <int R, int D>
 int laid_out(adadim_ctx* ctx, const Attention& a, bool keys, AttentionArgs& args, dim3& grid) {
     const int64_t tiles = a.tokens * a.group / R + a.sequences;
     const Shares s = shares_of(a, tiles, R, keys);
-    args = AttentionArgs{a, static_cast<int>(tiles), s.least, nullptr, nullptr};
+    args = AttentionArgs{a, static_cast<int>(tiles), s.least, s.most, nullptr, nullptr};
     grid = dim3(static_cast<unsigned>(tiles * a.heads), s.most);
     if (s.most == 1) return ADADIM_OK;
     void* shared = nullptr;
@@ -63,12 +64,19 @@ int launch_tiles(adadim_ctx* ctx, const Attention& a) {
     ProfScope prof(ctx, "mx4_attend_tiles");
     hipLaunchKernelGGL((mx4_attend_tiles<T, D>), grid, dim3(64 * TL_WAVES), Stage<D>::LDS, ctx->stream, args);
     ADADIM_LAUNCH_CHECK(ctx, "mx4_attend_tiles");
+    if (args.most == 1) return ADADIM_OK;
+    ProfScope prof_join(ctx, "mx4_attend_join");
+    hipLaunchKernelGGL((mx4_attend_join<D>), dim3(grid.x, TL_WAVES), dim3(512), 0, ctx->stream, args);
+    ADADIM_LAUNCH_CHECK(ctx, "mx4_attend_join");
     return ADADIM_OK;
 }
 
+// Up to 256 rows a sequence and head by tiles of 16, which read a cache once for each 16 rows but leave no wave without rows and share it finely:
+// 2 x 4000 positions, 256 rows, 32 heads 51 us by them, 54 to 60 by tiles of 256; 1000 rows 160 and 125; 20000 positions, 8 heads, 256 rows 54 and
+// 83, 1024 rows 158 and 112.
 template <class T, int D>
 int launch_head(adadim_ctx* ctx, const Attention& a) {
-    return a.max_new * a.group <= 64 ? launch_few<T, D>(ctx, a) : launch_tiles<T, D>(ctx, a);
+    return a.max_new * a.group <= 256 ? launch_few<T, D>(ctx, a) : launch_tiles<T, D>(ctx, a);
 }
 
 template <class T>

@@ -114,7 +114,7 @@ __global__ __launch_bounds__(64 * TL_WAVES, 2) void mx4_attend_tiles(AttentionAr
     constexpr int BUFFERS = Stage<D>::BUFFERS, RECORDS = Stage<D>::RECORDS, BYTES = Stage<D>::BYTES;
     extern __shared__ __attribute__((aligned(16))) uint8_t s_stage[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-    const Work w = work_of<R>(args);
+    const Work w = work_of<R>(args, blockIdx.y);
     if (w.shares == 0) return;
 
     // ---- the wave's rows and the records that they see
@@ -175,24 +175,36 @@ __global__ __launch_bounds__(64 * TL_WAVES, 2) void mx4_attend_tiles(AttentionAr
         convert_keys<T, D>(kb, at, half, lane);
         convert_values<D>(vb, at, half, lane, w.length - RECORD * r);
     };
+    auto hide = [&](float16v& s, int r) {
+        if (r >= all_from && r < all_to) return;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int key = RECORD * r + 8 * (i >> 2) + 4 * h + (i & 3);
+            s[i] = key >= lo && key < hi ? s[i] : -INFINITY;
+        }
+    };
+    // The SIMD's other wave converts half a stage later: one's conversion runs under the other's products.
+    auto next_stage = [&](int first, int buffer) {
+        bring(first + RECORDS, buffer ^ 1);
+        fetch(first + 2 * RECORDS);
+    };
     auto stage = [&](int first, int buffer) {
         const uint8_t* const at = s_stage + buffer * RECORDS * BYTES;
         const int r1 = min(first + RECORDS, to);
-        for (int r = max(first, from); r < r1; ++r) {
-            if (!whole && !there(page_of(r))) continue;
-            const uint8_t* const rec = at + (r - first) * BYTES;
-            float16v s = t.scores(rec, lane);
-            if (r < all_from || r >= all_to) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int key = RECORD * r + 8 * (i >> 2) + 4 * h + (i & 3);
-                    s[i] = key >= lo && key < hi ? s[i] : -INFINITY;
-                }
+        for (int part = 0; part < 2; ++part) {
+            if (BUFFERS == 2 && half == part) next_stage(first, buffer);
+            const int p1 = min(first + RECORDS / 2 * (part + 1), r1);
+            for (int r = max(first + RECORDS / 2 * part, from); r < p1; ++r) {
+                if (!whole && !there(page_of(r))) continue;
+                const uint8_t* const rec = at + (r - first) * BYTES;
+                float16v s = t.scores(rec, lane);
+                hide(s, r);
+                t.raise(s);
+                half8v p[2];
+                t.weigh(s, p);
+                t.values(rec, lane, p);
             }
-            t.raise(s);
-            half8v p[2];
-            t.weigh(s, p);
-            t.values(rec, lane, p);
         }
     };
     fetch(w.begin);
@@ -202,8 +214,6 @@ __global__ __launch_bounds__(64 * TL_WAVES, 2) void mx4_attend_tiles(AttentionAr
     int buffer = 0;
     for (int first = w.begin; first < w.end; first += RECORDS) {
         if constexpr (BUFFERS == 2) {
-            bring(first + RECORDS, buffer ^ 1);
-            fetch(first + 2 * RECORDS);
             stage(first, buffer);
             __syncthreads();
             buffer ^= 1;
@@ -217,7 +227,7 @@ __global__ __launch_bounds__(64 * TL_WAVES, 2) void mx4_attend_tiles(AttentionAr
     }
 
     // ---- out
-    float* const mine = args.parts + (int64_t(blockIdx.x) * gridDim.y + blockIdx.y) * (R * PART<D>);
+    float* const mine = args.parts + (int64_t(blockIdx.x) * args.most + blockIdx.y) * (R * PART<D>);
     const float l = t.l + __shfl_xor(t.l, 32), by = l == 0.0f ? 0.0f : 1.0f / l;
     if (w_row + (lane & 31) <= w_last) {
         const int64_t y = w.row_of_y(a, row);
@@ -229,16 +239,25 @@ __global__ __launch_bounds__(64 * TL_WAVES, 2) void mx4_attend_tiles(AttentionAr
             for (int j = 0; j < N; ++j) v[j] = t.o[j % (D / 32)][i + 8 * (j / (D / 32))];
             if (w.shares > 1) {
 #pragma unroll
-                for (int j = 0; j < N; j += 2) put(mine + row * PART<D> + d + j, v[j], v[j + 1]);
+                for (int j = 0; j < N; j += 2) *reinterpret_cast<float2v*>(mine + row * PART<D> + d + j) = float2v{v[j], v[j + 1]};
             } else {
 #pragma unroll
                 for (int j = 0; j < N; ++j) v[j] = l == 0.0f ? 0.0f : v[j] * by;
                 store_row(a, y, d, v);
             }
         }
-        if (w.shares > 1 && h == 0) put(mine + row * PART<D> + D, t.m, l);
+        if (w.shares > 1 && h == 0) *reinterpret_cast<float2v*>(mine + row * PART<D> + D) = float2v{t.m, l};
     }
-    if (w.shares > 1) join<R, D, TL_WAVES>(args, w);
+}
+
+// The shares of the tiles that have several: a launch of its own, in which a tile's rows are spread over as many workgroups as it had waves.
+// (Joined by the workgroup that finishes last, 20000 positions and 32 tokens of 64 heads over 8 took 198 us.)
+template <int D>
+__global__ __launch_bounds__(512) void mx4_attend_join(AttentionArgs args) {
+    constexpr int R = 32 * TL_WAVES;
+    const Work w = work_of<R>(args, 0);
+    const int row = 32 * blockIdx.y;
+    if (w.shares > 1 && row < w.tr.rows) join_rows<R, D>(args, w, row, min(row + 32, w.tr.rows), 32);
 }
 
 }  // namespace mx4
