@@ -1,12 +1,12 @@
 // Attention over a paged cache in mx4:  y = sum_j softmax_j(scale q . k_j) v_j  over the positions j that a query sees.
 //
 // A tile is a number of rows (a row: one query head of one new token) of a sequence that share a key-value head.  A wave goes over records of 32
-// positions:  S^T = K Q^T, keys converted in registers to the queries' type (exact:
-// 2 bits and fp16's or bf16's exponents), then p = 2^(scale log2(e) s - m + 8) in fp32, rounded to fp16 (11 bits; with the
-// 2^8 the smallest number that fp16 still holds is 2^-33 of the row's largest), and O^T += V^T P^T with the values in fp16 (exact).  Positions
-// lie along a lane's registers and rows along the lanes in S^T and in O^T: neither is turned round, and a row's maximum and
-// sum are numbers of its lanes.  The maximum m is only raised (and O^T and the sum scaled) where a score passes it by more than 7:
-// p stays below 2^15.  The sum is of p before rounding.  Scores, sums and O^T are fp32.
+// positions:  S^T = K Q^T, keys converted in registers to the queries' type (exact: 2 bits and a scale that fp16 and bf16 have), then
+// p = 2^(scale log2(e) s - m + 8) in fp32, rounded to fp16 (half a step of 11 bits; with the 2^8 the smallest number that fp16 still holds is
+// 2^-33 of the row's largest), and O^T += V^T P^T with the values in fp16 (exact).  Positions lie along a lane's registers and rows along the
+// lanes in S^T and in O^T: neither is turned round, and a row's maximum and sum are numbers of its lanes.  The maximum m is only raised (and
+// O^T and the sum scaled) where a score passes it by more than 7: p stays below 2^15.  The sum is of p before rounding.  Scores, sums and
+// O^T are fp32.
 //
 // Few rows (this file): the waves of a workgroup have the same rows and take records in turn; their sums meet in LDS.  Many rows:
 // mx4_attention_tiles.h.  Either way a tile's records may be shared between workgroups (gridDim.y), whose partial sums are joined in their order:

@@ -19,7 +19,8 @@ inline Shares shares_of(const Attention& a, int64_t tiles, int rows, bool few) {
     const int64_t real = std::max<int64_t>(1, std::min(tiles, a.sequences * ((a.max_new * a.group + rows - 1) / rows)) * a.heads);
     const int64_t wanted = (few ? 1024 : 256) / real;
     const int least = !few ? 16 : real * ((records + 31) / 32) > 512 ? 64 : 32;
-    const int64_t n = tiles * a.heads > AT_TICKETS ? 1 : std::min(wanted, records / least);
+    // (and no more than 35 MB of sums, 270 of many rows, where the host knows less of the sequences than there is)
+    const int64_t n = std::min({wanted, records / least, (few ? AT_TICKETS / 2 : 2048) / (tiles * a.heads)});
     return {static_cast<int>(std::min<int64_t>(std::max<int64_t>(n, 1), MOST_SHARES)), least};
 }
 

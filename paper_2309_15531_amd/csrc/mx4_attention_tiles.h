@@ -6,6 +6,13 @@
 // its left operand, lane by lane in 16 bytes (no bank is met twice in a read): keys [step][half][position], with step s of half h the
 // elements h D/2 + 8 s ..; values [tile jj][step][half][row r], with row r of tile jj the element (D/16) (r % 16) + (D/32) (r / 16) + jj, and
 // the step's positions 4 h .. and 8 + 4 h .. of 16 as S^T leaves them in a lane of half h.
+//
+// Bound by vector and matrix instructions together: of the 1000 clocks that a record takes a wave (two waves a SIMD, 2.1 GHz) the matrix pipe is
+// busy 512 and the vector unit about 500 (16 exponentials, 16 sums, 16 fma, 8 roundings, maxima, its share of the conversion).  4096 tokens into an
+// empty cache, 32 heads of 128: 149 us, 920 TFLOP/s; 2 x 2048 tokens over 16384, 64 heads over 8: 1417 us, 1050 TFLOP/s.  What did not
+// help there (that second case, beside 1420 to 1490 as the cards go): scores one record ahead in a wave, 1850 (in order or left to the
+// compiler); operands read from LDS ahead of use, 1500; waves' priorities, 1490; workgroups of six waves, three a SIMD, 1940, of four 1600;
+// one buffer for two, 1480.  Every wave converting for itself, 64 rows of 16-row tiles: 5400.
 #pragma once
 
 #include "mx4_attention.h"

@@ -1,4 +1,5 @@
-"""Layers of microscaled 4-bit weights: a linear layer, and a layer of experts behind a router.
+"""Layers of microscaled 4-bit weights: a linear layer, and a layer of experts behind a router; and a paged cache of keys and values in the
+same format with the attention over it.
 
 Allocation and call order only; all arithmetic happens in libadadim.so, but for the activation between an expert's two products, which
 is the caller's.
@@ -8,6 +9,8 @@ records a graph its stream has to be the current one; what the calls allocate th
 graph's alone until the graph is destroyed.
 """
 from __future__ import annotations
+
+from typing import NamedTuple
 
 import torch
 
@@ -189,3 +192,66 @@ class Mx4Experts:
         h = self._product(X, self.up, offsets, tokens * k, rows)
         z = self._product(self.activation(h), self.down, offsets, tokens * k)
         self.ctx.adadim_expert_combine(z, slots, weights, Y)
+
+
+class NewRows(NamedTuple):
+    """What CachePages.add gives, all int32 on the device."""
+    offsets: torch.Tensor                 # [sequences + 1]: where each sequence's new rows begin
+    slots: torch.Tensor                   # [tokens]: a row's place in the caches, -1 behind the last sequence's rows
+    positions: torch.Tensor               # [tokens]: its position in its sequence, -1 there
+    lacking: torch.Tensor                 # [1]: 0, or why nothing was added: pages short, or -1 (table or rows too small, a negative number)
+
+
+class CachePages:
+    """Which pages hold what, for the caches of all layers of a model: `pages` pages of `page` positions for up to `sequences` sequences of up to
+    `width` pages.  All of it lives on the device, and no call waits for it; a step can be recorded as a graph."""
+
+    def __init__(self, ctx: B.Context, pages: int, page: int, sequences: int, width: int, device="cuda"):
+        self.ctx, self.pages, self.page = ctx, pages, page
+        self.table = torch.full((sequences, width), -1, dtype=torch.int32, device=device)
+        self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)
+        self.free = torch.arange(pages, dtype=torch.int32, device=device)
+        self.count = torch.full((1,), pages, dtype=torch.int32, device=device)
+
+    def add(self, added, tokens: int) -> NewRows:
+        """added[s] (int32, device) more tokens for each sequence, `tokens` at most in all.  All or nothing: where lacking is not 0 no sequence
+        has grown and no row has a slot."""
+        n, dev = self.lengths.numel(), added.device
+        rows = NewRows(*(_output(self.ctx, (k,), torch.int32, dev) for k in (n + 1, tokens, tokens, 1)))
+        _ordered(self.ctx, added, self.ctx.adadim_cache_reserve, self.lengths, added, self.page, self.table, self.free, self.count, self.lengths,
+                 rows.offsets, rows.slots, rows.positions, self.count, rows.lacking)
+        return rows
+
+    def trim(self, kept):
+        """Each sequence keeps its first kept[s] (int32, device) tokens; the pages behind them are free again."""
+        _ordered(self.ctx, kept, self.ctx.adadim_cache_trim, self.lengths, kept, self.page, self.table, self.free, self.count, self.lengths, self.count)
+
+
+class Mx4Cache:
+    """A layer's keys and values, `heads` heads of `dim` elements, 4.25 bits each: 17 KB a token for 32 heads of 128, keys and values, where
+    fp16 takes 64."""
+
+    def __init__(self, pages: CachePages, heads: int, dim: int):
+        self.ctx, self.pages, self.heads, self.dim = pages.ctx, pages, heads, dim
+        self.records = torch.empty(B.mx4_cache_shape(pages.pages, pages.page, heads, dim), dtype=torch.uint8, device=pages.table.device)
+
+    def store(self, K, V, slots):
+        """Rows [tokens, heads * dim] (fp16, bf16 or fp32; views of one projection's output will do) to their slots."""
+        _ordered(self.ctx, K, self.ctx.adadim_mx4_cache_store, K, V, slots, self.records)
+
+    def load(self, slots, dtype=torch.float32):
+        """(K, V) [tokens, heads * dim] as stored."""
+        K, V = (_output(self.ctx, (slots.numel(), self.heads * self.dim), dtype, slots.device) for _ in range(2))
+        _ordered(self.ctx, slots, self.ctx.adadim_mx4_cache_load, slots, self.records, K, V)
+        return K, V
+
+    def attend(self, Q, offsets, Y=None, scale: float | None = None, causal: bool = True, window: int = 0, max_new: int = 0, max_length: int = 0):
+        """Attention of the rows of Q [tokens, query heads * dim] (fp16 or bf16), whose keys and values are stored already, to their sequences.
+        max_new, max_length: the most new rows and positions of a sequence, where the host knows them (a decoding step: 1); they lay the
+        launch out, the result does not depend on them.  Rows in no sequence are left as they are (without Y: not initialized)."""
+        if Y is None:
+            Y = _output(self.ctx, tuple(Q.shape), Q.dtype, Q.device)
+        p = self.pages
+        _ordered(self.ctx, Q, lambda: self.ctx.adadim_mx4_attention(Q, self.records, p.table, offsets, p.lengths, Y, self.dim, scale=scale, causal=causal,
+                                                                    window=window, max_new=max_new, max_length=max_length))
+        return Y

@@ -404,6 +404,29 @@ def test_offsets_and_lengths_outside_are_taken_as_the_nearer_end(ctx):
         check(got[keep], want[keep], weight[keep], slack[keep], dim, 96, 12.0, "f32")
 
 
+@pytest.mark.parametrize("added", [3, 300])
+def test_a_cache_beyond_32_bits(ctx, added):
+    """Pages on both sides of 4 GB: 70000 pages of 64 positions, 8 heads of 128."""
+    r = rng(12, added)
+    dim, page, heads, group, n, pages = 128, 64, 8, 1, 330, 70000
+    cache = torch.empty(B.mx4_cache_shape(pages, page, heads, dim), dtype=torch.uint8, device="cuda")
+    assert cache.numel() > 2 ** 32 + 2 ** 29
+    table = np.array([[69999, 0, 65000, 30839, 61681, 61682]], np.int32)
+    k, v = r.standard_normal((2, n, heads * dim)).astype(np.float32)
+    slots = table[0][np.arange(n) // page] * page + np.arange(n) % page
+    ctx.adadim_mx4_cache_store(torch.from_numpy(k).cuda(), torch.from_numpy(v).cuda(), ints(slots), cache)
+    small = np.zeros(B.mx4_cache_shape(6, page, heads, dim), np.uint8)
+    co.store(small, k.reshape(n, heads, dim), v.reshape(n, heads, dim), np.arange(n))
+    got = [torch.empty((n, heads * dim), device="cuda") for _ in range(2)]
+    ctx.adadim_mx4_cache_load(ints(slots), cache, *got)
+    assert all(np.array_equal(host(g).reshape(n, heads, dim), w) for g, w in zip(got, co.load(small, np.arange(n), dim)))
+    q = rounded(r.standard_normal((added, heads * group, dim)), "f16")
+    y = torch.empty((added, heads * group * dim), dtype=torch.float32, device="cuda")
+    ctx.adadim_mx4_attention(torch.from_numpy(q.reshape(added, -1)).half().cuda(), cache, ints(table), ints([0, added]), ints([n]), y, dim, max_new=added)
+    want, weight, slack = co.attention(q[-3:], small, np.arange(6)[None], [0, 3], [n], dim, dim ** -0.5)
+    check(host(y).astype(np.float64).reshape(added, heads * group, dim)[-3:], want, weight, slack, dim, n, 8.0, "f32")
+
+
 def test_same_bits_every_run(ctx):
     r = rng(9)
     dim, page, heads, group, n = 128, 64, 4, 8, 9000
