@@ -204,7 +204,8 @@ __device__ __forceinline__ float2p get(const float* p) {
 // What all lanes have the same goes into a scalar register: branches and loads by it are scalar then.  (Quotients come from the vector unit.)
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// The rows of tile `tile` of R rows: sequence s has the tiles from offsets[s] * group / R + s on (enough for it: each begins one of its own).
+// The rows of tile `tile` of R rows: the first `sequences` tiles are each sequence's first one; the further ones of sequence s are those from
+// offsets[s] * group / R on behind them (enough for it: its rows are R times as many, and one tile is there already).
 struct TileRows {
     int64_t first;                                // token of row 0
     int rows;                                     // rows of the tile, 0: no such tile
@@ -218,25 +219,35 @@ template <int R>
 __device__ __forceinline__ TileRows tile_rows(const Attention& a, int tile) {
     const int lane = threadIdx.x & 63;
     auto offset = [&](int s) { return static_cast<int>(min(max(int64_t(a.offsets[s]), int64_t(0)), a.tokens)); };
-    auto begin = [&](int o, int s) { return static_cast<int>(int64_t(o) * a.group / R) + s; };
-    int lo = 0, n = a.sequences, o0, o1, length;  // the last of the n from lo on that begins at or before the tile
-    while (n > 63) {
-        const int step = (n + 63) / 64, s = min(lo + lane * step, a.sequences);
-        const uint64_t at = __ballot(s < lo + n && begin(offset(s), s) <= tile);
-        const int last = at ? 63 - __builtin_clzll(at) : 0;
-        n = min(step, n - last * step);
-        lo += last * step;
-    }
-    {                                             // what is left, and all of it that is needed, in one load of each array
+    int lo = tile, o0, o1, length;
+    int64_t r0 = 0;
+    if (tile < a.sequences) {                     // one load of each array
+        const int o = offset(lo + (lane & 1));
+        length = a.lengths[lo];
+        o0 = __builtin_amdgcn_readlane(o, 0);
+        o1 = __builtin_amdgcn_readlane(o, 1);
+    } else {
+        const int extra = tile - a.sequences;
+        auto begin = [&](int o) { return static_cast<int>(int64_t(o) * a.group / R); };
+        int n = a.sequences;                      // the last of the n from lo on whose further tiles begin at or before this one
+        lo = 0;
+        while (n > 63) {
+            const int step = (n + 63) / 64, s = min(lo + lane * step, a.sequences);
+            const uint64_t at = __ballot(s < lo + n && begin(offset(s)) <= extra);
+            const int last = at ? 63 - __builtin_clzll(at) : 0;
+            n = min(step, n - last * step);
+            lo += last * step;
+        }
         const int s = lo + min(lane, n), o = offset(s), l = a.lengths[min(s, a.sequences - 1)];
-        const uint64_t at = __ballot(lane < n && begin(o, s) <= tile);
+        const uint64_t at = __ballot(lane < n && begin(o) <= extra);
         const int last = at ? 63 - __builtin_clzll(at) : 0;
         o0 = __builtin_amdgcn_readlane(o, last);
         o1 = __builtin_amdgcn_readlane(o, last + 1);
         length = __builtin_amdgcn_readlane(l, last);
         lo += last;
+        r0 = int64_t(extra - begin(o0) + 1) * R;
     }
-    const int64_t r0 = int64_t(tile - begin(o0, lo)) * R, have = int64_t(o1 - o0) * a.group;
+    const int64_t have = int64_t(o1 - o0) * a.group;
     const bool ok = r0 >= 0 && r0 < have;
     TileRows t;
     t.sequence = uniform(lo);
@@ -264,13 +275,14 @@ struct Work {
         return (tr.first - tr.token + token_of(a, row)) * a.ldy + int64_t(head_of(a, row)) * a.dim;
     }
 };
-template <int R>
+template <int R, bool LAST_FIRST>
 __device__ __forceinline__ Work work_of(const AttentionArgs& args, int y) {
     const Attention& a = args.a;
     Work w;
     w.shares = 0;
     w.head = blockIdx.x % a.heads;
-    w.tr = tile_rows<R>(a, args.tiles - 1 - static_cast<int>(blockIdx.x / a.heads));         // (the longest rows first)
+    const int tile = blockIdx.x / a.heads;
+    w.tr = tile_rows<R>(a, LAST_FIRST && tile >= a.sequences ? args.tiles - 1 - (tile - a.sequences) : tile);
     if (w.tr.rows == 0) return w;
     w.length = w.tr.length;
     w.before = w.length - w.tr.added;
@@ -371,7 +383,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, FEW_WAVES<D>) void mx4_attend_few(At
     constexpr int R = 16, TILES = D / 16, W = D / 32;
     typedef typename Dots<T>::vec vec;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
-    const Work w = work_of<R>(args, blockIdx.y);
+    const Work w = work_of<R, false>(args, blockIdx.y);
     if (w.shares == 0) return;
     int b = w.begin + wave;
     const int e = w.end;

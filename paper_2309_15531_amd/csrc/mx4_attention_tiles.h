@@ -121,7 +121,7 @@ __global__ __launch_bounds__(64 * TL_WAVES, 2) void mx4_attend_tiles(AttentionAr
     constexpr int BUFFERS = Stage<D>::BUFFERS, RECORDS = Stage<D>::RECORDS, BYTES = Stage<D>::BYTES;
     extern __shared__ __attribute__((aligned(16))) uint8_t s_stage[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-    const Work w = work_of<R>(args, blockIdx.y);
+    const Work w = work_of<R, true>(args, blockIdx.y);                                        // (behind the first tiles those that see most first)
     if (w.shares == 0) return;
 
     // ---- the wave's rows and the records that they see
@@ -262,7 +262,7 @@ __global__ __launch_bounds__(64 * TL_WAVES, 2) void mx4_attend_tiles(AttentionAr
 template <int D>
 __global__ __launch_bounds__(512) void mx4_attend_join(AttentionArgs args) {
     constexpr int R = 32 * TL_WAVES;
-    const Work w = work_of<R>(args, 0);
+    const Work w = work_of<R, true>(args, 0);
     const int row = 32 * blockIdx.y;
     if (w.shares > 1 && row < w.tr.rows) join_rows<R, D>(args, w, row, min(row + 32, w.tr.rows), 32);
 }
