@@ -242,6 +242,23 @@ def _array(t, what: str, dtype: str, shape) -> int:
     return t.data_ptr()
 
 
+def _int32s(*arrays):
+    """Addresses of contiguous int32 device tensors, each given as (tensor, number of elements, name)."""
+    at = []
+    for t, n, what in arrays:
+        if t.numel() != n or _DTYPES[t.dtype][0] != "torch.int32" or not t.is_contiguous() or not t.is_cuda:
+            _need(t, what, "int32")
+            raise ValueError(f"{what}: expected {n} elements, got shape {tuple(t.shape)}")
+        at.append(t.data_ptr())
+    return at
+
+
+def _width(table) -> int:
+    if table.dim() != 2:
+        raise ValueError(f"table: expected [sequences, width], got shape {tuple(table.shape)}")
+    return table.shape[1]
+
+
 def _matrix(t, what: str):
     """(address, TYPE_ number, rows, columns, row pitch in elements) of a device matrix in one of the float types whose
     rows may be pitched."""
@@ -568,24 +585,22 @@ class Context:
     def adadim_cache_reserve(self, held, added, page: int, table, free, count, lengths, offsets, slots, positions, left, lacking):
         """Pages from the stack free[0 .. count) for added[s] more tokens of each sequence, and their rows' slots and positions; all int32.
         table [sequences, width], offsets [sequences + 1]; slots and positions as many as there may be rows."""
-        i32, n, tokens = "torch.int32", held.numel(), slots.numel()
-        width = table.shape[-1]
-        rc = self._lib.adadim_cache_reserve(
-            self._h, _array(held, "held", i32, (n,)), _array(added, "added", i32, (n,)), n, page, _array(table, "table", i32, (n, width)), width,
-            _array(free, "free", i32, (free.numel(),)), free.numel(), _array(count, "count", i32, (1,)), _array(lengths, "lengths", i32, (n,)),
-            _array(offsets, "offsets", i32, (n + 1,)), _array(slots, "slots", i32, (tokens,)), _array(positions, "positions", i32, (tokens,)),
-            tokens, _array(left, "left", i32, (1,)), _array(lacking, "lacking", i32, (1,)))
+        n, tokens, pool, width = held.numel(), slots.numel(), free.numel(), _width(table)
+        (held, added, lengths, offsets, slots, positions, table, free, count, left, lacking) = _int32s(
+            (held, n, "held"), (added, n, "added"), (lengths, n, "lengths"), (offsets, n + 1, "offsets"), (slots, tokens, "slots"),
+            (positions, tokens, "positions"), (table, n * width, "table"), (free, pool, "free"), (count, 1, "count"), (left, 1, "left"),
+            (lacking, 1, "lacking"))
+        rc = self._lib.adadim_cache_reserve(self._h, held, added, n, page, table, width, free, pool, count, lengths, offsets, slots, positions, tokens,
+                                            left, lacking)
         if rc:
             self._check(rc)
 
     def adadim_cache_trim(self, held, kept, page: int, table, free, count, lengths, left):
         """The pages behind the first kept[s] tokens of each sequence back to the stack."""
-        i32, n = "torch.int32", held.numel()
-        width = table.shape[-1]
-        rc = self._lib.adadim_cache_trim(
-            self._h, _array(held, "held", i32, (n,)), _array(kept, "kept", i32, (n,)), n, page, _array(table, "table", i32, (n, width)), width,
-            _array(free, "free", i32, (free.numel(),)), free.numel(), _array(count, "count", i32, (1,)), _array(lengths, "lengths", i32, (n,)),
-            _array(left, "left", i32, (1,)))
+        n, pool, width = held.numel(), free.numel(), _width(table)
+        held, kept, lengths, table, free, count, left = _int32s((held, n, "held"), (kept, n, "kept"), (lengths, n, "lengths"),
+                                                                (table, n * width, "table"), (free, pool, "free"), (count, 1, "count"), (left, 1, "left"))
+        rc = self._lib.adadim_cache_trim(self._h, held, kept, n, page, table, width, free, pool, count, lengths, left)
         if rc:
             self._check(rc)
 
@@ -603,7 +618,7 @@ class Context:
         if v_kind != kind or v_tokens != tokens or v_cols != cols or heads < 1 or cols % heads:
             raise ValueError(f"K and V: one type and shape, columns a multiple of the cache's {heads} heads, got {tuple(K.shape)} and {tuple(V.shape)}")
         c, pages, page, heads = self._mx4_cache(cache, cols // heads)
-        return k, v, kind, tokens, ldk, ldv, _array(slots, "slots", "torch.int32", (tokens,)), c, pages, page, heads, cols // heads
+        return k, v, kind, tokens, ldk, ldv, _int32s((slots, tokens, "slots"))[0], c, pages, page, heads, cols // heads
 
     def adadim_mx4_cache_store(self, K, V, slots, cache):
         """Rows of K and V [tokens, heads * dim] (rows may be pitched) to their slots in cache [pages, heads, page / 32, record]."""
@@ -628,12 +643,10 @@ class Context:
         c, pages, page, heads = self._mx4_cache(cache, dim)
         if y_tokens != tokens or y_cols != cols or cols % dim:
             raise ValueError(f"Q and Y: one shape, columns a multiple of {dim}, got {tuple(Q.shape)} and {tuple(Y.shape)}")
-        n = lengths.numel()
-        width = table.shape[-1]
-        rc = self._lib.adadim_mx4_attention(
-            self._h, q, kind, tokens, ldq, cols // dim, c, pages, page, heads, dim, _array(table, "table", "torch.int32", (n, width)), width, n,
-            _array(offsets, "offsets", "torch.int32", (n + 1,)), _array(lengths, "lengths", "torch.int32", (n,)), y, y_kind, ldy,
-            dim ** -0.5 if scale is None else scale, 1 if causal else 0, window, max_new, max_length)
+        n, width = lengths.numel(), _width(table)
+        table, offsets, lengths = _int32s((table, n * width, "table"), (offsets, n + 1, "offsets"), (lengths, n, "lengths"))
+        rc = self._lib.adadim_mx4_attention(self._h, q, kind, tokens, ldq, cols // dim, c, pages, page, heads, dim, table, width, n, offsets, lengths, y,
+                                            y_kind, ldy, dim ** -0.5 if scale is None else scale, 1 if causal else 0, window, max_new, max_length)
         if rc:
             self._check(rc)
 
