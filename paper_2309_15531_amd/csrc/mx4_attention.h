@@ -66,8 +66,9 @@ template <int D>
 struct ValueBytes {
     static constexpr int W = D / 32;
     uint32_t words[W], scale_word;
-    __device__ __forceinline__ void load(const uint8_t* r, int t, int lane) {
-        const int m = lane & 15, g = lane >> 4;
+    // dim: elements that are not filled up; lanes of units behind them (nobody stores what these come to) read the first unit's bytes again, not their own
+    __device__ __forceinline__ void load(const uint8_t* r, int t, int lane, int dim) {
+        const int m = (lane & 15) * (D / 16) < dim ? lane & 15 : 0, g = lane >> 4;
         const uint32_t* p = reinterpret_cast<const uint32_t*>(r + Record<D>::VALUES + ((g * 16 + m) * 8 + 4 * t) * Record<D>::UNIT);
 #pragma unroll
         for (int c = 0; c < W; ++c) words[c] = p[c];
@@ -399,7 +400,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, FEW_WAVES<D>) void mx4_attend_few(At
     KeyBytes<D> kb[2];
     ValueBytes<D> vb[2];
     auto load_keys = [&](const uint8_t* r) { kb[0].load(r, 0, lane); kb[1].load(r, 1, lane); };
-    auto load_values = [&](const uint8_t* r) { vb[0].load(r, 0, lane); vb[1].load(r, 1, lane); };
+    auto load_values = [&](const uint8_t* r) { vb[0].load(r, 0, lane, a.dim); vb[1].load(r, 1, lane, a.dim); };
     if (b < e) {
         load_keys(record(page, b));
         load_values(record(page, b));

@@ -173,7 +173,7 @@ __global__ __launch_bounds__(64 * TL_WAVES, 2) void mx4_attend_tiles(AttentionAr
         const uint8_t* const rec = a.cache + (((p * a.heads + w.head) << per_page) + (r & ((1 << per_page) - 1))) * Record<D>::BYTES;
         page = page_ahead(r + RECORDS);
         kb.load(rec, half, lane);
-        vb.load(rec, half, lane);
+        vb.load(rec, half, lane, a.dim);
     };
     auto bring = [&](int first, int buffer) {
         const int r = first + part;
