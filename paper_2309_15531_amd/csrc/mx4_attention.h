@@ -27,6 +27,7 @@ struct AttentionArgs {
     int tiles;                                    // row tiles, of which each sequence has one that may not exist
     int least;                                    // records that a share has at least
     int most;                                     // shares of a tile at most
+    int round;                                    // workgroups that run at a time, where shares are to be alike over all sequences; or 0
     unsigned* tickets;
     float* parts;
 };
@@ -289,7 +290,27 @@ __device__ __forceinline__ Work work_of(const AttentionArgs& args, int y) {
     w.before = w.length - w.tr.added;
     const int begin = uniform(w.sees_from(a, w.tr.token) >> 5), end = uniform((w.sees_to(a, w.token_of(a, w.tr.rows - 1)) + 31) >> 5);
     const int records = max(end - begin, 0);
-    const int share = uniform(max((records + args.most - 1) / args.most, args.least));
+    int least = args.least;
+    if constexpr (!LAST_FIRST) {
+        // Shares as long in one sequence as in the other, so long that all of them (those that are not divisible among them) are whole rounds
+        // of workgroups; one sequence to a lane.  2 sequences to 100003: 131 us, 147 with as many shares for each.
+        if (args.round > 0) {
+            const int lane = threadIdx.x & 63, s = min(lane, a.sequences - 1);
+            const int o0 = min(max(a.offsets[s], 0), static_cast<int>(a.tokens)), o1 = min(max(a.offsets[s + 1], o0), static_cast<int>(a.tokens));
+            const int64_t length = min(max(int64_t(a.lengths[s]), int64_t(0)), a.width << a.log_page);
+            const int64_t from = a.window ? max(length - (o1 - o0) + 1 - a.window, int64_t(0)) : 0;
+            float tiles = lane < a.sequences ? static_cast<float>((int64_t(o1 - o0) * a.group + R - 1) / R) : 0.0f;
+            float all = tiles * static_cast<float>(((length + 31) >> 5) - (from >> 5));
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                tiles += __shfl_xor(tiles, d);
+                all += __shfl_xor(all, d);
+            }
+            const float items = tiles * a.heads, rounds = args.round * fmaxf(ceilf(1.5f * items / args.round), 1.0f);
+            least = uniform(max(static_cast<int>(all * a.heads / (rounds - 0.5f * items)) + 1, args.least));
+        }
+    }
+    const int share = uniform(max((records + args.most - 1) / args.most, least));
     const int shares = uniform(max((records + share - 1) / share, 1));
     w.shares = y < shares ? shares : 0;
     w.begin = begin + share * y;

@@ -12,12 +12,14 @@ namespace mx4 {
 // to the join), a record of eight waves 0.15: cut below 64 records only while the shares are one round.  Many rows: one round (2 x 4000 positions, 1000
 // new ones, 32 heads: 125 us, 138 with two); a record takes 0.5 us there.
 struct Shares { int most, least; };
+// Whether the shares of several sequences are made alike on the device (work_of): longer ones then have more of them than two rounds would give each.
+inline bool alike(const Attention& a) { return a.sequences > 1 && a.sequences <= 64; }
 inline Shares shares_of(const Attention& a, int64_t tiles, int rows, bool few) {
     const int64_t seen = a.window ? std::min(a.max_length, a.window + a.max_new) : a.max_length;
     const int64_t records = (seen + 31) / 32 + 1;
     // tiles that hold rows, as far as the host can tell
     const int64_t real = std::max<int64_t>(1, std::min(tiles, a.sequences * ((a.max_new * a.group + rows - 1) / rows)) * a.heads);
-    const int64_t wanted = (few ? 1024 : 256) / real;
+    const int64_t wanted = (few ? alike(a) ? 2048 : 1024 : 256) / real;
     const int least = !few ? 16 : real * ((records + 31) / 32) > 512 ? 64 : 32;
     // (and no more than 35 MB of sums, 270 of many rows, where the host knows less of the sequences than there is)
     const int64_t n = std::min({wanted, records / least, (few ? AT_TICKETS / 2 : 2048) / (tiles * a.heads)});
@@ -26,10 +28,10 @@ inline Shares shares_of(const Attention& a, int64_t tiles, int rows, bool few) {
 
 // The launch's tiles, shares and scratch; R: rows of a tile.
 template <int R, int D>
-int laid_out(adadim_ctx* ctx, const Attention& a, bool keys, AttentionArgs& args, dim3& grid) {
+int laid_out(adadim_ctx* ctx, const Attention& a, bool few, AttentionArgs& args, dim3& grid) {
     const int64_t tiles = a.tokens * a.group / R + a.sequences;
-    const Shares s = shares_of(a, tiles, R, keys);
-    args = AttentionArgs{a, static_cast<int>(tiles), s.least, s.most, nullptr, nullptr};
+    const Shares s = shares_of(a, tiles, R, few);
+    args = AttentionArgs{a, static_cast<int>(tiles), s.least, s.most, few && s.most > 1 && alike(a) ? (D <= 128 ? 512 : 256) : 0, nullptr, nullptr};
     grid = dim3(static_cast<unsigned>(tiles * a.heads), s.most);
     if (s.most == 1) return ADADIM_OK;
     void* shared = nullptr;
