@@ -501,8 +501,8 @@ int adadim_mx4_cache_load(adadim_ctx* ctx, const int32_t* slots, int64_t tokens,
  *            are not written.
  *   lengths  int32 [sequences]: inside [0, width * page] (values outside are taken as the nearer end)
  *   scale    positive;  window  0: none
- *   max_new, max_length  the most new tokens and positions that a sequence has, as far as the host knows (0: unknown): what the launch is
- *            laid out for.  Results do not depend on them but for the order of sums.
+ *   max_new, max_length  the most new tokens and positions that a sequence has, as far as the host knows (0: unknown; the mean of the new tokens and
+ *            all that the table has room for are taken): what the launch is laid out for.  Results do not depend on them but for the order of sums.
  * A row that sees nothing is zeros.  A row that sees a position stored with an infinity or a NaN is NaN; positions that it does not see do
  * not touch it, whatever they hold.  Scores and sums are fp32 and keys and values enter exactly; the weights 2^(score - largest) are rounded
  * to fp16 (2^-33 of the row's largest is kept) for the product with the values.  Sums in a fixed order: same bits every run.

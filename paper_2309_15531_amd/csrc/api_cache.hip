@@ -149,7 +149,7 @@ int adadim_mx4_attention(adadim_ctx* ctx, const void* Q, int q_type, int64_t tok
         return adadim_fail(ctx, ADADIM_EALIGN, "%s: cache must be 16-byte, the others element aligned", me);
     const int64_t most = width * page;
     const mx4::Attention a{Q, tokens, ldq, cache, pages, log_of_page(page), heads, group, dim, table, width, sequences, offsets, lengths, Y, y_type, ldy,
-                           scale, causal, window < most ? window : 0, max_new < 1 || max_new > tokens ? tokens : max_new,
+                           scale, causal, window < most ? window : 0, max_new < 1 ? (tokens + sequences - 1) / sequences : max_new > tokens ? tokens : max_new,
                            max_length < 1 || max_length > most ? most : max_length};
     return launch_mx4_attention(ctx, a, q_type);
 }

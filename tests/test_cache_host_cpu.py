@@ -34,6 +34,10 @@ for new, length, group, want in ((1, 100, 8, ['few']), (32, 100, 8, ['few']), (3
     fake.fake_reset()
     assert attend(ctx, new, length, group=group) == OK, lib.adadim_last_error(ctx)
     assert {ATTEND} == ['mx4_attend_' + w for w in want], (new, length, names())
+# of new tokens nothing is known: the mean of 64 sequences' 64 is one each
+fake.fake_reset()
+assert lib.adadim_mx4_attention(ctx, A, 0, c_int64(64), c_int64(8192), 64, A, c_int64(1 << 20), 64, 8, 128, A, c_int64(16), 64, A, A, A, 0, c_int64(8192),
+                                c_float(1.0), 1, c_int64(0), c_int64(0), c_int64(0)) == OK and {ATTEND} == ['mx4_attend_few'], names()
 fake.fake_reset()
 assert attend(ctx, 1, 1000, sequences=4096) == OK and {ATTEND} == ['mx4_attend_few']
 for tokens, want in ((0, 1), (4096, 1), (4097, 2), (1 << 20, 2)):
