@@ -266,7 +266,7 @@ __device__ __forceinline__ TileRows tile_rows(const Attention& a, int tile) {
 struct Work {
     TileRows tr;
     int head, length, before;                     // before + t: the position of new token t
-    int begin, end, shares;
+    int shares, begin, end;
     __device__ __forceinline__ int token_of(const Attention& a, int row) const { return tr.token + (tr.rest + row) / a.group; }
     __device__ __forceinline__ int head_of(const Attention& a, int row) const { return head * a.group + (tr.rest + row) % a.group; }
     __device__ __forceinline__ int sees_to(const Attention& a, int token) const { return a.causal ? min(max(before + token + 1, 0), length) : length; }
@@ -312,7 +312,8 @@ __device__ __forceinline__ Work work_of(const AttentionArgs& args, int y) {
     }
     const int share = uniform(max((records + args.most - 1) / args.most, least));
     const int shares = uniform(max((records + share - 1) / share, 1));
-    w.shares = y < shares ? shares : 0;
+    if (y >= shares) return w;
+    w.shares = shares;
     w.begin = begin + share * y;
     w.end = min(w.begin + share, end);
     return w;

@@ -228,8 +228,7 @@ class CachePages:
 
 
 class Mx4Cache:
-    """A layer's keys and values, `heads` heads of `dim` elements, 4.25 bits each: 17 KB a token for 32 heads of 128, keys and values, where
-    fp16 takes 64."""
+    """A layer's keys and values, `heads` heads of `dim` elements, 4.25 bits each: 4.25 KB a token for 32 heads of 128, where fp16 takes 16."""
 
     def __init__(self, pages: CachePages, heads: int, dim: int):
         self.ctx, self.pages, self.heads, self.dim = pages.ctx, pages, heads, dim

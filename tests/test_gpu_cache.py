@@ -335,6 +335,15 @@ def test_masks(ctx, case, causal, window):
     run_attention(ctx, 200 + case, added, lengths, heads, group, dim, page, "f16", "f32", causal, window, hints=(max(added), max(lengths)))
 
 
+@pytest.mark.parametrize("dim,added,lengths,window", [(64, [1, 2, 1], [4200, 130, 2500], 0), (128, [1, 1, 1, 0, 1], [2100, 33, 5000, 400, 2], 0),
+                                                      (128, [3, 9], [6000, 2500], 2200), (256, [1, 1], [2600, 4400], 0), (100, [7, 1], [40, 3000], 0),
+                                                      (128, [120, 90], [4000, 5000], 0)])
+def test_long_and_short_sequences_in_shares(ctx, dim, added, lengths, window):
+    """Shares of the same length over sequences of unlike ones, more for the longer; and many rows in shares."""
+    run_attention(ctx, 500 + dim, added, lengths, 1, 3, dim, 64, "f16", "f32", window=window, hints=(max(added), max(lengths)))
+    run_attention(ctx, 501 + dim, added, lengths, 1, 3, dim, 64, "bf16", "bf16", window=window, hints=(1, 0))
+
+
 @pytest.mark.parametrize("most", [1, 20, 1000])
 def test_rows_that_see_nothing_are_zeros(ctx, most):
     """No positions, fewer than rows, pages that are not there, and sequences without rows."""
