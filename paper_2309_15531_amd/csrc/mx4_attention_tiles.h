@@ -1,8 +1,8 @@
 // Attention of many rows over a paged cache in mx4 (the mathematics: mx4_attention.h).
 //
 // A workgroup has eight waves, two a SIMD, of 32 rows each: while one weighs scores on the vector unit the other multiplies.  Its records go
-// through LDS four at a time, each converted by two of the waves, half of its positions each: what costs most to prepare, the
-// values of codes with their scales, is done once for all 256 rows.  They lie there as the 32-row instruction takes
+// through LDS four at a time, converted by one or two of the waves each: what costs most to prepare, the values of codes with their
+// scales, is done once for all 256 rows.  They lie there as the 32-row instruction takes
 // its left operand, lane by lane in 16 bytes (no bank is met twice in a read): keys [step][half][position], with step s of half h the
 // elements h D/2 + 8 s ..; values [tile jj][step][half][row r], with row r of tile jj the element (D/16) (r % 16) + (D/32) (r / 16) + jj, and
 // the step's positions 4 h .. and 8 + 4 h .. of 16 as S^T leaves them in a lane of half h.
@@ -154,10 +154,13 @@ __global__ __launch_bounds__(64 * TL_WAVES, 2) void mx4_attend_tiles(AttentionAr
     // whether all the pages are there, looked up once for all: a scalar load for each record would be waited for
     bool whole = true;
     for (int p = (w.begin >> per_page) + lane, end = w.begin < w.end ? (w.end - 1) >> per_page : -1; __any(p <= end); p += 64) whole = whole && !__any(p <= end && !there(table[p]));
-    // the wave's part of a stage: half a record
-    const int part = wave & 3, half = wave >> 2;
-    KeyBytes<D> kb;
-    ValueBytes<D> vb;
+    // The first four waves convert a record of a stage each: they are issued first and would wait for the others, which are left more of the
+    // vector unit so (4 % less time than with half a record to each of eight).  With 256 elements that takes too many registers: half a record each.
+    constexpr int OWN = D > 128 ? 1 : 2;          // halves of a record
+    const int part = wave & 3, own = OWN == 2 ? 0 : wave >> 2;
+    const bool converts = OWN == 1 || wave < 4;
+    KeyBytes<D> kb[OWN];
+    ValueBytes<D> vb[OWN];
     // (the page's number a stage ahead, by a vector load: waiting for a scalar one would wait for LDS, too, and the other way)
     auto page_ahead = [&](int r) {
         int i = r < w.end ? r >> per_page : 0;
@@ -167,20 +170,26 @@ __global__ __launch_bounds__(64 * TL_WAVES, 2) void mx4_attend_tiles(AttentionAr
     int page = page_ahead(w.begin + part);
     auto fetch = [&](int first) {
         const int r = first + part;
-        if (r >= w.end) return;
+        if (r >= w.end || !converts) return;
         const int id = uniform(page);
         const int64_t p = there(id) ? id : 0;                 // (a page that is not there is not used; page 0 is)
         const uint8_t* const rec = a.cache + (((p * a.heads + w.head) << per_page) + (r & ((1 << per_page) - 1))) * Record<D>::BYTES;
         page = page_ahead(r + RECORDS);
-        kb.load(rec, half, lane);
-        vb.load(rec, half, lane, a.dim);
+#pragma unroll
+        for (int i = 0; i < OWN; ++i) {
+            kb[i].load(rec, own + i, lane);
+            vb[i].load(rec, own + i, lane, a.dim);
+        }
     };
     auto bring = [&](int first, int buffer) {
         const int r = first + part;
-        if (r >= w.end) return;
+        if (r >= w.end || !converts) return;
         uint8_t* const at = s_stage + (buffer * RECORDS + part) * BYTES;
-        convert_keys<T, D>(kb, at, half, lane);
-        convert_values<D>(vb, at, half, lane, w.length - RECORD * r);
+#pragma unroll
+        for (int i = 0; i < OWN; ++i) {
+            convert_keys<T, D>(kb[i], at, own + i, lane);
+            convert_values<D>(vb[i], at, own + i, lane, w.length - RECORD * r);
+        }
     };
     auto hide = [&](float16v& s, int r) {
         if (r >= all_from && r < all_to) return;
@@ -190,28 +199,18 @@ __global__ __launch_bounds__(64 * TL_WAVES, 2) void mx4_attend_tiles(AttentionAr
             s[i] = key >= lo && key < hi ? s[i] : -INFINITY;
         }
     };
-    // The SIMD's other wave converts half a stage later: one's conversion runs under the other's products.
-    auto next_stage = [&](int first, int buffer) {
-        bring(first + RECORDS, buffer ^ 1);
-        fetch(first + 2 * RECORDS);
-    };
     auto stage = [&](int first, int buffer) {
         const uint8_t* const at = s_stage + buffer * RECORDS * BYTES;
         const int r1 = min(first + RECORDS, to);
-#pragma unroll
-        for (int part = 0; part < 2; ++part) {
-            if (BUFFERS == 2 && half == part) next_stage(first, buffer);
-            const int p1 = min(first + RECORDS / 2 * (part + 1), r1);
-            for (int r = max(first + RECORDS / 2 * part, from); r < p1; ++r) {
-                if (!whole && !there(page_of(r))) continue;
-                const uint8_t* const rec = at + (r - first) * BYTES;
-                float16v s = t.scores(rec, lane);
-                hide(s, r);
-                t.raise(s);
-                half8v p[2];
-                t.weigh(s, p);
-                t.values(rec, lane, p);
-            }
+        for (int r = max(first, from); r < r1; ++r) {
+            if (!whole && !there(page_of(r))) continue;
+            const uint8_t* const rec = at + (r - first) * BYTES;
+            float16v s = t.scores(rec, lane);
+            hide(s, r);
+            t.raise(s);
+            half8v p[2];
+            t.weigh(s, p);
+            t.values(rec, lane, p);
         }
     };
     fetch(w.begin);
@@ -221,6 +220,8 @@ __global__ __launch_bounds__(64 * TL_WAVES, 2) void mx4_attend_tiles(AttentionAr
     int buffer = 0;
     for (int first = w.begin; first < w.end; first += RECORDS) {
         if constexpr (BUFFERS == 2) {
+            bring(first + RECORDS, buffer ^ 1);
+            fetch(first + 2 * RECORDS);
             stage(first, buffer);
             __syncthreads();
             buffer ^= 1;
