@@ -9,8 +9,8 @@
 //
 // Bound by vector and matrix instructions together: of the 1000 clocks that a record takes a wave (two waves a SIMD, 2.1 GHz) the matrix pipe is
 // busy 512 and the vector unit about 500 (16 exponentials, 16 sums, 16 fma, 8 roundings, maxima, its share of the conversion).  4096 tokens into an
-// empty cache, 32 heads of 128: 149 us, 920 TFLOP/s; 2 x 2048 tokens over 16384, 64 heads over 8: 1417 us, 1050 TFLOP/s.  What did not
-// help there (that second case, beside 1420 to 1490 as the cards go): scores one record ahead in a wave, 1850 (in order or left to the
+// empty cache, 32 heads of 128: 148 us, 930 TFLOP/s; 2 x 2048 tokens over 16384, 64 heads over 8: 1389 us, 1070 TFLOP/s.  What did not
+// help there (that second case, beside 1420 to 1490 as the cards went): scores one record ahead in a wave, 1850 (in order or left to the
 // compiler); operands read from LDS ahead of use, 1500; waves' priorities, 1490; workgroups of six waves, three a SIMD, 1940, of four 1600;
 // one buffer for two, 1480.  Every wave converting for itself, 64 rows of 16-row tiles: 5400.
 #pragma once
