@@ -182,6 +182,32 @@ def test_a_recorded_attention_in_shares(added, group):
     ctx.close()
 
 
+def test_two_contexts_at_once():
+    """Calls that share positions by way of scratch, on two streams at the same time: each context has its own."""
+    dim, page, heads, group, n = 128, 64, 4, 4, 6000
+    streams, made, got = [torch.cuda.Stream() for _ in range(2)], [], [[], []]
+    for i, stream in enumerate(streams):
+        with torch.cuda.stream(stream):
+            ctx = B.Context()
+            pages = mx4.CachePages(ctx, 300, page, 2, 100)
+            cache = mx4.Mx4Cache(pages, heads, dim)
+            rows = pages.add(ints([n, n // 3]), n + n // 3)
+            cache.store(*(randn(20 + 2 * i + j, n + n // 3, heads * dim).half() for j in range(2)), rows.slots)
+            q = [randn(30 + i, k, heads * group * dim).half() for k in (2, 300)]
+            offsets = [ints([0, 1, 2]), ints([0, 200, 300])]
+            made.append((ctx, cache, q, offsets, [cache.attend(x, o, max_new=m, max_length=n).clone() for x, o, m in zip(q, offsets, (1, 200))]))
+    torch.cuda.synchronize()
+    for turn in range(20):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                ctx, cache, q, offsets, _ = made[i]
+                got[i].append(cache.attend(q[turn % 2], offsets[turn % 2], max_new=(1, 200)[turn % 2], max_length=n))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(y, made[i][4][turn % 2]) and torch.isfinite(y).all() for turn, y in enumerate(got[i]))
+        made[i][0].close()
+
+
 def test_the_example_runs(capsys, monkeypatch):
     monkeypatch.setattr(sys, "argv", ["mx4_attention.py", "--heads", "4", "--kv-heads", "2", "--dim", "64", "--prompt", "150", "--sequences", "3", "--steps", "2"])
     spec = importlib.util.spec_from_file_location("mx4_attention", os.path.join(ROOT, "examples", "mx4_attention.py"))
