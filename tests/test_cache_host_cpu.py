@@ -40,10 +40,10 @@ assert lib.adadim_mx4_attention(ctx, A, 0, c_int64(64), c_int64(8192), 64, A, c_
                                 c_float(1.0), 1, c_int64(0), c_int64(0), c_int64(0)) == OK and {ATTEND} == ['mx4_attend_few'], names()
 fake.fake_reset()
 assert attend(ctx, 1, 1000, sequences=4096) == OK and {ATTEND} == ['mx4_attend_few']
-for tokens, want in ((0, 1), (4096, 1), (4097, 2), (1 << 20, 2)):
+for tokens, want in ((0, 1), (8192, 1), (8193, 2), (1 << 20, 2)):
     fake.fake_reset()
     assert reserve(ctx, tokens) == OK and len(names()) == want, (tokens, names())
-for n, width, want in ((1, 16384, 1), (1, 16385, 2), (4096, 4, 1), (4096, 5, 2)):
+for n, width, want in ((1, 65536, 1), (1, 65537, 2), (4096, 16, 1), (4096, 17, 2)):
     fake.fake_reset()
     assert trim(ctx, n, width) == OK and len(names()) == want, (n, width, names())
 """))
@@ -72,8 +72,8 @@ assert attend(ctx, 1, 100000) == OK
 
 def test_scratch_does_not_grow_while_a_graph_is_recorded(run):
     run(body("""
-for call, small in ((lambda c: attend(c, 1, 100000), lambda c: attend(c, 1, 100)), (lambda c: reserve(c, 5000), lambda c: reserve(c, 50)),
-                    (lambda c: trim(c, 1, 20000), lambda c: trim(c, 1, 20))):
+for call, small in ((lambda c: attend(c, 1, 100000), lambda c: attend(c, 1, 100)), (lambda c: reserve(c, 9000), lambda c: reserve(c, 50)),
+                    (lambda c: trim(c, 1, 70000), lambda c: trim(c, 1, 20))):
     ctx, g = context(), c_void_p()
     assert small(ctx) == OK
     assert lib.adadim_capture_begin(ctx) == OK

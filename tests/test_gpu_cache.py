@@ -99,7 +99,7 @@ def test_reserve_takes_all_or_nothing(ctx, held, added, count, tokens):
     same(got, want)
 
 
-@pytest.mark.parametrize("n,page,long", [(1, 32, 1), (1, 32, 3000), (5, 64, 700), (64, 64, 3000), (300, 32, 5000), (1500, 32, 50), (4096, 64, 300)])
+@pytest.mark.parametrize("n,page,long", [(1, 32, 1), (1, 32, 3000), (5, 64, 700), (64, 64, 3000), (300, 32, 5000), (300, 32, 9000), (1500, 32, 50), (4096, 64, 300)])
 def test_trim_is_the_oracles(ctx, n, page, long):
     r = rng(2, n, page)
     held = r.integers(0, long + 1, n)
@@ -132,7 +132,7 @@ def test_trim_drops_what_the_pool_has_no_room_for(ctx):
     assert f[:4].tolist() == want["free"] and f[4:].tolist() == guard[4:].tolist() and lengths.tolist() == want["lengths"] and left.tolist() == [4]
 
 
-@pytest.mark.parametrize("tokens", [100, 6000])
+@pytest.mark.parametrize("tokens", [100, 9000])
 def test_lengths_and_count_in_place(ctx, tokens):
     """A batch that grows step by step with one array of lengths and one count, and gives all back."""
     r = rng(3, tokens)
