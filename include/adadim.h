@@ -459,7 +459,8 @@ int64_t adadim_mx4_cache_bytes(int64_t pages, int page, int heads, int dim);
  *   lacking  int32 [1]: 0, or what the call was refused for on the device: the number of pages that the stack is short of; -1 where a
  *            sequence would outgrow its row of the table, the rows are too few, or a number is negative.  Then nothing is taken:
  *            lengths are held, offsets 0, slots and positions -1, left is count, and the table stays.
- * All arrays on the device; the host learns nothing of them.  sequences 1..4096.  Arrays must not overlap but for those named.
+ * All arrays on the device; the host learns nothing of them.  sequences 1..4096, sequences * width < 2^31.  Arrays must not overlap but for
+ * those named.
  */
 int adadim_cache_reserve(adadim_ctx* ctx, const int32_t* held, const int32_t* added, int sequences, int page, int32_t* table, int64_t width,
                          const int32_t* free, int64_t pool, const int32_t* count, int32_t* lengths, int32_t* offsets, int32_t* slots,

@@ -41,9 +41,11 @@ static int pages_checked(adadim_ctx* ctx, const char* me, const void* held, cons
     if (sequences <= 0 || sequences > MOST_SEQUENCES)
         return adadim_fail(ctx, ADADIM_EINVAL, "%s: sequences must be in [1,%d], got %d", me, MOST_SEQUENCES, sequences);
     if (log_of_page(page) == 0) return adadim_fail(ctx, ADADIM_EINVAL, "%s: page must be a power of two in [32,65536], got %d", me, page);
-    if (!pages_ok(width, page) || !pages_ok(pool, page))
-        return adadim_fail(ctx, ADADIM_EINVAL, "%s: need 1 <= width, pool and less than 2^31 positions in them (width=%lld pool=%lld page=%d)", me,
-                           (long long)width, (long long)pool, page);
+    // (sums of pages over the sequences are 32-bit numbers)
+    if (!pages_ok(width, page) || !pages_ok(pool, page) || sequences * width > INT32_MAX)
+        return adadim_fail(ctx, ADADIM_EINVAL,
+                           "%s: need 1 <= width, pool, less than 2^31 positions in them and entries in the table (sequences=%d width=%lld pool=%lld page=%d)", me,
+                           sequences, (long long)width, (long long)pool, page);
     if (!held || !change || !table || !free || !count || !lengths || !left)
         return adadim_fail(ctx, ADADIM_ENULL, "%s: a required pointer is NULL", me);
     if (!aligned_to(held, 4) || !aligned_to(change, 4) || !aligned_to(table, 4) || !aligned_to(free, 4) || !aligned_to(count, 4) ||

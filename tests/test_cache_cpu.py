@@ -105,7 +105,7 @@ def test_page_refusals(ctx, name):
         m = {"offsets": A16, "slots": A16, "positions": A16, "tokens": 5, "lacking": A16, **more}
         return ctx.raw(name, held, change, n, page, table, width, free, pool, count, lengths, m["offsets"], m["slots"], m["positions"], m["tokens"], left,
                        m["lacking"])
-    for bad in ({"n": 0}, {"n": 4097}, {"page": 16}, {"page": 96}, {"page": 1 << 17}, {"width": 0}, {"pool": 0}, {"width": 1 << 25}, {"pool": 1 << 25}):
+    for bad in ({"n": 0}, {"n": 4097}, {"page": 16}, {"page": 96}, {"page": 1 << 17}, {"width": 0}, {"pool": 0}, {"width": 1 << 25}, {"pool": 1 << 25}, {"n": 4096, "width": 1 << 19}):
         assert call(**bad) == B.EINVAL, bad
         assert name in ctx.last_error()
     pointers = ["held", "change", "table", "free", "count", "lengths", "left"]
