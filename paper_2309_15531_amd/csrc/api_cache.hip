@@ -141,8 +141,8 @@ int adadim_mx4_attention(adadim_ctx* ctx, const void* Q, int q_type, int64_t tok
         return adadim_fail(ctx, ADADIM_EINVAL,
                            "%s: need tokens in [0,2^20], ldq, ldy >= q_heads * dim, fewer than 2^24 tiles of 16 rows (tokens=%lld ldq=%lld ldy=%lld)", me,
                            (long long)tokens, (long long)ldq, (long long)ldy);
-    if (!(scale > 0.0f && scale <= 3e38f) || (causal != 0 && causal != 1) || window < 0)
-        return adadim_fail(ctx, ADADIM_EINVAL, "%s: need a positive finite scale, causal 0 or 1, window >= 0 (scale=%g causal=%d window=%lld)", me, scale,
+    if (!(scale > 0.0f && scale <= 2e38f) || (causal != 0 && causal != 1) || window < 0)
+        return adadim_fail(ctx, ADADIM_EINVAL, "%s: need a scale in (0, 2e38], causal 0 or 1, window >= 0 (scale=%g causal=%d window=%lld)", me, scale,
                            causal, (long long)window);
     if (tokens == 0) return ADADIM_OK;
     if (!Q || !cache || !table || !offsets || !lengths || !Y) return adadim_fail(ctx, ADADIM_ENULL, "%s: a required pointer is NULL", me);
