@@ -481,7 +481,7 @@ int adadim_cache_trim(adadim_ctx* ctx, const int32_t* held, const int32_t* kept,
  * 49152 is kept, and blocks of less than 2^-21 are kept to 2^-24.
  *   K, V   [tokens, heads * dim] of type F16, BF16 or F32, row pitches ldk, ldv; any alignment of an element
  *   slots  int32 [tokens]: each at most once; a row with one outside the pool is not stored
- * tokens 0 to 2^20.
+ * tokens 0 to 2^20, tokens * heads less than 2^29.
  */
 int adadim_mx4_cache_store(adadim_ctx* ctx, const void* K, const void* V, int type, int64_t tokens, int64_t ldk, int64_t ldv,
                            const int32_t* slots, uint8_t* cache, int64_t pages, int page, int heads, int dim);

@@ -92,9 +92,10 @@ int adadim_mx4_cache_store(adadim_ctx* ctx, const void* K, const void* V, int ty
     if (!is_float_type(type)) return adadim_fail(ctx, ADADIM_EINVAL, "%s: type must be F16, BF16 or F32, got %d", me, type);
     const int rc = cache_checked(ctx, me, pages, page, heads, dim);
     if (rc != ADADIM_OK) return rc;
-    if (tokens < 0 || tokens > MOST_TOKENS || ldk < int64_t(heads) * dim || ldv < int64_t(heads) * dim)
-        return adadim_fail(ctx, ADADIM_EINVAL, "%s: need tokens in [0,2^20], ldk, ldv >= heads * dim (tokens=%lld ldk=%lld ldv=%lld)", me, (long long)tokens,
-                           (long long)ldk, (long long)ldv);
+    if (tokens < 0 || tokens > MOST_TOKENS || ldk < int64_t(heads) * dim || ldv < int64_t(heads) * dim || !launchable((tokens + 31) / 32 * heads, 256))
+        return adadim_fail(ctx, ADADIM_EINVAL,
+                           "%s: need tokens in [0,2^20], ldk, ldv >= heads * dim, fewer than 2^24 runs of 32 rows of a head (tokens=%lld heads=%d ldk=%lld ldv=%lld)",
+                           me, (long long)tokens, heads, (long long)ldk, (long long)ldv);
     if (tokens == 0) return ADADIM_OK;
     if (!K || !V || !slots || !cache) return adadim_fail(ctx, ADADIM_ENULL, "%s: K, V, slots or cache is NULL", me);
     if (!aligned16(cache) || !aligned_to(slots, 4) || !aligned_to(K, type_size(type)) || !aligned_to(V, type_size(type)))
@@ -109,9 +110,10 @@ int adadim_mx4_cache_load(adadim_ctx* ctx, const int32_t* slots, int64_t tokens,
     if (!is_float_type(type)) return adadim_fail(ctx, ADADIM_EINVAL, "%s: type must be F16, BF16 or F32, got %d", me, type);
     const int rc = cache_checked(ctx, me, pages, page, heads, dim);
     if (rc != ADADIM_OK) return rc;
-    if (tokens < 0 || tokens > MOST_TOKENS || ldk < int64_t(heads) * dim || ldv < int64_t(heads) * dim)
-        return adadim_fail(ctx, ADADIM_EINVAL, "%s: need tokens in [0,2^20], ldk, ldv >= heads * dim (tokens=%lld ldk=%lld ldv=%lld)", me, (long long)tokens,
-                           (long long)ldk, (long long)ldv);
+    if (tokens < 0 || tokens > MOST_TOKENS || ldk < int64_t(heads) * dim || ldv < int64_t(heads) * dim || !launchable((tokens + 31) / 32 * heads, 256))
+        return adadim_fail(ctx, ADADIM_EINVAL,
+                           "%s: need tokens in [0,2^20], ldk, ldv >= heads * dim, fewer than 2^24 runs of 32 rows of a head (tokens=%lld heads=%d ldk=%lld ldv=%lld)",
+                           me, (long long)tokens, heads, (long long)ldk, (long long)ldv);
     if (tokens == 0) return ADADIM_OK;
     if (!K || !V || !slots || !cache) return adadim_fail(ctx, ADADIM_ENULL, "%s: K, V, slots or cache is NULL", me);
     if (!aligned16(cache) || !aligned_to(slots, 4) || !aligned_to(K, type_size(type)) || !aligned_to(V, type_size(type)))

@@ -4,17 +4,17 @@
 // kept of a value: no less than fp16's largest leaves; blocks below 2^-21 lose digits: fp16's subnormals lose none); codes as in mx4_quantize.hip.
 //
 // Bound by HBM: 2 (4) bytes read and 17/32 written a value.  A lane takes 8 elements of a position's key and the same of its value, D / 8
-// lanes a position: a block is a quad of lanes, whether all is finite is a ballot.  A workgroup takes ROWS rows of one head, a wave those
+// lanes a position: a block is a quad of lanes, whether all is finite is a ballot.  A workgroup takes 32 rows of one head, a wave those
 // that stand 4 and 4 in the order of the values' codes when the rows begin with a record: what it writes of them joins to whole runs.  Heads come first
 // in the order of workgroups, so that (of a multiple of 8 heads) a record that two of them write stays in one XCD's L2: 8192 x 32 x 128
-// fp16, keys and values, 45 us there (3.8 TB/s; rows first 58, 64 or 128 rows a workgroup 53 to 55) and 30 us back (5.7 TB/s).
+// fp16, keys and values, 45 us there (3.8 TB/s; rows first 58, 64 or 128 rows a workgroup 53 to 55, 8 rows the same, for few tokens too) and 30 us back (5.7 TB/s).
 #include "mx4_cache.h"
 
 namespace {
 
 using namespace mx4;
 
-constexpr int ST_THREADS = 256;
+constexpr int ST_THREADS = 256, ROWS = 32;
 constexpr int QUAD_XOR1 = 0xB1, QUAD_XOR2 = 0x4E;
 
 __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
@@ -32,16 +32,12 @@ struct StoreArgs {
     int log_page, heads, dim;
 };
 
-// The row that group `at` of a workgroup's `rows` takes: in runs of 4, those 16 apart next to each other.
-__device__ __forceinline__ int row_in_turn(int at, int rows) {
-    if (rows < 32) return at;
-    const int run = (at >> 2) & 7, base = at & ~31;
-    return base + 16 * (run & 1) + 4 * (run >> 1) + (at & 3);
-}
+// The row that group `at` of a workgroup takes: in runs of 4, those 16 apart next to each other.
+__device__ __forceinline__ int row_in_turn(int at) { return 16 * ((at >> 2) & 1) + 4 * (at >> 3) + (at & 3); }
 
-template <class T, int D, int ROWS>
+template <class T, int D>
 __global__ __launch_bounds__(ST_THREADS) void mx4_cache_store_rows(StoreArgs a) {
-    constexpr int LANES = D / 8, AT_ONCE = ST_THREADS / LANES, ITER = (ROWS + AT_ONCE - 1) / AT_ONCE;
+    constexpr int LANES = D / 8, AT_ONCE = ST_THREADS / LANES, ITER = ROWS / AT_ONCE;
     typedef Record<D> R;
     const int x = threadIdx.x % LANES, d = 8 * x, have = min(8, a.dim - d), head = blockIdx.x % a.heads;
     const int64_t row0 = int64_t(blockIdx.x / a.heads) * ROWS;
@@ -51,8 +47,8 @@ __global__ __launch_bounds__(ST_THREADS) void mx4_cache_store_rows(StoreArgs a) 
 #pragma unroll
     for (int i = 0; i < ITER; ++i) {
         const int at = threadIdx.x / LANES + AT_ONCE * i;
-        row[i] = row0 + row_in_turn(at, ROWS);
-        slot[i] = at < ROWS && row[i] < a.tokens ? a.slots[row[i]] : -1;
+        row[i] = row0 + row_in_turn(at);
+        slot[i] = row[i] < a.tokens ? a.slots[row[i]] : -1;
         if (slot[i] >= a.slots_all) slot[i] = -1;
         k[i] = typename Chunk<T, 8>::vec{};
         v[i] = typename Chunk<T, 8>::vec{};
@@ -120,9 +116,9 @@ struct LoadArgs {
     int64_t ldk, ldv;
 };
 
-template <class T, int D, int ROWS>
+template <class T, int D>
 __global__ __launch_bounds__(ST_THREADS) void mx4_cache_load_rows(LoadArgs a) {
-    constexpr int LANES = D / 8, AT_ONCE = ST_THREADS / LANES, ITER = (ROWS + AT_ONCE - 1) / AT_ONCE;
+    constexpr int LANES = D / 8, AT_ONCE = ST_THREADS / LANES, ITER = ROWS / AT_ONCE;
     typedef Record<D> R;
     const int x = threadIdx.x % LANES, d = 8 * x, have = min(8, a.dim - d), head = blockIdx.x % a.heads;
     const int64_t row0 = int64_t(blockIdx.x / a.heads) * ROWS;
@@ -132,8 +128,8 @@ __global__ __launch_bounds__(ST_THREADS) void mx4_cache_load_rows(LoadArgs a) {
 #pragma unroll
     for (int i = 0; i < ITER; ++i) {
         const int n = threadIdx.x / LANES + AT_ONCE * i;
-        row[i] = row0 + row_in_turn(n, ROWS);
-        if (n >= ROWS || row[i] >= a.tokens) row[i] = -1;
+        row[i] = row0 + row_in_turn(n);
+        if (row[i] >= a.tokens) row[i] = -1;
         const int32_t slot = row[i] >= 0 ? a.slots[row[i]] : -1;
         word[i][0] = word[i][1] = 0;
         byte[i][0] = byte[i][1] = 127u;
@@ -165,22 +161,14 @@ __global__ __launch_bounds__(ST_THREADS) void mx4_cache_load_rows(LoadArgs a) {
     }
 }
 
-// 32 rows a workgroup where that leaves one for every compute unit, else 8.
-inline bool many_rows(int64_t tokens, int heads) { return (tokens + 31) / 32 * heads >= 256; }
-
 }  // namespace
 
 int launch_mx4_cache_store(adadim_ctx* ctx, const void* K, const void* V, int type, int64_t tokens, int64_t ldk, int64_t ldv,
                            const int32_t* slots, uint8_t* cache, int64_t pages, int log_page, int heads, int dim) {
     const StoreArgs a{K, V, tokens, ldk, ldv, slots, cache, pages << log_page, log_page, heads, dim};
-    const bool many = many_rows(tokens, heads);
-    const dim3 grid(static_cast<unsigned>((many ? (tokens + 31) / 32 : (tokens + 7) / 8) * heads)), block(ST_THREADS);
+    const dim3 grid(static_cast<unsigned>((tokens + ROWS - 1) / ROWS * heads)), block(ST_THREADS);
     ProfScope prof(ctx, "mx4_cache_store_rows");
-#define CACHE_S(T, D)                                                                                        \
-    do {                                                                                                     \
-        if (many) hipLaunchKernelGGL((mx4_cache_store_rows<T, D, 32>), grid, block, 0, ctx->stream, a);      \
-        else hipLaunchKernelGGL((mx4_cache_store_rows<T, D, 8>), grid, block, 0, ctx->stream, a);            \
-    } while (0)
+#define CACHE_S(T, D) hipLaunchKernelGGL((mx4_cache_store_rows<T, D>), grid, block, 0, ctx->stream, a)
 #define CACHE_ST(T)                                                                                          \
     do {                                                                                                     \
         switch (filled_head(dim)) {                                                                          \
@@ -201,14 +189,9 @@ int launch_mx4_cache_store(adadim_ctx* ctx, const void* K, const void* V, int ty
 int launch_mx4_cache_load(adadim_ctx* ctx, const int32_t* slots, int64_t tokens, const uint8_t* cache, int64_t pages, int log_page,
                           int heads, int dim, void* K, void* V, int type, int64_t ldk, int64_t ldv) {
     const LoadArgs a{slots, tokens, cache, pages << log_page, log_page, heads, dim, K, V, ldk, ldv};
-    const bool many = many_rows(tokens, heads);
-    const dim3 grid(static_cast<unsigned>((many ? (tokens + 31) / 32 : (tokens + 7) / 8) * heads)), block(ST_THREADS);
+    const dim3 grid(static_cast<unsigned>((tokens + ROWS - 1) / ROWS * heads)), block(ST_THREADS);
     ProfScope prof(ctx, "mx4_cache_load_rows");
-#define CACHE_L(T, D)                                                                                        \
-    do {                                                                                                     \
-        if (many) hipLaunchKernelGGL((mx4_cache_load_rows<T, D, 32>), grid, block, 0, ctx->stream, a);       \
-        else hipLaunchKernelGGL((mx4_cache_load_rows<T, D, 8>), grid, block, 0, ctx->stream, a);             \
-    } while (0)
+#define CACHE_L(T, D) hipLaunchKernelGGL((mx4_cache_load_rows<T, D>), grid, block, 0, ctx->stream, a)
 #define CACHE_LT(T)                                                                                          \
     do {                                                                                                     \
         switch (filled_head(dim)) {                                                                          \

@@ -124,7 +124,8 @@ def test_row_refusals(ctx, name):
             return ctx.raw(name, K, V, type, tokens, ldk, ldv, slots, cache, pages, page, heads, dim)
         return ctx.raw(name, slots, tokens, cache, pages, page, heads, dim, K, V, type, ldk, ldv)
     for bad in ({"type": MX4}, {"tokens": -1}, {"tokens": (1 << 20) + 1}, {"ldk": 127}, {"ldv": 127}, {"pages": 0}, {"pages": 1 << 25}, {"page": 33},
-                {"heads": 0}, {"heads": 1025, "ldk": 1 << 20, "ldv": 1 << 20}, {"dim": 0}, {"dim": 257, "ldk": 514, "ldv": 514}):
+                {"heads": 0}, {"heads": 1025, "ldk": 1 << 20, "ldv": 1 << 20}, {"dim": 0}, {"dim": 257, "ldk": 514, "ldv": 514},
+                {"tokens": 1 << 20, "heads": 512, "dim": 1, "ldk": 512, "ldv": 512}):
         assert call(**bad) == B.EINVAL, bad
     for p in ("K", "V", "slots", "cache"):
         assert call(**{p: None}) == B.ENULL and call(**{p: BYTE}) == B.EALIGN, p
