@@ -139,9 +139,9 @@ int adadim_mx4_attention(adadim_ctx* ctx, const void* Q, int q_type, int64_t tok
                            MOST_SEQUENCES, sequences, (long long)width, page);
     const int group = q_heads / heads;
     if (tokens < 0 || tokens > MOST_TOKENS || ldq < int64_t(q_heads) * dim || ldy < int64_t(q_heads) * dim ||
-        !launchable((tokens * group / 16 + sequences) * heads, 256))
+        !launchable((tokens * group / 16 + sequences) * heads, 512))
         return adadim_fail(ctx, ADADIM_EINVAL,
-                           "%s: need tokens in [0,2^20], ldq, ldy >= q_heads * dim, fewer than 2^24 tiles of 16 rows (tokens=%lld ldq=%lld ldy=%lld)", me,
+                           "%s: need tokens in [0,2^20], ldq, ldy >= q_heads * dim, fewer than 2^23 tiles of 16 rows (tokens=%lld ldq=%lld ldy=%lld)", me,
                            (long long)tokens, (long long)ldq, (long long)ldy);
     if (!(scale > 0.0f && scale <= 2e38f) || (causal != 0 && causal != 1) || window < 0)
         return adadim_fail(ctx, ADADIM_EINVAL, "%s: need a scale in (0, 2e38], causal 0 or 1, window >= 0 (scale=%g causal=%d window=%lld)", me, scale,

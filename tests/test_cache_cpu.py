@@ -141,7 +141,8 @@ def test_attention_refusals(ctx):
     for bad in ({"type": F32}, {"type": MX4}, {"y_type": MX4}, {"tokens": -1}, {"tokens": (1 << 20) + 1}, {"ldq": 511}, {"ldy": 511}, {"q_heads": 7},
                 {"q_heads": 0}, {"pages": 0}, {"pages": 1 << 25}, {"page": 16}, {"heads": 0}, {"dim": 0}, {"dim": 257}, {"width": 0}, {"width": 1 << 25},
                 {"n": 0}, {"n": 4097}, {"scale": 0.0}, {"scale": -1.0}, {"scale": float("nan")}, {"scale": float("inf")}, {"causal": 2}, {"window": -1},
-                {"tokens": 1 << 20, "q_heads": 1024, "heads": 1024, "ldq": 1 << 16, "ldy": 1 << 16}):
+                {"tokens": 1 << 20, "q_heads": 1024, "heads": 1024, "ldq": 1 << 16, "ldy": 1 << 16},
+                {"tokens": 1 << 20, "q_heads": 192, "heads": 192, "ldq": 12288, "ldy": 12288}):
         assert call(**bad) == B.EINVAL, bad
     for p in ("Q", "cache", "table", "offsets", "lengths", "Y"):
         assert call(**{p: None}) == B.ENULL and call(**{p: BYTE}) == B.EALIGN, p
