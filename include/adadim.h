@@ -501,7 +501,7 @@ int adadim_mx4_cache_load(adadim_ctx* ctx, const int32_t* slots, int64_t tokens,
  *   offsets  int32 [sequences + 1]: not decreasing, inside [0, tokens] (values outside are taken as the nearer end).  Rows of Y in no sequence
  *            are not written.
  *   lengths  int32 [sequences]: inside [0, width * page] (values outside are taken as the nearer end)
- *   scale    positive, at most 2e38;  window  0: none;  tokens 0 to 2^20, tokens * q_heads less than 2^26, sequences 1..4096
+ *   scale    positive, at most 2e38 (products with scores may pass fp32's range, the scores Q . k themselves may not);  window  0: none;  tokens 0 to 2^20, tokens * q_heads less than 2^26, sequences 1..4096
  *   max_new, max_length  the most new tokens and positions that a sequence has, as far as the host knows (0: unknown; the mean of the new tokens and
  *            all that the table has room for are taken): what the launch is laid out for.  Results do not depend on them but for the order of sums.
  * A row that sees nothing is zeros.  A row that sees a position stored with an infinity or a NaN is NaN; positions that it does not see do

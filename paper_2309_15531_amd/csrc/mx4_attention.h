@@ -2,11 +2,11 @@
 //
 // A tile is a number of rows (a row: one query head of one new token) of a sequence that share a key-value head.  A wave goes over records of 32
 // positions:  S^T = K Q^T, keys converted in registers to the queries' type (exact: 2 bits and a scale that fp16 and bf16 have), then
-// p = 2^(scale log2(e) s - m + 8) in fp32, rounded to fp16 (half a step of 11 bits; with the 2^8 the smallest number that fp16 still holds is
-// 2^-33 of the row's largest), and O^T += V^T P^T with the values in fp16 (exact).  Positions lie along a lane's registers and rows along the
-// lanes in S^T and in O^T: neither is turned round, and a row's maximum and sum are numbers of its lanes.  The maximum m is only raised (and
-// O^T and the sum scaled) where a score passes it by more than 7: p stays below 2^15.  The sum is of p before rounding.  Scores, sums and
-// O^T are fp32.
+// p = 2^(c (s - m) + 8) with c = scale log2(e) in fp32, rounded to fp16 (half a step of 11 bits; with the 2^8 the smallest number that fp16 still
+// holds is 2^-33 of the row's largest), and O^T += V^T P^T with the values in fp16 (exact).  Positions lie along a lane's registers and rows
+// along the lanes in S^T and in O^T: neither is turned round, and a row's maximum and sum are numbers of its lanes.  The maximum m, a score, is only
+// raised (and O^T and the sum scaled) where a score passes it by more than 7 / c: p stays below 2^15.2.  The sum is of p before rounding.
+// Scores, sums and O^T are fp32.
 //
 // Few rows (this file): the waves of a workgroup have the same rows and take records in turn; their sums meet in LDS.  Many rows:
 // mx4_attention_tiles.h.  Either way a tile's records may be shared between workgroups (gridDim.y), whose partial sums are joined in their order:
@@ -25,8 +25,9 @@ namespace mx4 {
 
 constexpr int AT_WAVES = 8;                       // of a workgroup of few rows
 constexpr int AT_TICKETS = 8192;                  // tiles that may be shared
-constexpr float LOWEST = -3e38f;                  // a maximum before the first score
 constexpr float RAISE = 7.0f, HEAD = 8.0f;
+constexpr float LARGEST = 3.402823466e38f;
+constexpr float FAR = 1048576.0f;                 // |c m| from which on a wave weighs by differences of scores
 
 struct AttentionArgs {
     Attention a;
@@ -34,6 +35,7 @@ struct AttentionArgs {
     int least;                                    // records that a share has at least
     int most;                                     // shares of a tile at most
     int round;                                    // workgroups that run at a time, where shares are to be alike over all sequences; or 0
+    float c, step;                                // scale log2(e); RAISE / c, or 0 where fp32 does not hold that
     unsigned* tickets;
     float* parts;
 };
@@ -87,7 +89,7 @@ struct ValueBytes {
         for (int i = 0; i < 4; ++i) v[i] = scale_operand((scale_word >> (8 * i)) & 255u);
         if (have < RECORD) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = 16 * t + 4 * g + i < have ? v[i] : 0.0f;
+            for (int i = 0; i < 4; ++i) v[i] = 4 * g < have - 16 * t - i ? v[i] : 0.0f;            // (one register for all four)
         }
     }
     // elements 2 u and 2 u + 1 of position i
@@ -109,13 +111,48 @@ __device__ __forceinline__ float quarters(float v, F f) {
     return f(v, __shfl_xor(v, 32));
 }
 
+// A difference from a row's maximum: finite also where there is none yet (m = -infinity), so that what is hidden stays -infinity.
+__device__ __forceinline__ float from_top(float s, float m) { return s - fmaxf(m, -LARGEST); }
+
+// A row's maximum m and how a wave takes weights from scores: by fma(s, c, base), in one of two ways that it chooses anew with each raise.
+//   near  |c m| < 2^20 in all its rows: base = 8 - c m, of whose roundings (at most 3/32 together) all of a row's weights have the same share
+//   far   the rounding of c m would be whole units of the exponent in the end: scores are taken as differences from m first (exact at the top), base = 8
+struct Maximum {
+    float limit, base;                            // a score beyond limit raises m: m + step when near, m itself when far; -infinity: no score yet
+    bool far;                                     // the same in all lanes
+    __device__ __forceinline__ void none() {
+        limit = -INFINITY;
+        base = HEAD;
+        far = false;
+    }
+    // (near it may be off by a rounding of limit, or by up to step where that would be beyond fp32: weights go by base, and are related to m by it)
+    __device__ __forceinline__ float m(float step) const { return far ? limit : limit - step; }
+    __device__ __forceinline__ float exponent(float s, float c) const { return __builtin_fmaf(far ? from_top(s, limit) : s, c, base); }
+    // top: the largest of a lane's new scores
+    __device__ __forceinline__ bool passed(float top) const { return __any(top > limit); }
+    // top: the row's; returns what sums so far are to be multiplied with
+    __device__ __forceinline__ float raise(float top, float c, float step) {
+        const float up = top > limit ? top : m(step), was = exponent(up, c), at = up * c;
+        const bool had = limit > -INFINITY, has = up > -INFINITY;
+        far = __any(has && !(fabsf(at) < FAR));
+        base = HEAD - (far || !has ? 0.0f : at);
+        limit = far ? up : fminf(up + step, LARGEST);
+        const float now = __builtin_fmaf(far ? 0.0f : up, c, base);
+        return had ? __builtin_amdgcn_exp2f(now - was) : 0.0f;
+    }
+    // what brings a row's sums to a weight of 2^8 for m
+    __device__ __forceinline__ float settled(float c, float step) const {
+        return far || !(limit > -INFINITY) ? 1.0f : __builtin_amdgcn_exp2f(HEAD - exponent(m(step), c));
+    }
+};
+
 template <class T, int D>
 struct Rows {
     static constexpr int W = D / 32, TILES = D / 16;
     typedef typename Dots<T>::vec vec;
     float4v o[TILES];
-    float m, l;                                   // m: largest score so far, times c, of all quarters; l: sum of this lane's p
-    float c;                                      // scale log2(e)
+    Maximum top;
+    float l;                                      // sum of this lane's p
 
     // q: the rows of Q in LDS, 64 lanes' 16 bytes for each of the W instructions
     static __device__ __forceinline__ void scores(const KeyBytes<D> (&b)[2], const vec* q, int lane, float4v (&s)[2]) {
@@ -137,22 +174,28 @@ struct Rows {
                 s[t][i] = at >= lo && at < hi ? s[t][i] : -INFINITY;
             }
     }
-    __device__ __forceinline__ void weigh(const float4v (&s)[2], half8v& p) {
-        const float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))) * c;
-        if (__any(top > m + RAISE)) {
-            const float up = fmaxf(m, quarters(top, [](float x, float y) { return fmaxf(x, y); }));
-            const float by = __builtin_amdgcn_exp2f(m - up);
-            m = up;
-            l *= by;
+    __device__ __forceinline__ void weigh(float4v (&s)[2], float c, float step, half8v& p) {
+        const float most = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+        const bool passed = top.passed(most);
+        if (passed || top.far) {
+            if (passed) {
+                const float by = top.raise(quarters(most, [](float x, float y) { return fmaxf(x, y); }), c, step);
+                l *= by;
 #pragma unroll
-            for (int j = 0; j < TILES; ++j) o[j] *= by;
+                for (int j = 0; j < TILES; ++j) o[j] *= by;
+            }
+            if (top.far) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[t][i] = from_top(s[t][i], top.limit);
+            }
         }
-        const float base = HEAD - m;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], c, base));
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], c, top.base));
                 l += e;
                 p[4 * t + i] = static_cast<_Float16>(e);
             }
@@ -337,17 +380,17 @@ __device__ __forceinline__ void join_rows(const AttentionArgs& args, const Work&
     for (int row0 = row_begin; row0 < row_end; row0 += at_once) {
         const int row = min(row0 + static_cast<int>(threadIdx.x >> 4), row_end - 1);
         const float* const p = all + row * PART<D>;
-        float by[MOST_SHARES / 16], m = LOWEST, l = 0.0f;
+        float by[MOST_SHARES / 16], m = -INFINITY, l = 0.0f;
         float2p ml[MOST_SHARES / 16];
 #pragma unroll
-        for (int i = 0; i < MOST_SHARES / 16; ++i) ml[i] = 16 * i + x < w.shares ? get(p + int64_t(16 * i + x) * (R * PART<D>) + D) : float2p{LOWEST, 0.0f};
+        for (int i = 0; i < MOST_SHARES / 16; ++i) ml[i] = 16 * i + x < w.shares ? get(p + int64_t(16 * i + x) * (R * PART<D>) + D) : float2p{-INFINITY, 0.0f};
 #pragma unroll
         for (int i = 0; i < MOST_SHARES / 16; ++i) m = fmaxf(m, ml[i].x);
 #pragma unroll
         for (int d = 1; d < 16; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
 #pragma unroll
         for (int i = 0; i < MOST_SHARES / 16; ++i) {
-            by[i] = __builtin_amdgcn_exp2f(ml[i].x - m);
+            by[i] = __builtin_amdgcn_exp2f(from_top(ml[i].x, m) * args.c);
             l += ml[i].y * by[i];
         }
 #pragma unroll
@@ -437,8 +480,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, FEW_WAVES<D>) void mx4_attend_few(At
     // ---- the rows: every wave has the same
     __shared__ vec s_q[W * 64];
     Rows<T, D> rows;
-    rows.c = a.scale * 1.44269504088896340736f;
-    rows.m = LOWEST;
+    rows.top.none();
     rows.l = 0.0f;
 #pragma unroll
     for (int j = 0; j < TILES; ++j) rows.o[j] = float4v{0, 0, 0, 0};
@@ -465,7 +507,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, FEW_WAVES<D>) void mx4_attend_few(At
         if (next < e) load_keys(record(page1, next));
         if (use) {
             if (b < all_from || b >= all_to) rows.hide(s, g, lo, hi, RECORD * b);
-            rows.weigh(s, p);
+            rows.weigh(s, args.c, args.step, p);
             __builtin_amdgcn_sched_barrier(0);
             rows.values(vb, g, w.length - RECORD * b, p);
         }
@@ -474,7 +516,8 @@ __global__ __launch_bounds__(64 * AT_WAVES, FEW_WAVES<D>) void mx4_attend_few(At
         page = page1;
         page1 = page2;
     }
-    rows.l = quarters(rows.l, [](float x, float y) { return x + y; });
+    const float settled = rows.top.settled(args.c, args.step), m_wave = rows.top.m(args.step);
+    rows.l = quarters(rows.l, [](float x, float y) { return x + y; }) * settled;
 
     // ---- the waves' sums, in PASSES of 64 elements (35 KB): of the TILES elements of a unit the four from 4 pass on (all with D = 64)
     float* const mine = args.parts + (int64_t(blockIdx.x) * args.most + blockIdx.y) * (R * PART<D>);
@@ -482,7 +525,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, FEW_WAVES<D>) void mx4_attend_few(At
     __shared__ __attribute__((aligned(16))) float s_o[AT_WAVES][16][64 + 4];
     __shared__ float s_m[AT_WAVES][R], s_l[AT_WAVES][R];
     if (lane < 16) {
-        s_m[wave][lane] = rows.m;
+        s_m[wave][lane] = m_wave;
         s_l[wave][lane] = rows.l;
     }
     __syncthreads();
@@ -493,9 +536,9 @@ __global__ __launch_bounds__(64 * AT_WAVES, FEW_WAVES<D>) void mx4_attend_few(At
         top = fmaxf(top, s_m[i][lane & 15]);
         m = fmaxf(m, s_m[i][row]);
     }
-    const float by = __builtin_amdgcn_exp2f(rows.m - top);
+    const float by = __builtin_amdgcn_exp2f(from_top(m_wave, top) * args.c) * settled;
 #pragma unroll
-    for (int i = 0; i < AT_WAVES; ++i) l += s_l[i][row] * __builtin_amdgcn_exp2f(s_m[i][row] - m);
+    for (int i = 0; i < AT_WAVES; ++i) l += s_l[i][row] * __builtin_amdgcn_exp2f(from_top(s_m[i][row], m) * args.c);
     const float by1 = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
     for (int pass = 0; pass < PASSES; ++pass) {

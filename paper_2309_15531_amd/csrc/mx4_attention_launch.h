@@ -31,7 +31,9 @@ template <int R, int D>
 int laid_out(adadim_ctx* ctx, const Attention& a, bool few, AttentionArgs& args, dim3& grid) {
     const int64_t tiles = a.tokens * a.group / R + a.sequences;
     const Shares s = shares_of(a, tiles, R, few);
-    args = AttentionArgs{a, static_cast<int>(tiles), s.least, s.most, few && s.most > 1 && alike(a) ? (D <= 128 ? 512 : 256) : 0, nullptr, nullptr};
+    const float c = a.scale * 1.44269504088896340736f, step = RAISE / c;
+    args = AttentionArgs{a, static_cast<int>(tiles), s.least, s.most, few && s.most > 1 && alike(a) ? (D <= 128 ? 512 : 256) : 0, c,
+                         step < INFINITY ? step : 0.0f, nullptr, nullptr};
     grid = dim3(static_cast<unsigned>(tiles * a.heads), s.most);
     if (s.most == 1) return ADADIM_OK;
     void* shared = nullptr;

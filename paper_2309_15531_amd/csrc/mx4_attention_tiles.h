@@ -75,7 +75,8 @@ struct Tiles32 {
     typedef typename Dots<T>::vec vec;
     vec q[STEPS];
     float16v o[OT];
-    float m, l, c;
+    Maximum top;
+    float l;
 
     __device__ __forceinline__ float16v scores(const uint8_t* r, int lane) const {
         float16v s = {};
@@ -83,24 +84,28 @@ struct Tiles32 {
         for (int k = 0; k < STEPS; ++k) s = Dots32<T>::mfma(*reinterpret_cast<const vec*>(r + (k * 64 + lane) * 16), q[k], s);
         return s;
     }
-    __device__ __forceinline__ void raise(const float16v& s) {
-        float top = fmaxf(s[0], s[1]);
+    __device__ __forceinline__ void raise(float16v& s, float c, float step) {
+        float most = fmaxf(s[0], s[1]);
 #pragma unroll
-        for (int i = 2; i < 16; ++i) top = fmaxf(top, s[i]);
-        top *= c;
-        if (__any(top > m + RAISE)) {
-            const float up = fmaxf(m, fmaxf(top, __shfl_xor(top, 32))), by = __builtin_amdgcn_exp2f(m - up);
-            m = up;
-            l *= by;
+        for (int i = 2; i < 16; ++i) most = fmaxf(most, s[i]);
+        const bool passed = top.passed(most);
+        if (passed || top.far) {
+            if (passed) {
+                const float by = top.raise(fmaxf(most, __shfl_xor(most, 32)), c, step);
+                l *= by;
 #pragma unroll
-            for (int j = 0; j < OT; ++j) o[j] *= by;
+                for (int j = 0; j < OT; ++j) o[j] *= by;
+            }
+            if (top.far) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = from_top(s[i], top.limit);
+            }
         }
     }
-    __device__ __forceinline__ void weigh(const float16v& s, half8v (&p)[2]) {
-        const float base = HEAD - m;
+    __device__ __forceinline__ void weigh(const float16v& s, float c, half8v (&p)[2]) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, base));
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, top.base));
             l += e;
             p[i >> 3][i & 7] = static_cast<_Float16>(e);
         }
@@ -133,8 +138,7 @@ __global__ __launch_bounds__(64 * TL_WAVES, 2) void mx4_attend_tiles(AttentionAr
     const int all_from = (w.sees_from(a, t_last) + 31) >> 5, all_to = w.sees_to(a, t_first) >> 5;         // (these hide nothing from any row)
     const int lo = w.sees_from(a, token), hi = w.sees_to(a, token);
     Tiles32<T, D> t;
-    t.c = a.scale * 1.44269504088896340736f;
-    t.m = LOWEST;
+    t.top.none();
     t.l = 0.0f;
 #pragma unroll
     for (int j = 0; j < D / 32; ++j) t.o[j] = float16v{};
@@ -207,9 +211,9 @@ __global__ __launch_bounds__(64 * TL_WAVES, 2) void mx4_attend_tiles(AttentionAr
             const uint8_t* const rec = at + (r - first) * BYTES;
             float16v s = t.scores(rec, lane);
             hide(s, r);
-            t.raise(s);
+            t.raise(s, args.c, args.step);
             half8v p[2];
-            t.weigh(s, p);
+            t.weigh(s, args.c, p);
             t.values(rec, lane, p);
         }
     };
@@ -236,9 +240,11 @@ __global__ __launch_bounds__(64 * TL_WAVES, 2) void mx4_attend_tiles(AttentionAr
 
     // ---- out
     float* const mine = args.parts + (int64_t(blockIdx.x) * args.most + blockIdx.y) * (R * PART<D>);
-    const float l = t.l + __shfl_xor(t.l, 32), by = l == 0.0f ? 0.0f : 1.0f / l;
+    const float l = t.l + __shfl_xor(t.l, 32), by = l == 0.0f ? 0.0f : 1.0f / l, settled = t.top.settled(args.c, args.step);
     if (w_row + (lane & 31) <= w_last) {
-        const int64_t y = w.row_of_y(a, row);
+        int out = row;                            // (worked out anew: no registers for it in the loop)
+        asm volatile("" : "+v"(out));
+        const int64_t y = w.row_of_y(a, out);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int d = N * (8 * (i >> 2) + 4 * h + (i & 3));
@@ -247,14 +253,14 @@ __global__ __launch_bounds__(64 * TL_WAVES, 2) void mx4_attend_tiles(AttentionAr
             for (int j = 0; j < N; ++j) v[j] = t.o[j % (D / 32)][i + 8 * (j / (D / 32))];
             if (w.shares > 1) {
 #pragma unroll
-                for (int j = 0; j < N; j += 2) *reinterpret_cast<float2v*>(mine + row * PART<D> + d + j) = float2v{v[j], v[j + 1]};
+                for (int j = 0; j < N; j += 2) *reinterpret_cast<float2v*>(mine + row * PART<D> + d + j) = float2v{v[j] * settled, v[j + 1] * settled};
             } else {
 #pragma unroll
                 for (int j = 0; j < N; ++j) v[j] = l == 0.0f ? 0.0f : v[j] * by;
                 store_row(a, y, d, v);
             }
         }
-        if (w.shares > 1 && h == 0) *reinterpret_cast<float2v*>(mine + row * PART<D> + D) = float2v{t.m, l};
+        if (w.shares > 1 && h == 0) *reinterpret_cast<float2v*>(mine + row * PART<D> + D) = float2v{t.top.m(args.step), l * settled};
     }
 }
 
