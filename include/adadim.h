@@ -442,7 +442,7 @@ int adadim_expert_combine(adadim_ctx* ctx, const void* Z, int z_type, int64_t n_
  *            the values' scales [4][D/32][8]         (g, block, i)
  *          so that a position's bytes are its own: appending one reads nothing and touches no other.
  *   Scales lie in 2^-23 .. 2^13.  A position with an infinity or a NaN in a head's key or value has key scales 255 and zeros otherwise there.
- * adadim_mx4_cache_bytes gives the size of the pool (0 for arguments that are none).
+ * adadim_mx4_cache_bytes gives the size of the pool (0 for arguments that are none, as 2^31 positions).
  */
 int64_t adadim_mx4_cache_bytes(int64_t pages, int page, int heads, int dim);
 

@@ -32,7 +32,7 @@ static bool pages_ok(int64_t pages, int page) { return pages >= 1 && pages <= IN
 extern "C" {
 
 int64_t adadim_mx4_cache_bytes(int64_t pages, int page, int heads, int dim) {
-    if (log_of_page(page) == 0 || pages <= 0 || pages > INT32_MAX || heads <= 0 || heads > MOST_HEADS || dim <= 0 || dim > 256) return 0;
+    if (log_of_page(page) == 0 || !pages_ok(pages, page) || heads <= 0 || heads > MOST_HEADS || dim <= 0 || dim > 256) return 0;
     return pages * heads * (page / mx4::RECORD) * (34 * mx4::filled_head(dim));
 }
 
