@@ -66,11 +66,13 @@ int launch_tiles(adadim_ctx* ctx, const Attention& a) {
     dim3 grid;
     const int rc = laid_out<TL_WAVES * 32, D>(ctx, a, false, args, grid);
     if (rc != ADADIM_OK) return rc;
-    ProfScope prof(ctx, "mx4_attend_tiles");
-    hipLaunchKernelGGL((mx4_attend_tiles<T, D>), grid, dim3(64 * TL_WAVES), Stage<D>::LDS, ctx->stream, args);
-    ADADIM_LAUNCH_CHECK(ctx, "mx4_attend_tiles");
+    {
+        ProfScope prof(ctx, "mx4_attend_tiles");
+        hipLaunchKernelGGL((mx4_attend_tiles<T, D>), grid, dim3(64 * TL_WAVES), Stage<D>::LDS, ctx->stream, args);
+        ADADIM_LAUNCH_CHECK(ctx, "mx4_attend_tiles");
+    }
     if (args.most == 1) return ADADIM_OK;
-    ProfScope prof_join(ctx, "mx4_attend_join");
+    ProfScope prof(ctx, "mx4_attend_join");
     hipLaunchKernelGGL((mx4_attend_join<D>), dim3(grid.x, TL_WAVES), dim3(512), 0, ctx->stream, args);
     ADADIM_LAUNCH_CHECK(ctx, "mx4_attend_join");
     return ADADIM_OK;
