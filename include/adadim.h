@@ -507,6 +507,8 @@ int adadim_mx4_cache_load(adadim_ctx* ctx, const int32_t* slots, int64_t tokens,
  * A row that sees nothing is zeros.  A row that sees a position stored with an infinity or a NaN is NaN; positions that it does not see do
  * not touch it, whatever they hold.  Scores and sums are fp32 and keys and values enter exactly; the weights 2^(score - largest) are rounded
  * to fp16 (2^-33 of the row's largest is kept) for the product with the values.  Sums in a fixed order: same bits every run.
+ * Where the positions of a sequence are shared among workgroups the context's scratch holds partial sums: at most 35 MB (68 where dim is beyond 128),
+ * with more than 256 rows (max_new * q_heads / heads) a sequence 274 MB (542).
  */
 int adadim_mx4_attention(adadim_ctx* ctx, const void* Q, int q_type, int64_t tokens, int64_t ldq, int q_heads, const uint8_t* cache,
                          int64_t pages, int page, int heads, int dim, const int32_t* table, int64_t width, int sequences,

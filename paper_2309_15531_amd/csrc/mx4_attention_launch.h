@@ -21,7 +21,8 @@ inline Shares shares_of(const Attention& a, int64_t tiles, int rows, bool few) {
     const int64_t real = std::max<int64_t>(1, std::min(tiles, a.sequences * ((a.max_new * a.group + rows - 1) / rows)) * a.heads);
     const int64_t wanted = (few ? alike(a) ? 2048 : 1024 : 256) / real;
     const int least = !few ? 16 : real * ((records + 31) / 32) > 512 ? 64 : 32;
-    // (and no more than 35 MB of sums, 270 of many rows, where the host knows less of the sequences than there is)
+    // (and no more shares in all than that, where the host knows less of the sequences than there is: sums of 17, 34 or 68 MB with heads filled up
+    // to 64, 128 or 256, of many rows 138, 273 or 541)
     const int64_t n = std::min({wanted, records / least, (few ? AT_TICKETS / 2 : 2048) / (tiles * a.heads)});
     return {static_cast<int>(std::min<int64_t>(std::max<int64_t>(n, 1), MOST_SHARES)), least};
 }

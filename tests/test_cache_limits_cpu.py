@@ -59,3 +59,27 @@ def test_a_profile_charges_each_launch_once(run):
         for i, k in enumerate(kernels):
             assert order[3 * i] == order[3 * i + 2] == "record" and k in order[3 * i + 1], order
     """)
+
+
+@pytest.mark.parametrize("dim,few,many", [(64, 18, 139), (128, 35, 274), (256, 68, 542)])
+def test_partial_sums_stay_within_the_scratch_that_is_stated(run, dim, few, many):
+    """Batches of all sizes, with hints that fit them and others; the bounds in units of 10^6 bytes, with the counters."""
+    run(f"""
+    import random
+    r = random.Random({dim})
+    largest = {{True: 0, False: 0}}
+    contexts = {{True: context(), False: context()}}
+    for i in range(6000):
+        n, heads, group = r.choice((1, 1, 2, 7, 64, 300, 4096)), r.choice((1, 1, 2, 8, 32)), r.choice((1, 4, 16))
+        tokens = min(n * r.choice((1, 4, 33, 300, 4000, 30000)), 1 << 20, (1 << 25) // (heads * group))
+        hint, length, window = r.choice((0, 1, 17, 257, 3000)), r.choice((0, 100, 5000, 100000, 1 << 20)), r.choice((0, 0, 3000))
+        new = -(-tokens // n) if hint == 0 else min(hint, tokens)
+        few = new * group <= 256
+        fake.fake_reset()
+        assert lib.adadim_mx4_attention(contexts[few], A, 0, c_int64(tokens), c_int64(heads * group * {dim}), heads * group, A, c_int64(1 << 20), 64, heads, {dim},
+                                        A, c_int64(1 << 14), n, A, A, A, 0, c_int64(heads * group * {dim}), c_float(1.0), 1, c_int64(window), c_int64(hint),
+                                        c_int64(length)) == OK, lib.adadim_last_error(contexts[few])
+        assert any(("mx4_attend_few" if few else "mx4_attend_tiles") in c for c in calls()), calls()
+        largest[few] = max([largest[few]] + [int(c.split()[1]) for c in calls() if c.startswith("hipMalloc")])
+    assert {few} * 0.9e6 < largest[True] <= {few} * 1e6 and {many} * 0.9e6 < largest[False] <= {many} * 1e6, largest
+    """)
