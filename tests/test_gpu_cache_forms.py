@@ -116,3 +116,35 @@ def test_many_sequences_of_unlike_lengths(ctx, n, long, many):
     names, _ = launched(ctx, lambda: run_attention(ctx, 750 + n, added.tolist(), lengths.tolist(), 1, 2, 64, 32, "f16", "f32", window=0 if n % 2 else 500,
                                                    hints=(int(added.max()), long), spare=2))
     assert (TILES if many else FEW) in names and (FEW if many else TILES) not in names
+
+
+@pytest.mark.parametrize("hints", [False, True])
+def test_a_mixed_batch_by_one_call_and_by_two(ctx, hints):
+    """A chunk beside decoding sequences: each call writes the rows of its own sequences, in one form or in two."""
+    r = rng(76)
+    dim, page, heads, group = 128, 32, 2, 4
+    added, lengths = [150, 1, 1, 2, 0, 1], [400, 300, 35, 90, 64, 700]
+    width = max(lengths) // page + 1
+    pages = sum(-(-n // page) for n in lengths)
+    table = batch(r, lengths, page, pages, width)
+    k, v = (r.standard_normal((pages * page, heads, dim)) for _ in range(2))
+    cache = torch.empty(B.mx4_cache_shape(pages, page, heads, dim), dtype=torch.uint8, device="cuda")
+    ctx.adadim_mx4_cache_store(*(torch.from_numpy(t.reshape(len(t), -1)).float().cuda() for t in (k, v)), ints(np.arange(pages * page)), cache)
+    offsets = np.concatenate([[0], np.cumsum(added)])
+    q = rounded(r.standard_normal((sum(added), heads * group, dim)) * 0.7, "f16")
+    qd, t, o, n = torch.from_numpy(q.reshape(len(q), -1)).half().cuda(), ints(table), ints(offsets), ints(lengths)
+    want, weight, slack = co.attention(q, cache.cpu().numpy(), table, offsets, lengths, dim, float(np.float32(dim ** -0.5)))
+
+    def call(y, a, b):
+        more = dict(max_new=max(added[a:b]), max_length=max(lengths[a:b])) if hints else {}
+        ctx.adadim_mx4_attention(qd, cache, t[a:b], o[a:b + 1], n[a:b], y, dim, **more)
+    whole, parts = (torch.full(qd.shape, 5.0, dtype=torch.float32, device="cuda") for _ in range(2))
+    call(whole, 0, 6)
+    names, _ = launched(ctx, lambda: call(parts, 0, 1))
+    assert TILES in names and (parts[150:] == 5.0).all() and (parts[:150] != 5.0).any(1).all()
+    first = parts[:150].clone()
+    names, _ = launched(ctx, lambda: call(parts, 1, 6))
+    assert names == {FEW} or not hints
+    assert torch.equal(parts[:150], first)
+    for y in (whole, parts):
+        check(host(y).astype(np.float64).reshape(want.shape), want, weight, slack, dim, max(lengths), 12.0, "f32")
