@@ -435,7 +435,8 @@ int adadim_expert_combine(adadim_ctx* ctx, const void* Z, int z_type, int64_t n_
  * A paged cache of keys and values in mx4 for serving: a pool of pages of `page` positions (a power of two, 32 to 65536), each with the
  * keys and values of `heads` key-value heads of `dim` elements (1..256, filled up to 64, 128 or 256: D).  A position is named by its
  * slot, page number * page + place in the page.  Fewer than 2^31 positions in a pool, and in a sequence's row of the table.
- *   cache  u8 [pages, heads, page/32, 34 D], 16-byte aligned: 4.25 bits a value.  In a record of 32 positions lie
+ *   cache  u8 [pages, heads, page/32, 34 D], 16-byte aligned: 4.25 D / dim bits a value (4.25 for heads of 64, 128 and 256; 5.7 for 96, 6.8 for 80,
+ *          8.4 for 65 and 129).  In a record of 32 positions lie
  *            the keys' codes    [32][D/2]            element 2i of a position in the low half of byte i
  *            the values' codes  [4][16][8][D/32]     (g, m, i): elements m D/16 .. of position 4g + i (i < 4) or 12 + 4g + i
  *            the keys' scales   [32][D/32]           a byte for each block of 32 elements
@@ -503,7 +504,8 @@ int adadim_mx4_cache_load(adadim_ctx* ctx, const int32_t* slots, int64_t tokens,
  *   lengths  int32 [sequences]: inside [0, width * page] (values outside are taken as the nearer end)
  *   scale    positive, at most 2e38 (products with scores may pass fp32's range, the scores Q . k themselves may not);  window  0: none;  tokens 0 to 2^20, tokens * q_heads less than 2^26, sequences 1..4096
  *   max_new, max_length  the most new tokens and positions that a sequence has, as far as the host knows (0: unknown; the mean of the new tokens and
- *            all that the table has room for are taken): what the launch is laid out for.  Results do not depend on them but for the order of sums.
+ *            all that the table has room for are taken): what the launch is laid out for.  Results do not depend on them but for the order of sums.  One form serves a whole call: a prompt's chunk beside
+ *            decoding sequences is faster by a call of its own (the same Q and Y; table, offsets and lengths from that sequence on).
  * A row that sees nothing is zeros.  A row that sees a position stored with an infinity or a NaN is NaN; positions that it does not see do
  * not touch it, whatever they hold.  Scores and sums are fp32 and keys and values enter exactly; the weights 2^(score - largest) are rounded
  * to fp16 (2^-33 of the row's largest is kept) for the product with the values.  Sums in a fixed order: same bits every run.

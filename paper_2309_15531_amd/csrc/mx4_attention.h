@@ -16,7 +16,7 @@
 // heads over 8 (354 MB) 86 us, 4.1 TB/s.  A record takes a wave 0.85 us by itself (conversions, dependent products, exponentials), so a SIMD
 // wants four of them: the bytes of one record at a time in registers and the queries in LDS leave 128 (149 registers and three waves with the
 // next record's bytes beside them, in workgroups of four waves: 94 us, where this took 92).  16 rows to a tile, not 32: those take 250 registers and
-// two waves (17 sequences, 6 tokens of 40 heads over 8: 36 us, 29 so).
+// two waves (17 sequences, 6 tokens of 40 heads over 8: 36 us, 30 so).
 #pragma once
 
 #include "mx4_cache.h"
@@ -342,7 +342,7 @@ __device__ __forceinline__ Work work_of(const AttentionArgs& args, int y) {
     int least = args.least;
     if constexpr (!LAST_FIRST) {
         // Shares as long in one sequence as in the other, so long that all of them (those that are not divisible among them) are whole rounds
-        // of workgroups; one sequence to a lane.  2 sequences to 100003: 131 us, 147 with as many shares for each.
+        // of workgroups; one sequence to a lane.  2 sequences to 100003: 126 us, 147 with as many shares for each.
         if (args.round > 0) {
             const int lane = threadIdx.x & 63, s = min(lane, a.sequences - 1);
             const int o0 = min(max(a.offsets[s], 0), static_cast<int>(a.tokens)), o1 = min(max(a.offsets[s + 1], o0), static_cast<int>(a.tokens));

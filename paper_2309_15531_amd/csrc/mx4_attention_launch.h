@@ -13,6 +13,8 @@ namespace mx4 {
 // new ones, 32 heads: 125 us, 138 with two); a record takes 0.5 us there.
 struct Shares { int most, least; };
 // Whether the shares of several sequences are made alike on the device (work_of): longer ones then have more of them than two rounds would give each.
+// Up to 64 sequences, which are one to a lane there.  64 of 1 to 16384 positions 146 us, 65 of them 153; one of 50000 beside 63 of 500 107 us, beside
+// 64 of 500, as many shares for each, 310.
 inline bool alike(const Attention& a) { return a.sequences > 1 && a.sequences <= 64; }
 inline Shares shares_of(const Attention& a, int64_t tiles, int rows, bool few) {
     const int64_t seen = a.window ? std::min(a.max_length, a.window + a.max_new) : a.max_length;
@@ -79,9 +81,9 @@ int launch_tiles(adadim_ctx* ctx, const Attention& a) {
     return ADADIM_OK;
 }
 
-// Up to 256 rows a sequence and head by tiles of 16, which read a cache once for each 16 rows but leave no wave without rows and share it finely:
+// One form for all sequences of a call.  Up to 256 rows a sequence and head by tiles of 16, which read a cache once for each 16 rows but leave no wave without rows and share it finely:
 // 2 x 4000 positions, 256 rows, 32 heads 51 us by them, 54 to 60 by tiles of 256; 1000 rows 160 and 125; 20000 positions, 8 heads, 256 rows 54 and
-// 83, 1024 rows 158 and 112.
+// 83, 1024 rows 158 and 112.  A chunk of 2048 tokens over 6144 positions beside 63 decoding sequences of 1024 to 8192, 64 heads over 8: 780 us, apart 568 and 85.
 template <class T, int D>
 int launch_head(adadim_ctx* ctx, const Attention& a) {
     return a.max_new * a.group <= 256 ? launch_few<T, D>(ctx, a) : launch_tiles<T, D>(ctx, a);

@@ -7,12 +7,13 @@
 // elements h D/2 + 8 s ..; values [tile jj][step][half][row r], with row r of tile jj the element (D/16) (r % 16) + (D/32) (r / 16) + jj, and
 // the step's positions 4 h .. and 8 + 4 h .. of 16 as S^T leaves them in a lane of half h.
 //
-// Bound by vector and matrix instructions together: of the 1000 clocks that a record takes a wave (two waves a SIMD, 2.1 GHz) the matrix pipe is
-// busy 512 and the vector unit about 500 (16 exponentials, 16 sums, 16 fma, 8 roundings, maxima, its share of the conversion).  4096 tokens into an
-// empty cache, 32 heads of 128: 148 us, 930 TFLOP/s; 2 x 2048 tokens over 16384, 64 heads over 8: 1389 us, 1070 TFLOP/s.  What did not
-// help there (that second case, beside 1420 to 1490 as the cards went): scores one record ahead in a wave, 1850 (in order or left to the
-// compiler); operands read from LDS ahead of use, 1500; waves' priorities, 1490; workgroups of six waves, three a SIMD, 1940, of four 1600;
-// one buffer for two, 1480.  Every wave converting for itself, 64 rows of 16-row tiles: 5400.
+// Neither unit is full: over the launch of chunks below the matrix pipe is busy 48 % and the vector unit 46 % of the clocks (16 exponentials, 16 sums,
+// 16 fma, 8 roundings, maxima of a record and its share of the conversion), and waves wait 30 % of their time, for LDS and for each other: within
+// a wave products and weights follow one another, and the SIMD's other wave does not fill the gaps.  4096 tokens into an empty cache, 32 heads of 128:
+// 147 us, 935 TFLOP/s; 2 x 2048 tokens over 16384, 64 heads over 8: 1375 us, 1080 TFLOP/s.  Heads of 64: 107 and 865 us (vector unit 65 %), of
+// 256, whose stages have one buffer: 331 and 2680 (waits 61 %).  What did not help there (the chunks, beside 1420 to 1490 as the cards went):
+// scores one record ahead in a wave, 1850 (in order or left to the compiler); operands read from LDS ahead of use, 1500; waves' priorities, 1490;
+// workgroups of six waves, three a SIMD, 1940, of four 1600; one buffer for two, 1480.  Every wave converting for itself, 64 rows of 16-row tiles: 5400.
 #pragma once
 
 #include "mx4_attention.h"

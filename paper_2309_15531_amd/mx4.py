@@ -228,7 +228,8 @@ class CachePages:
 
 
 class Mx4Cache:
-    """A layer's keys and values, `heads` heads of `dim` elements, 4.25 bits each: 4.25 KB a token for 32 heads of 128, where fp16 takes 16."""
+    """A layer's keys and values, `heads` heads of `dim` elements, filled up to 64, 128 or 256 and 4.25 bits each: 4.25 KB a token for 32 heads of 128,
+    where fp16 takes 16."""
 
     def __init__(self, pages: CachePages, heads: int, dim: int):
         self.ctx, self.pages, self.heads, self.dim = pages.ctx, pages, heads, dim
@@ -247,7 +248,7 @@ class Mx4Cache:
     def attend(self, Q, offsets, Y=None, scale: float | None = None, causal: bool = True, window: int = 0, max_new: int = 0, max_length: int = 0):
         """Attention of the rows of Q [tokens, query heads * dim] (fp16 or bf16), whose keys and values are stored already, to their sequences.
         max_new, max_length: the most new rows and positions of a sequence, where the host knows them (a decoding step: 1); they lay the
-        launch out, the result does not depend on them.  Rows in no sequence are left as they are (without Y: not initialized)."""
+        launch out for all sequences, the result does not depend on them.  Rows in no sequence are left as they are (without Y: not initialized)."""
         if Y is None:
             Y = _output(self.ctx, tuple(Q.shape), Q.dtype, Q.device)
         p = self.pages
